@@ -178,6 +178,126 @@ fp_status fp_sparse_attn(const fp_shape *shape, const void *q, const void *k,
 fp_status fp_sparse_attn_noalloc(const fp_shape *shape, const void *q, const void *k,
                                  const void *v, const fp_indices *idx, void *o, void *stream);
 
+/* ---------------------------------------------------------------------------------------
+ * After the prefill: a paged cache of keys and values, and the attention of the next tokens.
+ *
+ * A cache holds `layers` pools of `num_pages` pages of `page` tokens, shared by num_slots
+ * sequences ("slots").  The bookkeeping is one for all layers and lives on the device, so the
+ * calls of a decoding loop can be captured into a HIP graph: lengths and page numbers are read
+ * by the kernels, and only the lists of slots are host arrays.
+ *   k    : bf16 [layers][num_pages][Hkv][page][d]
+ *   v    : bf16 [layers][num_pages][Hkv][page / 16][d][16] -- steps of 16 tokens, transposed:
+ *          the operand of the matrix product that reads them, so a step is one contiguous copy
+ *   meta : int32, fp_cache_meta_size elements, 8-byte aligned:
+ *          state [8]                       pages in use, FP_CACHE_* error bits, 0, ...
+ *          used  [2 * ceil(num_pages/64)]  bit p % 32 of word p / 32: page p is in use
+ *          len   [num_slots]               tokens of a slot (0: empty)
+ *          ref   [num_pages]               slots that hold a page
+ *          table [num_slots][max_pages]    a slot's pages in order, -1 past its last one
+ * Two slots may hold the same page (fp_cache_fork).  A page is written only while one slot holds
+ * it: fp_cache_reserve first gives a slot that is about to grow a copy of a shared last page that
+ * is not full.  Pages are handed out lowest number first, so the state after a series of calls
+ * does not depend on how the GPU ordered their work.
+ *
+ * What only the device knows cannot be refused by the host.  A reserve that finds too few pages
+ * or too short a table row changes nothing and sets an error bit in state[1]; while a bit is set
+ * every call that changes the cache does nothing.  The caller reads the word when it synchronises
+ * anyway and clears it by storing 0. */
+#define FP_CACHE_FULL 1       /* fp_cache_reserve: fewer free pages than the call needs        */
+#define FP_CACHE_TOO_LONG 2   /* fp_cache_reserve: a slot would pass max_pages pages           */
+#define FP_CACHE_SHARED 4     /* fp_cache_write: tokens on a page that is not the slot's alone */
+                              /* (not reserved), which were left out                           */
+
+#define FP_MAX_CACHE_LIST 256         /* slots per call                                   */
+#define FP_MAX_CACHE_PAGES (1 << 22)  /* largest num_pages                                */
+#define FP_MAX_QUERIES 16             /* query tokens per sequence in fp_decode_attn      */
+
+typedef struct fp_cache {
+  int32_t layers;        /* >= 1                                                          */
+  int32_t num_pages;     /* pages per layer, 1..FP_MAX_CACHE_PAGES                        */
+  int32_t num_kv_heads;  /* Hkv, 1..1024                                                  */
+  int32_t head_dim;      /* d in {64, 128}                                                */
+  int32_t page;          /* tokens per page: 16, 32, 64, 128 or 256                       */
+  int32_t num_slots;     /* 1..65536                                                      */
+  int32_t max_pages;     /* pages a slot can hold: its capacity is max_pages * page       */
+                         /* tokens, at most 2^26; num_slots * max_pages < 2^31            */
+  void *k, *v;           /* device pools, 16-byte aligned                                 */
+  int32_t *meta;         /* device bookkeeping                                            */
+} fp_cache;
+
+/* int32 elements of fp_cache.meta (k, v and meta are not looked at).  Host only. */
+fp_status fp_cache_meta_size(const fp_cache *cache, size_t *elems);
+
+/* Device workspace bytes of fp_cache_reserve and fp_cache_compact: the list of page copies
+ * that the call makes, and for compact the new number of every page.  Host only. */
+fp_status fp_cache_workspace_size(const fp_cache *cache, size_t *bytes);
+
+/* Every slot empty, every page free, no error.  The pools are left as they are. */
+fp_status fp_cache_init(const fp_cache *cache, void *stream);
+
+/* Room for counts[i] >= 0 more tokens in slots[i], i < n (HOST arrays; 1 <= n <=
+ * FP_MAX_CACHE_LIST, slots distinct): len grows by counts[i], and new pages, lowest free number
+ * first, go to the slots in list order.  A slot that grows, whose last page is not full and
+ * held by others too, gets a copy of it (in every layer) as its first new page; of several
+ * such slots in the list, the last holder of a page keeps it.  The tokens themselves are
+ * written by fp_cache_write.  All or nothing (see FP_CACHE_FULL, FP_CACHE_TOO_LONG). */
+fp_status fp_cache_reserve(const fp_cache *cache, int32_t n, const int32_t *slots,
+                           const int32_t *counts, void *ws, size_t ws_bytes, void *stream);
+
+/* Keys and values of one layer for the last cu[i+1] - cu[i] tokens of slots[i] (HOST arrays,
+ * cu [n+1], cu[0] = 0, non-decreasing): rows cu[i] .. cu[i+1]-1 of k and v, each [Hkv][d] bf16
+ * contiguous, k_stride and v_stride elements from one token to the next (>= Hkv * d, a multiple
+ * of 8; pointers 16-byte aligned).  Rows beyond a slot's length are left out. */
+fp_status fp_cache_write(const fp_cache *cache, int32_t layer, int32_t n, const int32_t *slots,
+                         const int32_t *cu, const void *k, int64_t k_stride, const void *v,
+                         int64_t v_stride, void *stream);
+
+/* dst[i] becomes a copy of src[i] that shares its pages (HOST arrays; dst distinct, none of
+ * them in src; src may repeat).  What dst[i] held before is given back. */
+fp_status fp_cache_fork(const fp_cache *cache, int32_t n, const int32_t *src, const int32_t *dst,
+                        void *stream);
+
+/* slots[i] keeps its first min(len, lens[i]) tokens, lens[i] >= 0 (HOST arrays, slots
+ * distinct); pages past them are given back, and are free once no slot holds them.  lens =
+ * NULL frees the slots. */
+fp_status fp_cache_truncate(const fp_cache *cache, int32_t n, const int32_t *slots,
+                            const int32_t *lens, void *stream);
+
+/* The pages in use become pages 0 .. state[0]-1: the k-th free page below that number takes the
+ * content (in every layer), holders and place in every table of the k-th page in use at or above
+ * it.  The pools can then be cut to state[0] pages, or another cache laid behind them. */
+fp_status fp_cache_compact(const fp_cache *cache, void *ws, size_t ws_bytes, void *stream);
+
+/* One batch of fp_decode_attn. */
+typedef struct fp_decode {
+  int32_t batch;               /* sequences, 1..FP_MAX_CACHE_LIST                            */
+  const int32_t *slots;        /* HOST [batch]: the cache slot of a sequence, or -1: none    */
+  int32_t num_q_heads;         /* Hq, a multiple of Hkv                                      */
+  int32_t queries;             /* query tokens per sequence, 1..FP_MAX_QUERIES: its last     */
+                               /* `queries` tokens, whose keys and values are in the cache   */
+  int32_t groups;              /* 0, or groups of consecutive sequences that share a prefix  */
+  const int32_t *group_start;  /* HOST [groups+1], 0 .. batch ascending (groups > 0)         */
+  const int32_t *prefix_lens;  /* HOST [groups]: tokens at the start of every sequence of    */
+                               /* the group that are the same (>= 0)                         */
+  float softmax_scale;         /* 0 => 1/sqrt(d)                                             */
+} fp_decode;
+
+/* Device workspace bytes of fp_decode_attn: partial results of key ranges.  Host only. */
+fp_status fp_decode_workspace_size(const fp_cache *cache, const fp_decode *batch, size_t *bytes);
+
+/* Attention of each sequence's last `queries` tokens over the whole sequence: query t (of
+ * `queries`) of a sequence of n tokens attends to its keys 0 .. n - queries + t.  Row b *
+ * queries + t of q and o, each row [Hq][d] bf16 contiguous, q_stride elements from one row of q
+ * to the next (>= Hq * d, a multiple of 8); rows of o are contiguous.  A query with no key (an
+ * empty slot, slot -1, more queries than tokens) gets 0.  Only what the visible tokens hold
+ * matters: what lies in a page past its tokens, or in tokens after a query, does not reach it.
+ * The keys and values of a group's prefix are read once for all of its sequences, from the pages
+ * of the first one that is not empty; if a sequence of the group is shorter, as much of the
+ * prefix as every query of the group sees. */
+fp_status fp_decode_attn(const fp_cache *cache, const fp_decode *batch, int32_t layer,
+                         const void *q, int64_t q_stride, void *o, void *ws, size_t ws_bytes,
+                         void *stream);
+
 /* Static description of a status code. */
 const char *fp_status_string(fp_status status);
 

@@ -49,6 +49,21 @@ class FpIndices(ctypes.Structure):
                 ("softmax_scale", ctypes.c_float)]
 
 
+class FpCache(ctypes.Structure):
+    _fields_ = [("layers", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+                ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("page", ctypes.c_int32), ("num_slots", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("meta", ctypes.c_void_p)]
+
+
+class FpDecode(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("slots", ctypes.c_void_p),
+                ("num_q_heads", ctypes.c_int32), ("queries", ctypes.c_int32),
+                ("groups", ctypes.c_int32), ("group_start", ctypes.c_void_p),
+                ("prefix_lens", ctypes.c_void_p), ("softmax_scale", ctypes.c_float)]
+
+
 _lib_handle = None
 
 
@@ -71,13 +86,28 @@ def lib() -> ctypes.CDLL:
         h.fp_select.argtypes = [S, vp, vp, P, X, vp, ctypes.c_size_t, vp]
         h.fp_sparse_attn.argtypes = [S, vp, vp, vp, X, vp, vp, ctypes.c_size_t, vp]
         h.fp_sparse_attn_noalloc.argtypes = [S, vp, vp, vp, X, vp, vp]
+        C, D = ctypes.POINTER(FpCache), ctypes.POINTER(FpDecode)
+        i32, i64 = ctypes.c_int32, ctypes.c_int64
+        h.fp_cache_meta_size.argtypes = [C, sz]
+        h.fp_cache_workspace_size.argtypes = [C, sz]
+        h.fp_cache_init.argtypes = [C, vp]
+        h.fp_cache_reserve.argtypes = [C, i32, vp, vp, vp, ctypes.c_size_t, vp]
+        h.fp_cache_write.argtypes = [C, i32, i32, vp, vp, vp, i64, vp, i64, vp]
+        h.fp_cache_fork.argtypes = [C, i32, vp, vp, vp]
+        h.fp_cache_truncate.argtypes = [C, i32, vp, vp, vp]
+        h.fp_cache_compact.argtypes = [C, vp, ctypes.c_size_t, vp]
+        h.fp_decode_workspace_size.argtypes = [C, D, sz]
+        h.fp_decode_attn.argtypes = [C, D, i32, vp, i64, vp, vp, ctypes.c_size_t, vp]
         h.fp_status_string.argtypes = [ctypes.c_int]
         h.fp_status_string.restype = ctypes.c_char_p
         h.fp_last_error.argtypes = []
         h.fp_last_error.restype = ctypes.c_char_p
         for name in ("fp_indices_size", "fp_select_workspace_size", "fp_attn_workspace_size",
                      "fp_attn_workspace_preferred", "fp_validate", "fp_select", "fp_sparse_attn",
-                     "fp_sparse_attn_noalloc"):
+                     "fp_sparse_attn_noalloc", "fp_cache_meta_size", "fp_cache_workspace_size",
+                     "fp_cache_init", "fp_cache_reserve", "fp_cache_write", "fp_cache_fork",
+                     "fp_cache_truncate", "fp_cache_compact", "fp_decode_workspace_size",
+                     "fp_decode_attn"):
             getattr(h, name).restype = ctypes.c_int
         _lib_handle = h
     return _lib_handle
@@ -363,3 +393,9 @@ def masks_from_indices(indices: Indices):
                 m[I, kb_idx[base:base + c]] = True
             out[(s, h)] = m
     return out
+
+
+from .cache import (CACHE_FULL, CACHE_SHARED, CACHE_TOO_LONG, MAX_CACHE_LIST,  # noqa: E402,F401
+                    MAX_QUERIES, Cache, CacheError, DecodeBatch, cache_compact, cache_fork,
+                    cache_free, cache_init, cache_reserve, cache_truncate, cache_workspace_size,
+                    cache_write, decode_attn, decode_workspace_size)

@@ -1,0 +1,246 @@
+"""Paged cache of keys and values, and the attention of the next tokens over it.
+
+Marshalling only, as in the rest of the binding: a `Cache` holds the tensors of fp_cache, a
+`DecodeBatch` the host arrays of fp_decode with their pointers, and every call enqueues the
+library's kernels on the current stream (or `stream`) without waiting for the GPU.
+
+    cache = Cache(layers, num_pages, num_kv_heads, head_dim, num_slots, max_pages)
+    cache_reserve(cache, [0], [len(prompt)])          # once for all layers
+    cache_write(cache, layer, k, v, [0], [0, len(prompt)])    # per layer, beside the prefill
+    cache_fork(cache, [0] * 7, range(1, 8))           # eight samples of one prompt
+    batch = DecodeBatch(range(8), num_q_heads, group_start=[0, 8], prefix_lens=[len(prompt)])
+    # per step: cache_reserve(cache, slots, 1), then per layer cache_write and
+    o = decode_attn(q, cache, layer, batch)
+    cache_free(cache, slots); cache_compact(cache)
+"""
+from __future__ import annotations
+
+import ctypes
+
+import numpy as np
+
+from . import FpCache, FpDecode, _check, _check_tensor, _stream_ptr, _workspace, lib
+
+CACHE_FULL, CACHE_TOO_LONG, CACHE_SHARED = 1, 2, 4
+MAX_CACHE_LIST = 256
+MAX_QUERIES = 16
+
+
+class CacheError(RuntimeError):
+    """What the device refused (CACHE_* bits), found by Cache.check."""
+
+    def __init__(self, bits: int):
+        self.bits = bits
+        names = [n for b, n in ((CACHE_FULL, "too few free pages"),
+                                (CACHE_TOO_LONG, "a sequence passes max_pages pages"),
+                                (CACHE_SHARED, "tokens written without a reserve")) if bits & b]
+        super().__init__("; ".join(names) or f"error bits {bits}")
+
+
+def _ints(x, name, n=None):
+    """x as a contiguous int32 host array of n elements."""
+    a = np.ascontiguousarray(x if isinstance(x, np.ndarray) else list(x))
+    if a.dtype != np.int32:
+        if a.size and not np.issubdtype(a.dtype, np.integer):
+            raise ValueError(f"{name} must hold integers")
+        if a.size and (a.min() < -2 ** 31 or a.max() >= 2 ** 31):
+            raise ValueError(f"{name} must fit 32 bits")
+        a = a.astype(np.int32)
+    if a.ndim != 1 or (n is not None and a.size != n):
+        raise ValueError(f"{name} must be a list of {n if n is not None else 'any number of'} "
+                         f"integers, got shape {a.shape}")
+    return a
+
+
+def _ptr(a):
+    return ctypes.c_void_p(a.ctypes.data)
+
+
+class Cache:
+    """A cache and its device tensors: k [layers, num_pages, Hkv, page, d] and v [layers,
+    num_pages, Hkv, page / 16, d, 16] in bf16, and the int32 bookkeeping `meta`, of which
+    state, used, lens, refs and table are views.  Without k, v and meta they are allocated, and
+    the cache is empty; with them the cache is what they hold."""
+
+    def __init__(self, layers, num_pages, num_kv_heads, head_dim, num_slots, max_pages, page=64,
+                 device="cuda", k=None, v=None, meta=None):
+        import torch
+        self.c = FpCache(int(layers), int(num_pages), int(num_kv_heads), int(head_dim),
+                         int(page), int(num_slots), int(max_pages), None, None, None)
+        n = ctypes.c_size_t()
+        _check(lib().fp_cache_meta_size(ctypes.byref(self.c), ctypes.byref(n)),
+               "fp_cache_meta_size")
+        shape_k = (layers, num_pages, num_kv_heads, page, head_dim)
+        shape_v = (layers, num_pages, num_kv_heads, page // 16, head_dim, 16)
+        given = [x is not None for x in (k, v, meta)]
+        if any(given) and not all(given):
+            raise ValueError("k, v and meta come together")
+        if not any(given):
+            k = torch.empty(shape_k, dtype=torch.bfloat16, device=device)
+            v = torch.empty(shape_v, dtype=torch.bfloat16, device=device)
+            meta = torch.empty(n.value, dtype=torch.int32, device=device)
+        for name, x, shape, dtype in (("k", k, shape_k, torch.bfloat16),
+                                      ("v", v, shape_v, torch.bfloat16),
+                                      ("meta", meta, (n.value,), torch.int32)):
+            _check_tensor(x, name, len(shape), dtype)
+            if tuple(x.shape) != tuple(shape):
+                raise ValueError(f"{name} has shape {tuple(x.shape)}; the cache needs {shape}")
+        self.k, self.v, self.meta = k, v, meta
+        self.c.k, self.c.v, self.c.meta = k.data_ptr(), v.data_ptr(), meta.data_ptr()
+        words = 2 * -(-int(num_pages) // 64)
+        sizes = [8, words, int(num_slots), int(num_pages), int(num_slots) * int(max_pages)]
+        self.state, self.used, self.lens, self.refs, table = torch.split(meta, sizes)
+        self.table = table.view(int(num_slots), int(max_pages))
+        self.ref = ctypes.byref(self.c)
+        if not any(given):
+            cache_init(self)
+
+    def check(self):
+        """Waits for the calls so far; if the device refused one since the last check, clears
+        the error, so that calls work again, and raises CacheError."""
+        bits = int(self.state[1].item())
+        if bits:
+            self.state[1].zero_()
+            raise CacheError(bits)
+
+
+def cache_workspace_size(cache: Cache) -> int:
+    """Workspace bytes of cache_reserve and cache_compact."""
+    out = ctypes.c_size_t()
+    _check(lib().fp_cache_workspace_size(cache.ref, ctypes.byref(out)),
+           "fp_cache_workspace_size")
+    return out.value
+
+
+def _cache_workspace(cache, workspace, stream):
+    if workspace is None:
+        return _workspace(cache_workspace_size(cache), cache.meta.device, stream)
+    return workspace
+
+
+def cache_init(cache: Cache, stream=None):
+    """Every slot empty, every page free."""
+    _check(lib().fp_cache_init(cache.ref, _stream_ptr(stream)), "fp_cache_init")
+
+
+def cache_reserve(cache: Cache, slots, counts, workspace=None, stream=None):
+    """Room for counts[i] (or the same count for all) more tokens in slots[i], once for all
+    layers.  A shared last page that is not full is copied first.  If pages run out or a slot
+    would grow past max_pages nothing changes, and Cache.check raises."""
+    slots = _ints(slots, "slots")
+    counts = (np.full(slots.size, counts, np.int32) if np.ndim(counts) == 0
+              else _ints(counts, "counts", slots.size))
+    ws = _cache_workspace(cache, workspace, stream)
+    _check(lib().fp_cache_reserve(cache.ref, slots.size, _ptr(slots), _ptr(counts),
+                                  ctypes.c_void_p(ws.data_ptr()), ws.numel(),
+                                  _stream_ptr(stream)), "fp_cache_reserve")
+
+
+def _check_rows(x, name, heads, d):
+    """A [T, heads, d] bf16 tensor whose rows are contiguous, any stride between them."""
+    import torch
+    if not (x.is_cuda and x.dtype == torch.bfloat16 and x.dim() == 3
+            and tuple(x.shape[1:]) == (heads, d)
+            and (x.shape[0] == 0 or (x.stride(2) == 1 and x.stride(1) == d))):
+        raise ValueError(f"{name} must be a bf16 CUDA tensor [T, {heads}, {d}] with contiguous "
+                         "rows")
+    return x.stride(0) if x.shape[0] > 1 else heads * d
+
+
+def cache_write(cache: Cache, layer, k, v, slots, cu_seqlens, stream=None):
+    """Keys and values of `layer` for the last cu_seqlens[i+1] - cu_seqlens[i] tokens of
+    slots[i].  k, v: [T, Hkv, d] bf16, rows contiguous (slices of a fused projection do)."""
+    slots = _ints(slots, "slots")
+    cu = _ints(cu_seqlens, "cu_seqlens", slots.size + 1)
+    ks = _check_rows(k, "k", cache.c.num_kv_heads, cache.c.head_dim)
+    vs = _check_rows(v, "v", cache.c.num_kv_heads, cache.c.head_dim)
+    if k.shape[0] != cu[-1] or v.shape[0] != cu[-1]:
+        raise ValueError(f"k and v have {k.shape[0]} and {v.shape[0]} rows; cu_seqlens ends "
+                         f"at {cu[-1]}")
+    _check(lib().fp_cache_write(cache.ref, int(layer), slots.size, _ptr(slots), _ptr(cu),
+                                ctypes.c_void_p(k.data_ptr()), ks,
+                                ctypes.c_void_p(v.data_ptr()), vs, _stream_ptr(stream)),
+           "fp_cache_write")
+
+
+def cache_fork(cache: Cache, src, dst, stream=None):
+    """dst[i] becomes a copy of src[i] that shares its pages; what it held is given back."""
+    src = _ints(src, "src")
+    dst = _ints(dst, "dst", src.size)
+    _check(lib().fp_cache_fork(cache.ref, src.size, _ptr(src), _ptr(dst), _stream_ptr(stream)),
+           "fp_cache_fork")
+
+
+def cache_truncate(cache: Cache, slots, lens, stream=None):
+    """slots[i] keeps its first lens[i] tokens (drafts that were not accepted, for one)."""
+    slots = _ints(slots, "slots")
+    lens = _ints(lens, "lens", slots.size)
+    _check(lib().fp_cache_truncate(cache.ref, slots.size, _ptr(slots), _ptr(lens),
+                                   _stream_ptr(stream)), "fp_cache_truncate")
+
+
+def cache_free(cache: Cache, slots, stream=None):
+    """The slots become empty; their pages are free once no other slot holds them."""
+    slots = _ints(slots, "slots")
+    _check(lib().fp_cache_truncate(cache.ref, slots.size, _ptr(slots), None,
+                                   _stream_ptr(stream)), "fp_cache_truncate")
+
+
+def cache_compact(cache: Cache, workspace=None, stream=None):
+    """The pages in use become pages 0 .. state[0]-1, in every layer and table."""
+    ws = _cache_workspace(cache, workspace, stream)
+    _check(lib().fp_cache_compact(cache.ref, ctypes.c_void_p(ws.data_ptr()), ws.numel(),
+                                  _stream_ptr(stream)), "fp_cache_compact")
+
+
+class DecodeBatch:
+    """fp_decode and the host arrays that it points to: sequence b is the cache slot slots[b]
+    (-1: none) with its last `queries` tokens as queries; sequences group_start[g] ..
+    group_start[g+1]-1 begin with the same prefix_lens[g] tokens."""
+
+    def __init__(self, slots, num_q_heads, queries=1, group_start=None, prefix_lens=None,
+                 softmax_scale=0.0):
+        self.slots = _ints(slots, "slots")
+        self.group_start = self.prefix_lens = None
+        if (group_start is None) != (prefix_lens is None):
+            raise ValueError("group_start and prefix_lens come together")
+        self.c = FpDecode(self.slots.size, _ptr(self.slots), int(num_q_heads), int(queries), 0,
+                          None, None, float(softmax_scale))
+        if group_start is not None:
+            self.prefix_lens = _ints(prefix_lens, "prefix_lens")
+            self.group_start = _ints(group_start, "group_start", self.prefix_lens.size + 1)
+            self.c.groups = self.prefix_lens.size
+            self.c.group_start = _ptr(self.group_start)
+            self.c.prefix_lens = _ptr(self.prefix_lens)
+        self.ref = ctypes.byref(self.c)
+
+
+def decode_workspace_size(cache: Cache, batch: DecodeBatch) -> int:
+    """Workspace bytes of decode_attn."""
+    out = ctypes.c_size_t()
+    _check(lib().fp_decode_workspace_size(cache.ref, batch.ref, ctypes.byref(out)),
+           "fp_decode_workspace_size")
+    return out.value
+
+
+def decode_attn(q, cache: Cache, layer, batch: DecodeBatch, out=None, workspace=None,
+                stream=None):
+    """Attention of the batch's query tokens over their sequences.  q: [batch * queries, Hq, d]
+    bf16, rows contiguous, sequence by sequence; returns o of the same shape."""
+    import torch
+    T, hq, d = batch.c.batch * batch.c.queries, batch.c.num_q_heads, cache.c.head_dim
+    stride = _check_rows(q, "q", hq, d)
+    if q.shape[0] != T:
+        raise ValueError(f"q has {q.shape[0]} rows; the batch has {T} query tokens")
+    if out is None:
+        out = _workspace(2 * T * hq * d, q.device, stream).view(torch.bfloat16).view(T, hq, d)
+    _check_tensor(out, "out", 3)
+    if tuple(out.shape) != (T, hq, d):
+        raise ValueError(f"out has shape {tuple(out.shape)}; the batch needs {(T, hq, d)}")
+    if workspace is None:
+        workspace = _workspace(decode_workspace_size(cache, batch), q.device, stream)
+    _check(lib().fp_decode_attn(cache.ref, batch.ref, int(layer), ctypes.c_void_p(q.data_ptr()),
+                                stride, ctypes.c_void_p(out.data_ptr()),
+                                ctypes.c_void_p(workspace.data_ptr()), workspace.numel(),
+                                _stream_ptr(stream)), "fp_decode_attn")
+    return out

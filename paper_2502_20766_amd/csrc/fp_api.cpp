@@ -219,6 +219,134 @@ size_t plan_split(const fp::SeqTable &st, int hq, int hkv, int d, int block, siz
   return layout(extra, nullptr);
 }
 
+bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+
+// Sizes of a cache; `view` (or null) gets the kernels' view of it.
+fp_status check_cache(const fp_cache *c, fp::CacheView *view) {
+  if (!c) return FP_ERR_INVALID_ARG;
+  if (c->layers < 1 || c->num_pages < 1 || c->num_kv_heads < 1 || c->head_dim < 1 ||
+      c->page < 1 || c->num_slots < 1 || c->max_pages < 1)
+    return FP_ERR_INVALID_ARG;
+  if (c->head_dim != 64 && c->head_dim != 128) return FP_ERR_UNSUPPORTED;
+  if (c->page < 16 || c->page > 256 || (c->page & (c->page - 1))) return FP_ERR_UNSUPPORTED;
+  if (c->num_pages > FP_MAX_CACHE_PAGES || c->num_kv_heads > 1024 || c->num_slots > 65536)
+    return FP_ERR_UNSUPPORTED;
+  if ((int64_t)c->max_pages * c->page > ((int64_t)1 << 26)) return FP_ERR_UNSUPPORTED;
+  if ((int64_t)c->max_pages * c->num_slots > 0x7FFFFFFF) return FP_ERR_UNSUPPORTED;
+  if (!view) return FP_OK;
+  if (!c->k || !c->v || !c->meta || !aligned16(c->k) || !aligned16(c->v) ||
+      ((uintptr_t)c->meta & 7))
+    return FP_ERR_INVALID_ARG;
+  fp::CacheView &w = *view;
+  w.k = (uint16_t *)c->k;
+  w.v = (uint16_t *)c->v;
+  w.layers = c->layers;
+  w.pages = c->num_pages;
+  w.hkv = c->num_kv_heads;
+  w.d = c->head_dim;
+  w.page = c->page;
+  w.page_shift = __builtin_ctz((unsigned)c->page);
+  w.slots = c->num_slots;
+  w.max_pages = c->max_pages;
+  w.words = (c->num_pages + 63) / 64;
+  w.state = c->meta;
+  w.used = (unsigned long long *)(c->meta + 8);
+  w.len = c->meta + 8 + 2 * (size_t)w.words;
+  w.ref = w.len + w.slots;
+  w.table = w.ref + w.pages;
+  return FP_OK;
+}
+
+// Workspace of reserve and compact: the number of copies, their pages, and every page's new
+// number.
+size_t copies_layout(const fp_cache *c, char *base, fp::PageCopies *w) {
+  const size_t list = align_up(4 * (size_t)c->num_pages);
+  if (w) {
+    w->count = (int32_t *)base;
+    w->src = (int32_t *)(base + kAlign);
+    w->dst = (int32_t *)(base + kAlign + list);
+    w->renamed = (int32_t *)(base + kAlign + 2 * list);
+  }
+  return kAlign + 3 * list;
+}
+
+// Slot numbers of one call, distinct and in range; `seen` holds the slots so far.
+struct SlotSet {
+  uint64_t bits[65536 / 64] = {};
+  bool add(int32_t s) {
+    const uint64_t bit = (uint64_t)1 << (s & 63);
+    const bool fresh = !(bits[s >> 6] & bit);
+    bits[s >> 6] |= bit;
+    return fresh;
+  }
+  bool has(int32_t s) const { return bits[s >> 6] >> (s & 63) & 1; }
+};
+
+fp_status check_slots(const fp_cache *c, int32_t n, const int32_t *slots, SlotSet *seen) {
+  if (n < 1 || !slots) return FP_ERR_INVALID_ARG;
+  if (n > FP_MAX_CACHE_LIST) return FP_ERR_UNSUPPORTED;
+  for (int i = 0; i < n; ++i) {
+    if (slots[i] < 0 || slots[i] >= c->num_slots) return FP_ERR_INVALID_ARG;
+    if (seen && !seen->add(slots[i])) return FP_ERR_INVALID_ARG;
+  }
+  return FP_OK;
+}
+
+// Units of a decoding batch: query rows, tiles of kDecodeRows rows, workspace.
+struct DecodeDims {
+  int G;                       // query heads per KV head
+  int rows;                    // rows of a sequence and KV head
+  int tiles;                   // their row tiles
+  bool shared;                 // some group has a prefix to share
+  size_t slots_p, slots_s;     // partial results
+  size_t bytes_p, bytes_s;
+};
+
+fp_status check_decode(const fp_cache *c, const fp_decode *b, DecodeDims *dm) {
+  const fp_status st = check_cache(c, nullptr);
+  if (st != FP_OK) return st;
+  if (!b || !b->slots || b->batch < 1 || b->num_q_heads < 1 || b->queries < 1 || b->groups < 0)
+    return FP_ERR_INVALID_ARG;
+  if (b->num_q_heads % c->num_kv_heads) return FP_ERR_INVALID_ARG;
+  if (b->batch > FP_MAX_CACHE_LIST || b->queries > FP_MAX_QUERIES || b->num_q_heads > 8192)
+    return FP_ERR_UNSUPPORTED;
+  if (!scale_ok(b->softmax_scale)) return FP_ERR_INVALID_ARG;
+  for (int i = 0; i < b->batch; ++i)
+    if (b->slots[i] < -1 || b->slots[i] >= c->num_slots) return FP_ERR_INVALID_ARG;
+  dm->G = b->num_q_heads / c->num_kv_heads;
+  dm->rows = dm->G * b->queries;
+  dm->tiles = (dm->rows + fp::kDecodeRows - 1) / fp::kDecodeRows;
+  dm->shared = false;
+  // cost of all key ranges, in tiles of 64 keys: an int32 in the kernels
+  const int64_t most = ((int64_t)c->max_pages * c->page + 63) / 64;
+  int64_t cost = (int64_t)b->batch * dm->tiles * most;
+  if (b->groups > 0) {
+    if (!b->group_start || !b->prefix_lens || b->groups > b->batch) return FP_ERR_INVALID_ARG;
+    if (b->group_start[0] != 0 || b->group_start[b->groups] != b->batch)
+      return FP_ERR_INVALID_ARG;
+    for (int g = 0; g < b->groups; ++g) {
+      const int m = b->group_start[g + 1] - b->group_start[g];
+      if (m < 1 || m > b->batch || b->prefix_lens[g] < 0) return FP_ERR_INVALID_ARG;
+      if (m > 1 && b->prefix_lens[g] > 0) {
+        dm->shared = true;
+        cost += ((int64_t)m * dm->rows / fp::kDecodeRows + 1) *
+                std::min(most, ((int64_t)b->prefix_lens[g] + 63) / 64);
+      }
+    }
+  }
+  if (cost * c->num_kv_heads > 0x7FFFFFFF) return FP_ERR_UNSUPPORTED;
+  const size_t wgs = fp::decode_wgs(c->head_dim), row = 4 * (size_t)(c->head_dim + 2);
+  dm->slots_s = wgs + (size_t)b->batch * c->num_kv_heads * dm->tiles;
+  dm->bytes_s = align_up(dm->slots_s * std::min(dm->rows, fp::kDecodeRows) * row);
+  // a group's row tiles start at (its first row) / kDecodeRows + its number
+  dm->slots_p = !dm->shared ? 0
+                            : wgs + (size_t)c->num_kv_heads *
+                                        ((size_t)b->batch * dm->rows / fp::kDecodeRows +
+                                         b->groups + 1);
+  dm->bytes_p = align_up(dm->slots_p * fp::kDecodeRows * row);
+  return FP_OK;
+}
+
 fp_status hip_fail(hipError_t e, const char *what) {
   snprintf(g_last_error, sizeof(g_last_error), "%s: %s", what, hipGetErrorString(e));
   return FP_ERR_HIP;
@@ -390,6 +518,212 @@ fp_status fp_sparse_attn_noalloc(const fp_shape *shape, const void *q, const voi
   const hipError_t e = fp::noalloc_scratch(&ws);
   if (e != hipSuccess) return hip_fail(e, "fp_sparse_attn_noalloc(scratch)");
   return fp_sparse_attn(shape, q, k, v, idx, o, ws, (size_t)FP_NOALLOC_SCRATCH_BYTES, stream);
+}
+
+fp_status fp_cache_meta_size(const fp_cache *cache, size_t *elems) {
+  const fp_status st = check_cache(cache, nullptr);
+  if (st != FP_OK) return st;
+  if (!elems) return FP_ERR_INVALID_ARG;
+  *elems = 8 + 2 * (((size_t)cache->num_pages + 63) / 64) + (size_t)cache->num_slots +
+           (size_t)cache->num_pages + (size_t)cache->num_slots * cache->max_pages;
+  return FP_OK;
+}
+
+fp_status fp_cache_workspace_size(const fp_cache *cache, size_t *bytes) {
+  const fp_status st = check_cache(cache, nullptr);
+  if (st != FP_OK) return st;
+  if (!bytes) return FP_ERR_INVALID_ARG;
+  *bytes = copies_layout(cache, nullptr, nullptr);
+  return FP_OK;
+}
+
+fp_status fp_cache_init(const fp_cache *cache, void *stream) {
+  fp::CacheView c;
+  const fp_status st = check_cache(cache, &c);
+  if (st != FP_OK) return st;
+  const hipError_t e = fp::launch_cache_init(c, (hipStream_t)stream);
+  return e == hipSuccess ? FP_OK : hip_fail(e, "fp_cache_init");
+}
+
+fp_status fp_cache_reserve(const fp_cache *cache, int32_t n, const int32_t *slots,
+                           const int32_t *counts, void *ws, size_t ws_bytes, void *stream) {
+  fp::CacheView c;
+  fp_status st = check_cache(cache, &c);
+  if (st != FP_OK) return st;
+  SlotSet seen;
+  if ((st = check_slots(cache, n, slots, &seen)) != FP_OK) return st;
+  if (!counts) return FP_ERR_INVALID_ARG;
+  fp::CacheList l;
+  l.n = n;
+  for (int i = 0; i < n; ++i) {
+    if (counts[i] < 0) return FP_ERR_INVALID_ARG;
+    l.slot[i] = slots[i];
+    l.num[i] = counts[i];
+  }
+  if (!ws) return FP_ERR_INVALID_ARG;
+  if (ws_bytes < copies_layout(cache, nullptr, nullptr)) return FP_ERR_WORKSPACE;
+  fp::PageCopies w;
+  copies_layout(cache, (char *)ws, &w);
+  const hipError_t e = fp::launch_cache_reserve(c, l, w, (hipStream_t)stream);
+  return e == hipSuccess ? FP_OK : hip_fail(e, "fp_cache_reserve");
+}
+
+fp_status fp_cache_write(const fp_cache *cache, int32_t layer, int32_t n, const int32_t *slots,
+                         const int32_t *cu, const void *k, int64_t k_stride, const void *v,
+                         int64_t v_stride, void *stream) {
+  fp::CacheView c;
+  fp_status st = check_cache(cache, &c);
+  if (st != FP_OK) return st;
+  SlotSet seen;
+  if ((st = check_slots(cache, n, slots, &seen)) != FP_OK) return st;
+  if (layer < 0 || layer >= cache->layers || !cu || cu[0] != 0) return FP_ERR_INVALID_ARG;
+  const int64_t row = (int64_t)cache->num_kv_heads * cache->head_dim;
+  fp::WriteArgs a;
+  a.list.n = n;
+  int64_t blocks = 0;
+  for (int i = 0; i < n; ++i) {
+    const int64_t m = (int64_t)cu[i + 1] - cu[i];
+    if (m < 0) return FP_ERR_INVALID_ARG;
+    a.list.slot[i] = slots[i];
+    a.list.num[i] = cu[i];
+    a.blk[i] = (int32_t)blocks;
+    if (m > 0) blocks += (m + 62) / 64 + 1;   // 64-token blocks that m tokens can touch
+  }
+  if (cu[n] == 0) return FP_OK;
+  if (!k || !v || !aligned16(k) || !aligned16(v) || k_stride < row || v_stride < row ||
+      k_stride % 8 || v_stride % 8)
+    return FP_ERR_INVALID_ARG;
+  a.list.num[n] = cu[n];
+  a.blk[n] = (int32_t)blocks;
+  a.k = (const uint16_t *)k;
+  a.v = (const uint16_t *)v;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.layer = layer;
+  const hipError_t e = fp::launch_cache_write(c, a, (hipStream_t)stream);
+  return e == hipSuccess ? FP_OK : hip_fail(e, "fp_cache_write");
+}
+
+fp_status fp_cache_fork(const fp_cache *cache, int32_t n, const int32_t *src, const int32_t *dst,
+                        void *stream) {
+  fp::CacheView c;
+  fp_status st = check_cache(cache, &c);
+  if (st != FP_OK) return st;
+  SlotSet seen;
+  if ((st = check_slots(cache, n, dst, &seen)) != FP_OK) return st;
+  if ((st = check_slots(cache, n, src, nullptr)) != FP_OK) return st;
+  for (int i = 0; i < n; ++i)
+    if (seen.has(src[i])) return FP_ERR_INVALID_ARG;
+  // destinations by source, at most kForkChildren to an item
+  fp::ForkArgs a;
+  int16_t order[FP_MAX_CACHE_LIST];
+  for (int i = 0; i < n; ++i) order[i] = (int16_t)i;
+  std::stable_sort(order, order + n, [&](int x, int y) { return src[x] < src[y]; });
+  a.items = 0;
+  for (int i = 0; i < n; ++i) {
+    const int32_t s = src[order[i]];
+    if (a.items == 0 || a.src[a.items - 1] != s ||
+        i - a.first[a.items - 1] == fp::kForkChildren) {
+      a.src[a.items] = s;
+      a.first[a.items++] = i;
+    }
+    a.dst[i] = dst[order[i]];
+  }
+  a.first[a.items] = n;
+  const hipError_t e = fp::launch_cache_fork(c, a, (hipStream_t)stream);
+  return e == hipSuccess ? FP_OK : hip_fail(e, "fp_cache_fork");
+}
+
+fp_status fp_cache_truncate(const fp_cache *cache, int32_t n, const int32_t *slots,
+                            const int32_t *lens, void *stream) {
+  fp::CacheView c;
+  fp_status st = check_cache(cache, &c);
+  if (st != FP_OK) return st;
+  SlotSet seen;
+  if ((st = check_slots(cache, n, slots, &seen)) != FP_OK) return st;
+  fp::CacheList l;
+  l.n = n;
+  for (int i = 0; i < n; ++i) {
+    if (lens && lens[i] < 0) return FP_ERR_INVALID_ARG;
+    l.slot[i] = slots[i];
+    l.num[i] = lens ? lens[i] : 0;
+  }
+  const hipError_t e = fp::launch_cache_truncate(c, l, (hipStream_t)stream);
+  return e == hipSuccess ? FP_OK : hip_fail(e, "fp_cache_truncate");
+}
+
+fp_status fp_cache_compact(const fp_cache *cache, void *ws, size_t ws_bytes, void *stream) {
+  fp::CacheView c;
+  const fp_status st = check_cache(cache, &c);
+  if (st != FP_OK) return st;
+  if (!ws) return FP_ERR_INVALID_ARG;
+  if (ws_bytes < copies_layout(cache, nullptr, nullptr)) return FP_ERR_WORKSPACE;
+  fp::PageCopies w;
+  copies_layout(cache, (char *)ws, &w);
+  const hipError_t e = fp::launch_cache_compact(c, w, (hipStream_t)stream);
+  return e == hipSuccess ? FP_OK : hip_fail(e, "fp_cache_compact");
+}
+
+fp_status fp_decode_workspace_size(const fp_cache *cache, const fp_decode *batch,
+                                   size_t *bytes) {
+  DecodeDims dm;
+  const fp_status st = check_decode(cache, batch, &dm);
+  if (st != FP_OK) return st;
+  if (!bytes) return FP_ERR_INVALID_ARG;
+  *bytes = dm.bytes_p + dm.bytes_s;
+  return FP_OK;
+}
+
+fp_status fp_decode_attn(const fp_cache *cache, const fp_decode *batch, int32_t layer,
+                         const void *q, int64_t q_stride, void *o, void *ws, size_t ws_bytes,
+                         void *stream) {
+  DecodeDims dm;
+  fp_status st = check_decode(cache, batch, &dm);
+  if (st != FP_OK) return st;
+  fp::CacheView c;
+  if ((st = check_cache(cache, &c)) != FP_OK) return st;
+  if (layer < 0 || layer >= cache->layers || !q || !o || !ws || !aligned16(q) || !aligned16(o) ||
+      !aligned16(ws))
+    return FP_ERR_INVALID_ARG;
+  if (q_stride < (int64_t)batch->num_q_heads * c.d || q_stride % 8) return FP_ERR_INVALID_ARG;
+  if (ws_bytes < dm.bytes_p + dm.bytes_s) return FP_ERR_WORKSPACE;
+  fp::DecodeArgs a;
+  memset(&a, 0, sizeof(a));
+  const int64_t pool = (int64_t)layer * c.pages * c.hkv * c.page * c.d;
+  a.k = c.k + pool;
+  a.v = c.v + pool;
+  a.len = c.len;
+  a.table = c.table;
+  a.q = (const uint16_t *)q;
+  a.o = (uint16_t *)o;
+  a.q_stride = q_stride;
+  a.part_p = (float *)ws;
+  a.part_s = (float *)((char *)ws + dm.bytes_p);
+  a.pages = c.pages;
+  a.hkv = c.hkv;
+  a.page_shift = c.page_shift;
+  a.max_pages = c.max_pages;
+  a.G = dm.G;
+  a.hq = batch->num_q_heads;
+  a.nq = batch->queries;
+  a.batch = batch->batch;
+  a.wgs = fp::decode_wgs(c.d);
+  a.scale_log2 = resolved_scale(batch->softmax_scale, c.d) * 1.4426950408889634f;
+  for (int i = 0; i < batch->batch; ++i) a.slot[i] = batch->slots[i];
+  if (batch->groups > 0) {
+    a.groups = batch->groups;
+    for (int g = 0; g < batch->groups; ++g) {
+      a.start[g] = (int16_t)batch->group_start[g];
+      a.prefix[g] = batch->prefix_lens[g];
+      for (int i = batch->group_start[g]; i < batch->group_start[g + 1]; ++i)
+        a.group[i] = (uint8_t)g;
+    }
+  } else {
+    a.groups = 1;              // one group with nothing shared
+  }
+  a.start[a.groups] = (int16_t)batch->batch;
+  const hipError_t e = fp::launch_decode_attn(a, c.d, (hipStream_t)stream);
+  return e == hipSuccess ? FP_OK : hip_fail(e, "fp_decode_attn");
 }
 
 const char *fp_status_string(fp_status status) {

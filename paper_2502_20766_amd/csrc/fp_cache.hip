@@ -1,0 +1,453 @@
+// The paged cache of keys and values: bookkeeping of its pages, and the copies that move tokens
+// and pages.
+//
+// All bookkeeping is on the device (fp_cache.meta), so that a decoding loop needs no host wait
+// and can be captured into a graph.  Free pages are a bitmap beside the reference counts: pages
+// are taken lowest number first by counting bits, and given back by clearing them, in any order
+// with the same result, so no list has to be kept in order.
+#include "fp_internal.h"
+
+namespace fp {
+namespace {
+
+constexpr int kPlanThreads = 1024;   // the single workgroup that hands out pages
+constexpr int kCopyUnits = 1024;     // 16-byte units of a page copied by one workgroup at a time
+constexpr int kCopyGrid = 2048;      // workgroups of a copy whose length the host cannot know
+
+struct __attribute__((aligned(16))) Unit {
+  uint32_t x[4];
+};
+
+// Exclusive prefix sum over the workgroup (kPlanThreads threads) and the total; `part` is
+// 17 ints of LDS.
+__device__ __forceinline__ int block_scan(int x, int *part, int &total) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  int sum = x;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int y = __shfl_up(sum, d);
+    if (lane >= d) sum += y;
+  }
+  __syncthreads();                   // earlier reads of `part` are done
+  if (lane == 63) part[w] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    int run = 0;
+    for (int i = 0; i < kPlanThreads / 64; ++i) {
+      const int y = part[i];
+      part[i] = run;
+      run += y;
+    }
+    part[kPlanThreads / 64] = run;
+  }
+  __syncthreads();
+  total = part[kPlanThreads / 64];
+  return part[w] + sum - x;
+}
+
+__device__ __forceinline__ int pages_of(int tokens, int shift) {
+  return (int)(((unsigned)tokens + (1u << shift) - 1) >> shift);
+}
+
+// One holder less of page p; its bit is cleared when it was the last.  Returns 1 then.
+__device__ __forceinline__ int drop_page(const CacheView &c, int p) {
+  if ((unsigned)p >= (unsigned)c.pages) return 0;
+  if (atomicSub(c.ref + p, 1) != 1) return 0;
+  atomicAnd(c.used + (p >> 6), ~(1ull << (p & 63)));
+  return 1;
+}
+
+// state[0] less `gone` summed over the workgroup's waves.
+__device__ __forceinline__ void count_freed(const CacheView &c, int gone) {
+#pragma unroll
+  for (int d = 32; d > 0; d /= 2) gone += __shfl_xor(gone, d);
+  if ((threadIdx.x & 63) == 0 && gone) atomicSub(c.state, gone);
+}
+
+__global__ __launch_bounds__(256) void cache_init(CacheView c) {
+  const int64_t n_zero = 8 + 2 * (int64_t)c.words + c.slots + c.pages;
+  const int64_t n = n_zero + (int64_t)c.slots * c.max_pages;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256)
+    c.state[i] = i < n_zero ? 0 : -1;
+}
+
+// ---- reserve: one workgroup decides, a second launch makes the copies.
+//
+// Slot i of the list needs ceil((len + num) / page) - ceil(len / page) pages, and one more when
+// its last page is not full and another slot will still hold it: with r holders, the first
+// r - 1 such slots of the list take copies.  The free pages, in ascending order, go to the
+// slots in list order; rank r among the free pages belongs to the slot whose range of the
+// prefix sums holds r, found by bisection.
+// Latency bound (one workgroup, a chain of about six loads).
+__global__ __launch_bounds__(kPlanThreads) void cache_reserve(CacheView c, CacheList l,
+                                                              PageCopies w) {
+  __shared__ int part[kPlanThreads / 64 + 1];
+  __shared__ int s_slot[FP_MAX_CACHE_LIST], s_held[FP_MAX_CACHE_LIST];
+  __shared__ int s_begin[FP_MAX_CACHE_LIST + 1], s_tail[FP_MAX_CACHE_LIST];
+  __shared__ int s_copy[FP_MAX_CACHE_LIST];      // index of the slot's copy, or -1
+  __shared__ int s_base[kPlanThreads];
+  __shared__ unsigned long long s_free[kPlanThreads];
+  const int tid = threadIdx.x;
+  const int used_pages = c.state[0], error = c.state[1];
+  if (error != 0) {
+    if (tid == 0) w.count[0] = 0;
+    return;
+  }
+  const bool mine = tid < l.n;
+  const int64_t room = (int64_t)c.max_pages << c.page_shift;
+  int slot = 0, len = 0, num = 0, held = 0, tail = -1, refs = 0;
+  bool bad = false;
+  if (mine) {
+    slot = l.slot[tid];
+    num = l.num[tid];
+    len = c.len[slot];
+    bad = len < 0 || (int64_t)len + num > room;
+    if (!bad) {
+      held = pages_of(len, c.page_shift);
+      if (num > 0 && (len & (c.page - 1))) {
+        tail = c.table[(int64_t)slot * c.max_pages + held - 1];
+        if ((unsigned)tail < (unsigned)c.pages) refs = c.ref[tail];
+        else tail = -1;
+      }
+    }
+    s_tail[tid] = tail;
+  }
+  int copy = 0;
+  if (__syncthreads_or(refs > 1)) {
+    if (refs > 1) {
+      int before = 0;
+      for (int j = 0; j < tid; ++j) before += s_tail[j] == tail;
+      copy = refs - before > 1;
+    }
+  }
+  const int need = mine && !bad ? pages_of(len + num, c.page_shift) - held + copy : 0;
+  int total, copies;
+  const int begin = block_scan(need, part, total);
+  const int at = block_scan(copy, part, copies);
+  const int too_long = __syncthreads_or(bad) ? FP_CACHE_TOO_LONG : 0;
+  const int full = total > c.pages - used_pages ? FP_CACHE_FULL : 0;
+  if (too_long | full) {
+    if (tid == 0) {
+      c.state[1] = too_long | full;
+      w.count[0] = 0;
+    }
+    return;
+  }
+  if (mine) {
+    s_slot[tid] = slot;
+    s_held[tid] = held - copy;
+    s_begin[tid] = begin;
+    s_copy[tid] = copy ? at : -1;
+    c.len[slot] = len + num;
+    if (copy) {
+      w.src[at] = tail;
+      atomicSub(c.ref + tail, 1);
+    }
+  }
+  if (tid == 0) {
+    s_begin[l.n] = total;
+    c.state[0] = used_pages + total;
+    w.count[0] = copies;
+  }
+  // free pages, 64 to a word, kPlanThreads words at a time; a wave takes a word, a lane a page
+  for (int w0 = 0, taken = 0; taken < total && w0 < c.words; w0 += kPlanThreads) {
+    const int word = w0 + tid;
+    unsigned long long fr = 0;
+    if (word < c.words) {
+      fr = ~c.used[word];
+      const int left = c.pages - word * 64;
+      if (left < 64) fr &= (1ull << left) - 1;
+    }
+    int found;
+    const int base = block_scan(__popcll(fr), part, found) + taken;
+    s_base[tid] = base;
+    s_free[tid] = fr;
+    __syncthreads();
+    const int lane = tid & 63;
+    for (int i = tid >> 6; i < kPlanThreads; i += kPlanThreads / 64) {
+      const unsigned long long f = s_free[i];
+      const int first = s_base[i];
+      if (f == 0 || first >= total) continue;
+      const int rank = first + __popcll(f & ((1ull << lane) - 1));
+      const bool take = (f >> lane & 1) && rank < total;
+      if (take) {
+        const int p = (w0 + i) * 64 + lane;
+        int lo = 0, hi = l.n;              // s_begin[lo] <= rank < s_begin[hi]
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) / 2;
+          if (s_begin[mid] <= rank) lo = mid;
+          else hi = mid;
+        }
+        const int j = rank - s_begin[lo];
+        c.table[(int64_t)s_slot[lo] * c.max_pages + s_held[lo] + j] = p;
+        c.ref[p] = 1;
+        if (j == 0 && s_copy[lo] >= 0) w.dst[s_copy[lo]] = p;
+      }
+      const unsigned long long got = __ballot(take);
+      if (lane == 0) c.used[w0 + i] |= got;
+    }
+    taken += found;
+  }
+}
+
+// Part `part` (kCopyUnits 16-byte units) of page copy `i` in one layer of K or V; jobs are
+// numbered part fastest.  Plain 16-byte loads and stores, four in flight per thread.
+__device__ __forceinline__ void copy_job(const CacheView &c, const PageCopies &w, int64_t job,
+                                         int units, int parts) {
+  const int part = (int)(job % parts);
+  int64_t r = job / parts;
+  const int kv = (int)(r & 1);
+  r >>= 1;
+  const int layer = (int)(r % c.layers), i = (int)(r / c.layers);
+  if ((unsigned)w.src[i] >= (unsigned)c.pages || (unsigned)w.dst[i] >= (unsigned)c.pages) return;
+  uint16_t *pool = (kv ? c.v : c.k) + (int64_t)layer * c.pages * units * 8;
+  const Unit *from = (const Unit *)pool + (int64_t)w.src[i] * units;
+  Unit *to = (Unit *)pool + (int64_t)w.dst[i] * units;
+  const int u0 = part * kCopyUnits + threadIdx.x;
+  Unit x[kCopyUnits / 256];
+#pragma unroll
+  for (int j = 0; j < kCopyUnits / 256; ++j)
+    if (u0 + 256 * j < units) x[j] = from[u0 + 256 * j];
+#pragma unroll
+  for (int j = 0; j < kCopyUnits / 256; ++j)
+    if (u0 + 256 * j < units) to[u0 + 256 * j] = x[j];
+}
+
+__device__ __forceinline__ void copy_pages(const CacheView &c, const PageCopies &w) {
+  const int units = c.hkv * c.page * c.d / 8;
+  const int parts = (units + kCopyUnits - 1) / kCopyUnits;
+  const int64_t jobs = (int64_t)w.count[0] * c.layers * 2 * parts;
+  for (int64_t job = blockIdx.x; job < jobs; job += gridDim.x) copy_job(c, w, job, units, parts);
+}
+
+__global__ __launch_bounds__(256) void cache_copy(CacheView c, PageCopies w) { copy_pages(c, w); }
+
+// ---- write: a workgroup writes the new tokens among 64 positions of one slot and KV head.
+// Keys are rows, copied as they are; values go through LDS and leave as 16-byte units of eight
+// tokens of one head dimension.  A unit that also holds older tokens is written element by
+// element.
+template <int D>
+__global__ __launch_bounds__(256) void cache_write(CacheView c, WriteArgs a) {
+  constexpr int CPR = D / 8;                 // 16-byte chunks per row
+  __shared__ __attribute__((aligned(16))) uint16_t tile[64][D + 8];
+  int i = 0, hi = a.list.n;                  // the slot whose blocks hold blockIdx.x
+  while (hi - i > 1) {
+    const int mid = (i + hi) / 2;
+    if (a.blk[mid] <= (int)blockIdx.x) i = mid;
+    else hi = mid;
+  }
+  if (c.state[1] & (FP_CACHE_FULL | FP_CACHE_TOO_LONG)) return;
+  const int h = blockIdx.y, tid = threadIdx.x;
+  const int row0 = a.list.num[i], n = a.list.num[i + 1] - row0;
+  const int slot = a.list.slot[i];
+  const int len = min(c.len[slot], c.max_pages << c.page_shift);
+  const int start = len - n;                 // position of the first row
+  const int p0 = (max(start, 0) & ~63) + 64 * ((int)blockIdx.x - a.blk[i]);
+  const int lo = max(start, p0), end = min(len, p0 + 64);
+  if (lo >= end) return;
+  const int32_t *table = c.table + (int64_t)slot * c.max_pages;
+  // page of position t, or -1 when it is not this slot's alone
+  auto page_at = [&](int t) {
+    const int p = table[t >> c.page_shift];
+    if ((unsigned)p >= (unsigned)c.pages || c.ref[p] != 1) return -1;
+    return p;
+  };
+  auto tile_of = [&](int p, int t) {         // element offset of position t's 16-token step
+    return ((((int64_t)a.layer * c.pages + p) * c.hkv + h) << c.page_shift) * D +
+           (int64_t)(t & (c.page - 1) & ~15) * D;
+  };
+  for (int u = tid; u < 64 * CPR; u += 256) {
+    const int r = u / CPR, ch = u % CPR, t = p0 + r;
+    if (t < lo || t >= end) continue;
+    const int64_t row = row0 + (t - start);
+    const Unit kx = *(const Unit *)(a.k + row * a.k_stride + h * D + ch * 8);
+    const Unit vx = *(const Unit *)(a.v + row * a.v_stride + h * D + ch * 8);
+    *(Unit *)&tile[r][ch * 8] = vx;
+    const int p = page_at(t);
+    if (p >= 0)
+      *(Unit *)(c.k + tile_of(p, t) + (t & 15) * D + ch * 8) = kx;
+    else if (ch == 0)
+      atomicOr(c.state + 1, FP_CACHE_SHARED);
+  }
+  __syncthreads();
+  for (int u = tid; u < 8 * D; u += 256) {   // 8 half steps x D
+    const int half = u & 1, d = (u >> 1) % D, step = (u >> 1) / D;
+    const int r = 16 * step + 8 * half, t = p0 + r;
+    if (t + 8 <= lo || t >= end) continue;
+    const int p = page_at(t);
+    if (p < 0) continue;
+    uint16_t *to = c.v + tile_of(p, t) + d * 16 + 8 * half;
+    if (t >= lo && t + 8 <= end) {
+      Unit x;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        x.x[j] = tile[r + 2 * j][d] | (uint32_t)tile[r + 2 * j + 1][d] << 16;
+      *(Unit *)to = x;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (t + j >= lo && t + j < end) to[j] = tile[r + j][d];
+    }
+  }
+}
+
+// ---- fork: a thread takes one place of the source's table to its copies.  The source keeps its
+// pages throughout, so a page is never free in between, whatever the order of the counts.
+__global__ __launch_bounds__(256) void cache_fork(CacheView c, ForkArgs a) {
+  if (c.state[1] != 0) return;
+  const int item = blockIdx.y, j = blockIdx.x * 256 + threadIdx.x;
+  const int src = a.src[item], first = a.first[item], n = a.first[item + 1] - first;
+  int gone = 0;
+  if (j < c.max_pages) {
+    const int p = c.table[(int64_t)src * c.max_pages + j];
+    int more = 0;
+    for (int i = 0; i < n; ++i) {
+      int32_t *to = c.table + (int64_t)a.dst[first + i] * c.max_pages + j;
+      const int old = *to;
+      if (old == p) continue;
+      *to = p;
+      ++more;
+      if (old >= 0) gone += drop_page(c, old);
+    }
+    if (more && (unsigned)p < (unsigned)c.pages) atomicAdd(c.ref + p, more);
+  }
+  count_freed(c, gone);
+  if (blockIdx.x == 0 && threadIdx.x < n) c.len[a.dst[first + threadIdx.x]] = c.len[src];
+}
+
+// ---- truncate: a thread gives back one place of a slot's table
+__global__ __launch_bounds__(256) void cache_truncate(CacheView c, CacheList l) {
+  if (c.state[1] != 0) return;
+  const int slot = l.slot[blockIdx.y], keep = l.num[blockIdx.y];
+  const int j = blockIdx.x * 256 + threadIdx.x;
+  int gone = 0;
+  if (j < c.max_pages && j >= pages_of(keep, c.page_shift)) {
+    int32_t *at = c.table + (int64_t)slot * c.max_pages + j;
+    const int p = *at;
+    if (p >= 0) {
+      *at = -1;
+      gone = drop_page(c, p);
+    }
+  }
+  count_freed(c, gone);
+  if (j == 0) c.len[slot] = min(c.len[slot], keep);
+}
+
+// ---- compact: one workgroup pairs holes with the pages behind them, a second launch copies the
+// pages and renames them in the tables.  Sources lie at or above state[0] and targets below, so
+// no copy reads what another writes.
+__global__ __launch_bounds__(kPlanThreads) void cache_compact_plan(CacheView c, PageCopies w) {
+  __shared__ int part[kPlanThreads / 64 + 1];
+  __shared__ int s_base[kPlanThreads];
+  __shared__ unsigned long long s_bits[kPlanThreads];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int n_used = c.state[0];
+  if (c.state[1] != 0 || n_used < 0 || n_used > c.pages) {
+    if (tid == 0) w.count[0] = 0;
+    return;
+  }
+  int holes = 0;
+  for (int pass = 0; pass < 2; ++pass) {     // free pages below n_used, then used ones above
+    int seen = 0;
+    const int first_word = pass == 0 ? 0 : n_used / 64;
+    const int end_word = pass == 0 ? (n_used + 63) / 64 : c.words;
+    for (int w0 = first_word; w0 < end_word; w0 += kPlanThreads) {
+      const int word = w0 + tid;
+      unsigned long long bits = 0;
+      if (word < end_word) {
+        bits = c.used[word];
+        const int below = min(max(n_used - word * 64, 0), 64);
+        const unsigned long long mask = below == 64 ? ~0ull : (1ull << below) - 1;
+        bits = pass == 0 ? ~bits & mask : bits & ~mask;
+      }
+      int found;
+      s_base[tid] = block_scan(__popcll(bits), part, found) + seen;
+      s_bits[tid] = bits;
+      __syncthreads();
+      for (int i = tid >> 6; i < kPlanThreads; i += kPlanThreads / 64) {
+        const unsigned long long b = s_bits[i];
+        if (!(b >> lane & 1)) continue;
+        const int p = (w0 + i) * 64 + lane;
+        const int rank = s_base[i] + __popcll(b & ((1ull << lane) - 1));
+        if (pass == 0) {
+          w.dst[rank] = p;
+        } else if (rank < holes) {
+          w.src[rank] = p;
+          w.renamed[p] = w.dst[rank];
+        }
+      }
+      seen += found;
+      __syncthreads();
+    }
+    if (pass == 0) {
+      holes = seen;
+      if (holes == 0) break;
+    }
+  }
+  if (tid == 0) w.count[0] = holes;
+  if (holes == 0) return;
+  for (int word = tid; word < c.words; word += kPlanThreads) {
+    const int below = min(max(n_used - word * 64, 0), 64);
+    c.used[word] = below == 64 ? ~0ull : (1ull << below) - 1;
+  }
+}
+
+__global__ __launch_bounds__(256) void cache_compact_move(CacheView c, PageCopies w) {
+  const int n = w.count[0], n_used = c.state[0];
+  if (n == 0) return;
+  const int64_t me = (int64_t)blockIdx.x * 256 + threadIdx.x, all = (int64_t)gridDim.x * 256;
+  for (int64_t i = me; i < n; i += all) {
+    c.ref[w.dst[i]] = c.ref[w.src[i]];
+    c.ref[w.src[i]] = 0;
+  }
+  for (int64_t i = me; i < (int64_t)c.slots * c.max_pages; i += all) {
+    const int p = c.table[i];
+    if (p >= n_used && p < c.pages) c.table[i] = w.renamed[p];
+  }
+  copy_pages(c, w);
+}
+
+}  // namespace
+
+hipError_t launch_cache_init(const CacheView &c, hipStream_t s) {
+  cache_init<<<1024, 256, 0, s>>>(c);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_reserve(const CacheView &c, const CacheList &l, const PageCopies &w,
+                                hipStream_t s) {
+  cache_reserve<<<1, kPlanThreads, 0, s>>>(c, l, w);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int64_t units = (int64_t)c.hkv * c.page * c.d / 8;
+  const int64_t most = (int64_t)l.n * c.layers * 2 * ((units + kCopyUnits - 1) / kCopyUnits);
+  cache_copy<<<(int)(most < kCopyGrid ? most : kCopyGrid), 256, 0, s>>>(c, w);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_write(const CacheView &c, const WriteArgs &a, hipStream_t s) {
+  const dim3 grid(a.blk[a.list.n], c.hkv);
+  if (c.d == 64) cache_write<64><<<grid, 256, 0, s>>>(c, a);
+  else cache_write<128><<<grid, 256, 0, s>>>(c, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_fork(const CacheView &c, const ForkArgs &a, hipStream_t s) {
+  cache_fork<<<dim3((c.max_pages + 255) / 256, a.items), 256, 0, s>>>(c, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_truncate(const CacheView &c, const CacheList &l, hipStream_t s) {
+  cache_truncate<<<dim3((c.max_pages + 255) / 256, l.n), 256, 0, s>>>(c, l);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_compact(const CacheView &c, const PageCopies &w, hipStream_t s) {
+  cache_compact_plan<<<1, kPlanThreads, 0, s>>>(c, w);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  cache_compact_move<<<kCopyGrid, 256, 0, s>>>(c, w);
+  return hipGetLastError();
+}
+
+}  // namespace fp

@@ -140,6 +140,72 @@ struct AttnArgs {
   SplitArgs split;
 };
 
+// A cache as the kernels see it: fp_cache with the parts of its bookkeeping.
+struct CacheView {
+  uint16_t *k, *v;
+  int32_t *state;              // [8]: pages in use, error bits
+  unsigned long long *used;    // [words] one bit per page
+  int32_t *len;                // [slots]
+  int32_t *ref;                // [pages]
+  int32_t *table;              // [slots][max_pages]
+  int32_t layers, pages, hkv, d, page, page_shift, slots, max_pages, words;
+};
+
+// Slots of one call and a number for each, passed by value.
+struct CacheList {
+  int32_t n;
+  int32_t slot[FP_MAX_CACHE_LIST];
+  int32_t num[FP_MAX_CACHE_LIST + 1];
+};
+
+// Page copies that a call makes in every layer, made by its first launch (workspace).
+struct PageCopies {
+  int32_t *count;              // [4]: copies
+  int32_t *src, *dst;          // [pages]
+  int32_t *renamed;            // [pages] compact: new number of a page that moves
+};
+
+struct WriteArgs {
+  CacheList list;              // num: row of a slot's first token; [n]: rows in all
+  int32_t blk[FP_MAX_CACHE_LIST + 1];   // prefix sums of the 64-token blocks that a slot's
+                                        // rows can touch
+  const uint16_t *k, *v;
+  int64_t k_stride, v_stride;
+  int32_t layer;
+};
+
+// Forks of one source to at most kForkChildren slots, one workgroup column each.
+constexpr int kForkChildren = 16;
+struct ForkArgs {
+  int32_t items;
+  int32_t src[FP_MAX_CACHE_LIST];
+  int32_t first[FP_MAX_CACHE_LIST + 1];   // item -> its first entry of dst
+  int32_t dst[FP_MAX_CACHE_LIST];
+};
+
+struct DecodeArgs {
+  const uint16_t *k, *v;       // pools of the layer
+  const int32_t *len, *table;
+  const uint16_t *q;
+  uint16_t *o;
+  int64_t q_stride;
+  float *part_p, *part_s;      // partial results of prefix and of own key ranges
+  int32_t pages, hkv, page_shift, max_pages;
+  int32_t G, hq, nq, batch, groups;
+  int32_t wgs;                 // workgroups that the key ranges are divided among
+  float scale_log2;            // softmax scale * log2(e)
+  int32_t slot[FP_MAX_CACHE_LIST];
+  int32_t prefix[FP_MAX_CACHE_LIST];       // per group
+  int16_t start[FP_MAX_CACHE_LIST + 1];    // per group: its first sequence
+  uint8_t group[FP_MAX_CACHE_LIST];        // per sequence
+};
+
+// Query rows of one unit of decoding work: 4 waves of 32.
+constexpr int kDecodeRows = 128;
+// Workgroups that fp_decode_attn divides its keys among: every one resident, two (head dim 128)
+// or three (64) on each of 256 CUs.
+constexpr int decode_wgs(int d) { return d == 64 ? 768 : 512; }
+
 // Device address of the current device's fixed scratch array (fp_noalloc.hip).
 hipError_t noalloc_scratch(void **out);
 
@@ -148,5 +214,13 @@ hipError_t launch_sparse_attn(const AttnArgs &a, hipStream_t s);
 hipError_t launch_select_pipeline(const SelectArgs &a, hipStream_t s);
 hipError_t launch_dense_lists(const SelectArgs &a, hipStream_t s);
 hipError_t launch_qa_rows(const SelectArgs &a, hipStream_t s);
+hipError_t launch_cache_init(const CacheView &c, hipStream_t s);
+hipError_t launch_cache_reserve(const CacheView &c, const CacheList &l, const PageCopies &w,
+                                hipStream_t s);
+hipError_t launch_cache_write(const CacheView &c, const WriteArgs &a, hipStream_t s);
+hipError_t launch_cache_fork(const CacheView &c, const ForkArgs &a, hipStream_t s);
+hipError_t launch_cache_truncate(const CacheView &c, const CacheList &l, hipStream_t s);
+hipError_t launch_cache_compact(const CacheView &c, const PageCopies &w, hipStream_t s);
+hipError_t launch_decode_attn(const DecodeArgs &a, int d, hipStream_t s);
 
 }  // namespace fp
