@@ -297,9 +297,9 @@ struct DecodeDims {
   int G;                       // query heads per KV head
   int rows;                    // rows of a sequence and KV head
   int tiles;                   // their row tiles
-  bool shared;                 // some group has a prefix to share
-  size_t slots_p, slots_s;     // partial results
-  size_t bytes_p, bytes_s;
+  bool many, few;              // some group has a prefix to share, with that many rows
+  size_t bytes_many, bytes_few, bytes_own;   // workspace: partial results
+  size_t bytes() const { return bytes_many + bytes_few + bytes_own; }
 };
 
 fp_status check_decode(const fp_cache *c, const fp_decode *b, DecodeDims *dm) {
@@ -316,7 +316,7 @@ fp_status check_decode(const fp_cache *c, const fp_decode *b, DecodeDims *dm) {
   dm->G = b->num_q_heads / c->num_kv_heads;
   dm->rows = dm->G * b->queries;
   dm->tiles = (dm->rows + fp::kDecodeRows - 1) / fp::kDecodeRows;
-  dm->shared = false;
+  dm->many = dm->few = false;
   // cost of all key ranges, in tiles of 64 keys: an int32 in the kernels
   const int64_t most = ((int64_t)c->max_pages * c->page + 63) / 64;
   int64_t cost = (int64_t)b->batch * dm->tiles * most;
@@ -328,7 +328,7 @@ fp_status check_decode(const fp_cache *c, const fp_decode *b, DecodeDims *dm) {
       const int m = b->group_start[g + 1] - b->group_start[g];
       if (m < 1 || m > b->batch || b->prefix_lens[g] < 0) return FP_ERR_INVALID_ARG;
       if (m > 1 && b->prefix_lens[g] > 0) {
-        dm->shared = true;
+        (m * dm->rows > fp::kDecodeFew ? dm->many : dm->few) = true;
         cost += ((int64_t)m * dm->rows / fp::kDecodeRows + 1) *
                 std::min(most, ((int64_t)b->prefix_lens[g] + 63) / 64);
       }
@@ -336,14 +336,14 @@ fp_status check_decode(const fp_cache *c, const fp_decode *b, DecodeDims *dm) {
   }
   if (cost * c->num_kv_heads > 0x7FFFFFFF) return FP_ERR_UNSUPPORTED;
   const size_t wgs = fp::decode_wgs(c->head_dim), row = 4 * (size_t)(c->head_dim + 2);
-  dm->slots_s = wgs + (size_t)b->batch * c->num_kv_heads * dm->tiles;
-  dm->bytes_s = align_up(dm->slots_s * std::min(dm->rows, fp::kDecodeRows) * row);
+  const size_t own = wgs + (size_t)b->batch * c->num_kv_heads * dm->tiles;
+  dm->bytes_own = align_up(own * std::min(dm->rows, fp::kDecodeRows) * row);
+  const size_t few = wgs + (size_t)c->num_kv_heads * b->groups;
+  dm->bytes_few = dm->few ? align_up(few * fp::kDecodeFew * row) : 0;
   // a group's row tiles start at (its first row) / kDecodeRows + its number
-  dm->slots_p = !dm->shared ? 0
-                            : wgs + (size_t)c->num_kv_heads *
-                                        ((size_t)b->batch * dm->rows / fp::kDecodeRows +
-                                         b->groups + 1);
-  dm->bytes_p = align_up(dm->slots_p * fp::kDecodeRows * row);
+  const size_t many = wgs + (size_t)c->num_kv_heads *
+                                ((size_t)b->batch * dm->rows / fp::kDecodeRows + b->groups + 1);
+  dm->bytes_many = dm->many ? align_up(many * fp::kDecodeRows * row) : 0;
   return FP_OK;
 }
 
@@ -670,7 +670,7 @@ fp_status fp_decode_workspace_size(const fp_cache *cache, const fp_decode *batch
   const fp_status st = check_decode(cache, batch, &dm);
   if (st != FP_OK) return st;
   if (!bytes) return FP_ERR_INVALID_ARG;
-  *bytes = dm.bytes_p + dm.bytes_s;
+  *bytes = dm.bytes();
   return FP_OK;
 }
 
@@ -686,7 +686,7 @@ fp_status fp_decode_attn(const fp_cache *cache, const fp_decode *batch, int32_t 
       !aligned16(ws))
     return FP_ERR_INVALID_ARG;
   if (q_stride < (int64_t)batch->num_q_heads * c.d || q_stride % 8) return FP_ERR_INVALID_ARG;
-  if (ws_bytes < dm.bytes_p + dm.bytes_s) return FP_ERR_WORKSPACE;
+  if (ws_bytes < dm.bytes()) return FP_ERR_WORKSPACE;
   fp::DecodeArgs a;
   memset(&a, 0, sizeof(a));
   const int64_t pool = (int64_t)layer * c.pages * c.hkv * c.page * c.d;
@@ -697,8 +697,10 @@ fp_status fp_decode_attn(const fp_cache *cache, const fp_decode *batch, int32_t 
   a.q = (const uint16_t *)q;
   a.o = (uint16_t *)o;
   a.q_stride = q_stride;
-  a.part_p = (float *)ws;
-  a.part_s = (float *)((char *)ws + dm.bytes_p);
+  a.part_many = (float *)ws;
+  a.part_few = (float *)((char *)ws + dm.bytes_many);
+  a.part_own = (float *)((char *)ws + dm.bytes_many + dm.bytes_few);
+  a.any_many = dm.many;
   a.pages = c.pages;
   a.hkv = c.hkv;
   a.page_shift = c.page_shift;

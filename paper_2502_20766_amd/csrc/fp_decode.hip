@@ -8,16 +8,17 @@
 // over one run of keys: the prefix of a group (rows: all query heads of the KV head, all queries,
 // all sequences of the group) or the rest of one sequence (rows: its own).  All segments, one
 // after the other in tiles of 64 keys, form a line that is cut into equal parts, one for each
-// resident workgroup, so every workgroup has the same number of tiles whatever the lengths.  A
-// piece (the part of a segment in one workgroup) leaves O_R, m_R and l_R in float32; a second
-// launch joins the pieces of each row in the order of the line.  A segment in one piece whose
+// resident workgroup, so every workgroup has the same number of tiles whatever the lengths.
+// Prefixes with more than 64 rows, whose products and not bytes are what costs, form a line and a
+// launch of their own.  A piece (the part of a segment in one workgroup) leaves O_R, m_R and l_R
+// in float32; a last launch joins the pieces of each row in the order of the line.  A segment in one piece whose
 // rows have no prefix is finished on the spot.  Where the cuts fall follows from the lengths
 // alone, so results do not depend on timing.
 //
 // One workgroup is four waves.  The 64 keys of a tile go through LDS (double buffered, by DMA,
 // each wave bringing 16 keys, which always lie in one page); with more than 64 rows each wave
 // has 32 rows of its own, with fewer two waves, or two pairs of waves, take 32 keys each and join
-// in LDS.  The products are those of the prefill: S^T = K Q^T with K rows permuted so that a
+// in LDS at the end of the piece.  The products are those of the prefill: S^T = K Q^T with K rows permuted so that a
 // lane's scores are the consecutive keys that P^T of O^T += V^T P^T needs.
 #include <type_traits>
 
@@ -42,6 +43,7 @@ struct Plan {
   int lead[kMaxList];                     // per group: sequence whose pages hold them
   int live[kMaxList];
   int cum[2 * kMaxList + 1];              // starts: groups, then sequences at kMaxList + b
+  int cum_many[kMaxList + 1];             // starts of the groups on the other line
   int scan[4];
 };
 
@@ -51,6 +53,17 @@ __device__ __forceinline__ int row_tiles(int rows) { return (rows + kDecodeRows 
 
 __device__ __forceinline__ int group_rows(const DecodeArgs &a, int g) {
   return (a.start[g + 1] - a.start[g]) * a.nq * a.G;
+}
+
+// Groups whose prefix is on the line of many rows.
+__device__ __forceinline__ bool is_many(const DecodeArgs &a, int g) {
+  return group_rows(a, g) > kDecodeFew;
+}
+
+// Partial results of prefixes: on the line of many rows, row tile 0 of group g and KV head 0 is
+// number (first row of g) / kDecodeRows + g, times Hkv; on the other, one row tile each.
+__device__ __forceinline__ int prefix_base(const DecodeArgs &a, int g, bool many) {
+  return (many ? a.start[g] * a.nq * a.G / kDecodeRows + g : g) * a.hkv;
 }
 
 // Exclusive prefix sum over the workgroup's 256 threads, and the total.
@@ -96,22 +109,27 @@ __device__ __forceinline__ void make_plan(const DecodeArgs &a, Plan &p) {
     }
   }
   __syncthreads();
-  int cost = 0;
+  int cost = 0, cost_many = 0;
   if (t < a.groups) {
     // one sequence alone has nothing to share
     const int keys = p.live[t] >= 2 ? min(p.prefix[t], a.prefix[t]) & ~15 : 0;
     p.prefix[t] = keys;
-    cost = a.hkv * row_tiles(group_rows(a, t)) * tiles_of(keys);
+    (is_many(a, t) ? cost_many : cost) = a.hkv * row_tiles(group_rows(a, t)) * tiles_of(keys);
   }
-  int total_g, total;
-  const int at_g = scan256(cost, p.scan, total_g);   // (its barriers publish p.prefix)
+  int total_many, total_g, total;
+  const int at_many = scan256(cost_many, p.scan, total_many);   // (publishes p.prefix)
+  const int at_g = scan256(cost, p.scan, total_g);
   cost = 0;
   if (t < a.batch && len > 0)
     cost = a.hkv * row_tiles(a.G * a.nq) * tiles_of(len - p.prefix[g]);
   const int at_s = scan256(cost, p.scan, total);
+  p.cum_many[t] = at_many;
   p.cum[t] = at_g;
   p.cum[kMaxList + t] = total_g + at_s;
-  if (t == 0) p.cum[2 * kMaxList] = total_g + total;
+  if (t == 0) {
+    p.cum_many[kMaxList] = total_many;
+    p.cum[2 * kMaxList] = total_g + total;
+  }
   __syncthreads();
 }
 
@@ -139,17 +157,19 @@ struct Piece {
   int whole;            // the piece is all that its rows have
 };
 
+template <bool MANY>
 __device__ __forceinline__ Piece piece_at(const DecodeArgs &a, const Plan &p, int x, int hi,
                                           int wg) {
-  int lo = 0, up = 2 * kMaxList;           // cum[lo] <= x < cum[up]
+  const int *cum = MANY ? p.cum_many : p.cum;
+  int lo = 0, up = MANY ? kMaxList : 2 * kMaxList;   // cum[lo] <= x < cum[up]
   while (up - lo > 1) {
     const int mid = (lo + up) / 2;
-    if (p.cum[mid] <= x) lo = mid;
+    if (cum[mid] <= x) lo = mid;
     else up = mid;
   }
   lo = __builtin_amdgcn_readfirstlane(lo);
   Piece r;
-  r.shared = lo < kMaxList;
+  r.shared = MANY || lo < kMaxList;
   const int e = r.shared ? lo : lo - kMaxList;
   const int g = r.shared ? e : a.group[e];
   const int prefix = p.prefix[g];
@@ -160,7 +180,7 @@ __device__ __forceinline__ Piece piece_at(const DecodeArgs &a, const Plan &p, in
     r.limit = r.vis = prefix;
     rows = group_rows(a, e);
     r.token0 = a.start[e] * a.nq;
-    base = (r.token0 * a.G / kDecodeRows + e) * a.hkv;
+    base = prefix_base(a, e, MANY);
   } else {
     r.row = a.slot[e];
     r.key0 = prefix;
@@ -172,7 +192,7 @@ __device__ __forceinline__ Piece piece_at(const DecodeArgs &a, const Plan &p, in
   }
   r.n = tiles_of(r.limit - r.key0);
   const int rt = row_tiles(rows);
-  const int off = x - p.cum[lo];
+  const int off = x - cum[lo];
   const int seg = off / r.n;               // (KV head, row tile) of the segment
   r.head = seg / rt;
   r.row0 = (seg - r.head * rt) * kDecodeRows;
@@ -215,10 +235,14 @@ struct DecGeo {
   static constexpr int RPI = 1024 / RB;            // key rows per copy
 };
 
-template <int D>
+// MANY: the line of prefixes with more than kDecodeFew rows, every wave with rows of its own and
+// both 32-key halves of a tile under one update of the reference.  Otherwise halves are taken one
+// at a time, by different waves where there are rows for two of them or for one.
+template <int D, bool MANY>
 __global__ __launch_bounds__(kThreads)
 __attribute__((amdgpu_waves_per_eu(DecGeo<D>::OCC, DecGeo<D>::OCC)))
 void decode_fwd(DecodeArgs a) {
+  constexpr int NB = MANY ? 2 : 1;        // 32-key halves under one update
   using S = DecGeo<D>;
   constexpr int KS = D / 16, DB = D / 32;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * S::BYTES];   // [2 tiles][K, V]
@@ -231,7 +255,8 @@ void decode_fwd(DecodeArgs a) {
   const float c = a.scale_log2;
   const float lazy_raw = fminf(kLazy / c, 3.0e38f);
   make_plan(a, plan);
-  const int total = __builtin_amdgcn_readfirstlane(plan.cum[2 * kMaxList]);
+  const int total =
+      __builtin_amdgcn_readfirstlane(MANY ? plan.cum_many[kMaxList] : plan.cum[2 * kMaxList]);
   // workgroups of one XCD (every eighth) take neighbouring parts of the line, which share keys;
   // with fewer tiles than workgroups, one tile each
   const int wgs = min(a.wgs, total);
@@ -255,17 +280,16 @@ void decode_fwd(DecodeArgs a) {
 #pragma unroll
   for (int k = 0; k < KS; ++k) kaddr[k] = kr * S::RB + swz_k<D>(2 * k + lh, kr) * 16;
 
-  // page of this wave's 16 keys of tile t
+  // table entry of this wave's 16 keys of tile t; loaded a tile ahead and first looked at in
+  // `issue`, so that nothing waits for it
   auto page_of = [&](const Piece &r, int t) {
-    const int key = r.key0 + kKeys * t + 16 * w;
-    if (key >= r.limit) return -1;
-    const int pg = a.table[(int64_t)r.row * a.max_pages + (key >> a.page_shift)];
-    return min(max(pg, 0), a.pages - 1);
+    const int key = min(r.key0 + kKeys * t + 16 * w, r.limit - 1);
+    return a.table[(int64_t)r.row * a.max_pages + (key >> a.page_shift)];
   };
   auto issue = [&](const Piece &r, int t, int pg, int into) {
-    pg = __builtin_amdgcn_readfirstlane(pg);
-    if (pg < 0) return;                   // past the segment: those keys are masked
     const int key = r.key0 + kKeys * t + 16 * w;
+    if (key >= r.limit) return;           // past the segment: those keys are masked
+    pg = min(max(__builtin_amdgcn_readfirstlane(pg), 0), a.pages - 1);
     const int64_t off = ((((int64_t)pg * a.hkv + r.head) << a.page_shift) +
                          (key & ((1 << a.page_shift) - 1))) * D;
     const __amdgpu_buffer_rsrc_t rk = uniform_rsrc(a.k + off, 16 * S::RB);
@@ -280,13 +304,13 @@ void decode_fwd(DecodeArgs a) {
     asm volatile("" ::: "memory");
   };
 
-  Piece cur = uniform(piece_at(a, plan, cut(total, wgs, wg), hi, wg));
+  Piece cur = uniform(piece_at<MANY>(a, plan, cut(total, wgs, wg), hi, wg));
   int buf = 0;
   issue(cur, cur.t0, page_of(cur, cur.t0), 0);
-  int page_next = cur.t0 + 1 < cur.t1 ? page_of(cur, cur.t0 + 1) : -1;
+  int page_next = page_of(cur, min(cur.t0 + 1, cur.t1 - 1));
   while (true) {
     // ---- rows of this wave, and the half of a tile that it takes (both with `four`)
-    const bool four = cur.rows > 64;
+    const bool four = MANY || cur.rows > 64;
     const int rb = four ? w : cur.rows > 32 ? w >> 1 : 0;
     const bool active = four ? 32 * w < cur.rows : cur.rows > 32 || w < 2;
     const int half = w & 1;
@@ -310,13 +334,12 @@ void decode_fwd(DecodeArgs a) {
     float m_ref = -INFINITY, mc = 0.f, m_trig = -INFINITY, l_run = 0.f;
     const bool more = cur.end < hi;
     if (more) {                           // published by the first tile's barrier
-      const Piece nxt = piece_at(a, plan, cur.end, hi, wg);
+      const Piece nxt = piece_at<MANY>(a, plan, cur.end, hi, wg);
       if (tid == 0) s_next = nxt;
     }
 
     // NB 32-key halves of the tile in `buf`, from half h0 on
-    auto compute = [&](auto nbc, int h0, int k0) {
-      constexpr int NB = decltype(nbc)::value;
+    auto compute = [&](int h0, int k0) {
       const uint8_t *ks = lds + buf * 2 * S::BYTES + h0 * 32 * S::RB;
       const uint8_t *vs = lds + (buf * 2 + 1) * S::BYTES + h0 * 32 * S::RB + vaddr;
       k0 += 32 * h0;
@@ -357,9 +380,9 @@ void decode_fwd(DecodeArgs a) {
         mc = none ? 0.f : m_new * c;
         m_trig = none ? -INFINITY : m_new + lazy_raw;
       }
-      // Weights: with few rows (NB = 1) the keys' bytes bound the kernel, and a weight is the sum
-      // of two bf16 numbers, its error 2^-17; with many rows the products do, and it is one, as in
-      // the prefill, its error 2^-8 in O and in the sum alike.
+      // Weights: with few rows the keys' bytes bound the kernel, and a weight is the sum of two
+      // bf16 numbers, its error 2^-17; with many the products do, and it is one, as in the prefill,
+      // its error 2^-8 in O and in the sum alike.
       bf16x8 pf[2 * NB], pl[2 * NB];
 #pragma unroll
       for (int b = 0; b < NB; ++b)
@@ -368,20 +391,20 @@ void decode_fwd(DecodeArgs a) {
           const float wt = __builtin_amdgcn_exp2f(fmaf(sacc[b][v], c, -mc));
           const __bf16 top = (__bf16)wt;
           pf[2 * b + (v >> 3)][v & 7] = top;
-          if constexpr (NB == 1) pl[v >> 3][v & 7] = (__bf16)(wt - (float)top);
+          if constexpr (!MANY) pl[v >> 3][v & 7] = (__bf16)(wt - (float)top);
         }
       l_run = sum_weights(pf, l_run);
-      if constexpr (NB == 1) l_run = sum_weights(pl, l_run);
+      if constexpr (!MANY) l_run = sum_weights(pl, l_run);
 #pragma unroll
       for (int t = 0; t < 2 * NB; ++t)
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
           const bf16x8 vf = *reinterpret_cast<const bf16x8 *>(vs + db * 1024 + t * 32 * D);
           oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[t], oacc[db], 0, 0, 0);
-          if constexpr (NB == 1)
+          if constexpr (!MANY)
             oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pl[t], oacc[db], 0, 0, 0);
         }
-      if (edge && (s_odd[buf][0] | s_odd[buf][1] | s_odd[buf][2] | s_odd[buf][3])) {
+      if (!MANY && edge && (s_odd[buf][0] | s_odd[buf][1] | s_odd[buf][2] | s_odd[buf][3])) {
         // the values that settle_edge took out, for the rows that see them
         const int32_t *table = a.table + (int64_t)cur.row * a.max_pages;
         for (int key = max(cur.vis, k0); key < min(cur.limit, k0 + 32 * NB); ++key) {
@@ -437,23 +460,24 @@ void decode_fwd(DecodeArgs a) {
       barrier();                                         // ... and every wave's
       if (t + 1 < cur.t1) {
         issue(cur, t + 1, page_next, buf ^ 1);
-        if (t + 2 < cur.t1) page_next = page_of(cur, t + 2);
+        page_next = page_of(cur, min(t + 2, cur.t1 - 1));
       } else if (more) {
         const Piece nxt = uniform(s_next);
         issue(nxt, nxt.t0, page_of(nxt, nxt.t0), buf ^ 1);
-        if (nxt.t0 + 1 < nxt.t1) page_next = page_of(nxt, nxt.t0 + 1);
+        page_next = page_of(nxt, min(nxt.t0 + 1, nxt.t1 - 1));
       }
-      if (four) {
-        if (active) compute(std::integral_constant<int, 2>{}, 0, k0);
-      } else if (active && k0 + 32 * half < cur.limit) {
-        compute(std::integral_constant<int, 1>{}, half, k0);
+      if constexpr (MANY) {
+        if (active) compute(0, k0);
+      } else if (active) {
+        for (int h = four ? 0 : half; h < (four ? 2 : half + 1); ++h)
+          if (k0 + 32 * h < cur.limit) compute(h, k0);
       }
       buf ^= 1;
     }
 
     // ---- the two key halves of a row joined in LDS (in the tile just used)
     float l_tot = wave_pair_sum(l_run);
-    if (!four) {
+    if (!MANY && !four) {
       barrier();
       float *box = reinterpret_cast<float *>(lds + (buf ^ 1) * 2 * S::BYTES) +
                    (w >> 1) * 64 * 16 * DB;
@@ -495,8 +519,10 @@ void decode_fwd(DecodeArgs a) {
             *reinterpret_cast<bf16x4 *>(op + 32 * db + 8 * g) = ov;
           }
       } else {
-        const int slot_rows = cur.shared ? kDecodeRows : min(a.G * a.nq, kDecodeRows);
-        float *to = (cur.shared ? a.part_p : a.part_s) + (int64_t)cur.slot * slot_rows * (D + 2);
+        const int slot_rows =
+            MANY ? kDecodeRows : cur.shared ? kDecodeFew : min(a.G * a.nq, kDecodeRows);
+        float *to = (MANY ? a.part_many : cur.shared ? a.part_few : a.part_own) +
+                    (int64_t)cur.slot * slot_rows * (D + 2);
         if (lh == 0) *reinterpret_cast<float2 *>(to + slot_rows * D + 2 * row) =
             make_float2(m_ref, l_tot);
         to += row * D + 4 * lh;
@@ -521,8 +547,6 @@ template <int D>
 __global__ __launch_bounds__(kThreads) void decode_join(DecodeArgs a) {
   __shared__ Plan plan;
   make_plan(a, plan);
-  const int total = plan.cum[2 * kMaxList];
-  const int wgs = min(a.wgs, total);
   const int lane = threadIdx.x & 63;
   const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (id >= (int64_t)a.batch * a.nq * a.hq) return;
@@ -537,6 +561,7 @@ __global__ __launch_bounds__(kThreads) void decode_join(DecodeArgs a) {
     for (int e = 0; e < E; ++e) op[lane * E + e] = 0;
     return;
   }
+  const bool many = is_many(a, g);
   // segment of the row and its pieces, for the prefix (kind 0) and its own keys (1)
   int first[2], count[2], row[2];
   int64_t slot[2];
@@ -547,13 +572,15 @@ __global__ __launch_bounds__(kThreads) void decode_join(DecodeArgs a) {
                             : (token - b * a.nq) * a.G + kk;
     const int n = tiles_of(kind == 0 ? prefix : len - prefix);
     const int rt = row_tiles(rows), seg = head * rt + r / kDecodeRows;
-    const int x = plan.cum[kind == 0 ? g : kMaxList + b] + seg * n;
+    const bool line = kind == 0 && many;
+    const int total = line ? plan.cum_many[kMaxList] : plan.cum[2 * kMaxList];
+    const int wgs = min(a.wgs, total);
+    const int x =
+        (line ? plan.cum_many[g] : plan.cum[kind == 0 ? g : kMaxList + b]) + seg * n;
     first[kind] = n ? owner(total, wgs, x) : 0;
     count[kind] = n ? owner(total, wgs, x + n - 1) - first[kind] + 1 : 0;
     row[kind] = r % kDecodeRows;
-    const int base = kind == 0 ? (a.start[g] * a.nq * a.G / kDecodeRows + g) * a.hkv
-                               : b * a.hkv * rt;
-    slot[kind] = base + seg;
+    slot[kind] = (kind == 0 ? prefix_base(a, g, many) : b * a.hkv * rt) + seg;
   }
   if (prefix == 0 && count[1] == 1) return;       // finished by its workgroup
   const int own_rows = min(a.G * a.nq, kDecodeRows);
@@ -561,8 +588,8 @@ __global__ __launch_bounds__(kThreads) void decode_join(DecodeArgs a) {
   // partial i of the row: its floats, and its reference and weight sum
   auto part = [&](int i, const float *&ml) {
     const int kind = i >= count[0];
-    const int slot_rows = kind ? own_rows : kDecodeRows;
-    const float *base = (kind ? a.part_s : a.part_p) +
+    const int slot_rows = kind ? own_rows : many ? kDecodeRows : kDecodeFew;
+    const float *base = (kind ? a.part_own : many ? a.part_many : a.part_few) +
                         (slot[kind] + first[kind] + (kind ? i - count[0] : i)) * slot_rows * (D + 2);
     ml = base + slot_rows * D + 2 * row[kind];
     return base + row[kind] * D;
@@ -604,7 +631,12 @@ __global__ __launch_bounds__(kThreads) void decode_join(DecodeArgs a) {
 
 template <int D>
 hipError_t launch(const DecodeArgs &a, hipStream_t s) {
-  decode_fwd<D><<<a.wgs, kThreads, 0, s>>>(a);
+  if (a.any_many) {
+    decode_fwd<D, true><<<a.wgs, kThreads, 0, s>>>(a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  decode_fwd<D, false><<<a.wgs, kThreads, 0, s>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int64_t rows = (int64_t)a.batch * a.nq * a.hq;

@@ -189,7 +189,9 @@ struct DecodeArgs {
   const uint16_t *q;
   uint16_t *o;
   int64_t q_stride;
-  float *part_p, *part_s;      // partial results of prefix and of own key ranges
+  // partial results of key ranges: prefixes with many and with few rows, sequences' own keys
+  float *part_many, *part_few, *part_own;
+  int32_t any_many;            // some group's prefix has more than kDecodeFew rows
   int32_t pages, hkv, page_shift, max_pages;
   int32_t G, hq, nq, batch, groups;
   int32_t wgs;                 // workgroups that the key ranges are divided among
@@ -202,6 +204,8 @@ struct DecodeArgs {
 
 // Query rows of one unit of decoding work: 4 waves of 32.
 constexpr int kDecodeRows = 128;
+// Rows up to which a prefix is read like a sequence's own keys.
+constexpr int kDecodeFew = 64;
 // Workgroups that fp_decode_attn divides its keys among: every one resident, two (head dim 128)
 // or three (64) on each of 256 CUs.
 constexpr int decode_wgs(int d) { return d == 64 ? 768 : 512; }
