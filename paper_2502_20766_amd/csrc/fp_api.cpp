@@ -296,10 +296,12 @@ fp_status check_slots(const fp_cache *c, int32_t n, const int32_t *slots, SlotSe
 struct DecodeDims {
   int G;                       // query heads per KV head
   int rows;                    // rows of a sequence and KV head
-  int tiles;                   // their row tiles
+  int tile_rows, tiles;        // their row tiles
   bool many, few;              // some group has a prefix to share, with that many rows
   size_t bytes_many, bytes_few, bytes_own;   // workspace: partial results
-  size_t bytes() const { return bytes_many + bytes_few + bytes_own; }
+  size_t bytes() const {
+    return align_up(sizeof(fp::DecodeJoin)) + bytes_many + bytes_few + bytes_own;
+  }
 };
 
 fp_status check_decode(const fp_cache *c, const fp_decode *b, DecodeDims *dm) {
@@ -315,11 +317,11 @@ fp_status check_decode(const fp_cache *c, const fp_decode *b, DecodeDims *dm) {
     if (b->slots[i] < -1 || b->slots[i] >= c->num_slots) return FP_ERR_INVALID_ARG;
   dm->G = b->num_q_heads / c->num_kv_heads;
   dm->rows = dm->G * b->queries;
-  dm->tiles = (dm->rows + fp::kDecodeRows - 1) / fp::kDecodeRows;
+  dm->tile_rows = dm->rows > 16 ? 32 : 16;
   dm->many = dm->few = false;
   // cost of all key ranges, in tiles of 64 keys: an int32 in the kernels
   const int64_t most = ((int64_t)c->max_pages * c->page + 63) / 64;
-  int64_t cost = (int64_t)b->batch * dm->tiles * most;
+  int64_t cost = 0;
   if (b->groups > 0) {
     if (!b->group_start || !b->prefix_lens || b->groups > b->batch) return FP_ERR_INVALID_ARG;
     if (b->group_start[0] != 0 || b->group_start[b->groups] != b->batch)
@@ -329,17 +331,20 @@ fp_status check_decode(const fp_cache *c, const fp_decode *b, DecodeDims *dm) {
       if (m < 1 || m > b->batch || b->prefix_lens[g] < 0) return FP_ERR_INVALID_ARG;
       if (m > 1 && b->prefix_lens[g] > 0) {
         (m * dm->rows > fp::kDecodeFew ? dm->many : dm->few) = true;
+        if (m * dm->rows > 16 && m * dm->rows <= fp::kDecodeFew) dm->tile_rows = 32;
         cost += ((int64_t)m * dm->rows / fp::kDecodeRows + 1) *
-                std::min(most, ((int64_t)b->prefix_lens[g] + 63) / 64);
+                (std::min(most, ((int64_t)b->prefix_lens[g] + 63) / 64) + 8);
       }
     }
   }
+  dm->tiles = (dm->rows + dm->tile_rows - 1) / dm->tile_rows;
+  cost += (int64_t)b->batch * dm->tiles * (most + 8);   // 8: more than a segment's fixed cost
   if (cost * c->num_kv_heads > 0x7FFFFFFF) return FP_ERR_UNSUPPORTED;
   const size_t wgs = fp::decode_wgs(c->head_dim), row = 4 * (size_t)(c->head_dim + 2);
   const size_t own = wgs + (size_t)b->batch * c->num_kv_heads * dm->tiles;
-  dm->bytes_own = align_up(own * std::min(dm->rows, fp::kDecodeRows) * row);
+  dm->bytes_own = align_up(own * dm->tile_rows * row);
   const size_t few = wgs + (size_t)c->num_kv_heads * b->groups;
-  dm->bytes_few = dm->few ? align_up(few * fp::kDecodeFew * row) : 0;
+  dm->bytes_few = dm->few ? align_up(few * dm->tile_rows * row) : 0;
   // a group's row tiles start at (its first row) / kDecodeRows + its number
   const size_t many = wgs + (size_t)c->num_kv_heads *
                                 ((size_t)b->batch * dm->rows / fp::kDecodeRows + b->groups + 1);
@@ -697,10 +702,13 @@ fp_status fp_decode_attn(const fp_cache *cache, const fp_decode *batch, int32_t 
   a.q = (const uint16_t *)q;
   a.o = (uint16_t *)o;
   a.q_stride = q_stride;
-  a.part_many = (float *)ws;
-  a.part_few = (float *)((char *)ws + dm.bytes_many);
-  a.part_own = (float *)((char *)ws + dm.bytes_many + dm.bytes_few);
+  a.join = (fp::DecodeJoin *)ws;
+  char *part = (char *)ws + align_up(sizeof(fp::DecodeJoin));
+  a.part_many = (float *)part;
+  a.part_few = (float *)(part + dm.bytes_many);
+  a.part_own = (float *)(part + dm.bytes_many + dm.bytes_few);
   a.any_many = dm.many;
+  a.tile_rows = dm.tile_rows;
   a.pages = c.pages;
   a.hkv = c.hkv;
   a.page_shift = c.page_shift;

@@ -4,22 +4,18 @@
 //
 // Split softmax: over a range R of keys, with reference m and weights w_j = exp2(s_j - m),
 //   O_R = sum w_j v_j,  l_R = sum w_j;   o = (sum_R 2^(m_R - M) O_R) / (sum_R 2^(m_R - M) l_R).
-// The ranges are cut as follows.  A segment is the work of one KV head and up to 128 query rows
+// The ranges are cut as follows.  A segment is the work of one KV head and one tile of query rows
 // over one run of keys: the prefix of a group (rows: all query heads of the KV head, all queries,
 // all sequences of the group) or the rest of one sequence (rows: its own).  All segments, one
 // after the other in tiles of 64 keys, form a line that is cut into equal parts, one for each
-// resident workgroup, so every workgroup has the same number of tiles whatever the lengths.
-// Prefixes with more than 64 rows, whose products and not bytes are what costs, form a line and a
-// launch of their own.  A piece (the part of a segment in one workgroup) leaves O_R, m_R and l_R
-// in float32; a last launch joins the pieces of each row in the order of the line.  A segment in one piece whose
-// rows have no prefix is finished on the spot.  Where the cuts fall follows from the lengths
-// alone, so results do not depend on timing.
+// resident workgroup, so every workgroup has the same work whatever the lengths.  A piece (the
+// part of a segment in one workgroup) leaves O_R, m_R and l_R in float32; a last launch joins the
+// pieces of each row in the order of the line.  A segment in one piece whose rows have no prefix
+// is finished on the spot.  Where the cuts fall follows from the lengths alone, so results do not
+// depend on timing.
 //
-// One workgroup is four waves.  The 64 keys of a tile go through LDS (double buffered, by DMA,
-// each wave bringing 16 keys, which always lie in one page); with more than 64 rows each wave
-// has 32 rows of its own, with fewer two waves, or two pairs of waves, take 32 keys each and join
-// in LDS at the end of the piece.  The products are those of the prefill: S^T = K Q^T with K rows permuted so that a
-// lane's scores are the consecutive keys that P^T of O^T += V^T P^T needs.
+// Segments with up to 32 rows are bound by the bytes of their keys, those with more by their
+// products, so there are two kernels, each with a line of its own (decode_lean, decode_many).
 #include <type_traits>
 
 #include "fp_attn_dev.h"
@@ -28,28 +24,32 @@
 namespace fp {
 namespace {
 
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
 constexpr int kKeys = 64;                 // keys per tile
 constexpr int kThreads = 256;
 constexpr int kMaxList = FP_MAX_CACHE_LIST;
 constexpr float kLazy = 8.f;              // rise (log2 units) that moves a row's reference
+// Places of the line, beside its tiles, that a segment takes: starting and ending a piece costs a
+// workgroup about as much as this many tiles.
+constexpr int kSegCost = 2;
 
 static_assert(kThreads == kMaxList, "the plan has one thread per sequence");
 
-// The line of a call: lengths, prefixes, and where each group's prefix and each sequence's own
-// keys start on it.
+// The lines of a call.  Starts are the places where the segments of a group's prefix and of a
+// sequence's own keys begin; an entry without keys has the start of the next one.
 struct Plan {
   int len[kMaxList];                      // tokens of a sequence (0: no sequence)
   int prefix[kMaxList];                   // per group: keys read once, a multiple of 16
-  int lead[kMaxList];                     // per group: sequence whose pages hold them
+  int lead[kMaxList];                     // per group: a sequence whose pages hold them
   int live[kMaxList];
-  int cum[2 * kMaxList + 1];              // starts: groups, then sequences at kMaxList + b
-  int cum_many[kMaxList + 1];             // starts of the groups on the other line
-  int scan[4];
+  int lean[2 * kMaxList + 1];             // starts: groups, then sequences at kMaxList + b
+  int many[kMaxList + 1];                 // starts of the groups that are on the other line
+  int scan[3][4];
+  int first;                              // entry that this workgroup's part begins in
 };
 
 __device__ __forceinline__ int tiles_of(int keys) { return (keys + kKeys - 1) / kKeys; }
-
-__device__ __forceinline__ int row_tiles(int rows) { return (rows + kDecodeRows - 1) / kDecodeRows; }
 
 __device__ __forceinline__ int group_rows(const DecodeArgs &a, int g) {
   return (a.start[g + 1] - a.start[g]) * a.nq * a.G;
@@ -60,587 +60,800 @@ __device__ __forceinline__ bool is_many(const DecodeArgs &a, int g) {
   return group_rows(a, g) > kDecodeFew;
 }
 
-// Partial results of prefixes: on the line of many rows, row tile 0 of group g and KV head 0 is
-// number (first row of g) / kDecodeRows + g, times Hkv; on the other, one row tile each.
+// Row tiles: kDecodeRows rows on the line of many, a.tile_rows (16 or 32) on the other.
+__device__ __forceinline__ int many_tiles(int rows) {
+  return (rows + kDecodeRows - 1) / kDecodeRows;
+}
+__device__ __forceinline__ int lean_tiles(const DecodeArgs &a, int rows) {
+  return (rows + a.tile_rows - 1) / a.tile_rows;
+}
+
+// Number of the partial result of row tile 0 and KV head 0 of a prefix, less its workgroup's: the
+// tiles of a group of many rows start at (its first row) / kDecodeRows + its number; a prefix of
+// few rows is one tile.
 __device__ __forceinline__ int prefix_base(const DecodeArgs &a, int g, bool many) {
   return (many ? a.start[g] * a.nq * a.G / kDecodeRows + g : g) * a.hkv;
 }
 
-// Exclusive prefix sum over the workgroup's 256 threads, and the total.
-__device__ __forceinline__ int scan256(int x, int *part, int &total) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  int sum = x;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int y = __shfl_up(sum, d);
-    if (lane >= d) sum += y;
+// A line of `total` places in `wgs` equal parts, the first total % wgs of them one place longer.
+struct Cut {
+  int per, rem;
+  __device__ __forceinline__ Cut(int total, int wgs) : per(total / wgs), rem(total % wgs) {}
+  __device__ __forceinline__ int begin(int w) const { return per * w + min(w, rem); }
+  __device__ __forceinline__ int owner(int x) const {
+    const int longer = rem * (per + 1);
+    return x < longer ? x / (per + 1) : rem + (x - longer) / per;
   }
-  __syncthreads();
-  if (lane == 63) part[w] = sum;
-  __syncthreads();
-  int base = 0;
-  total = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (i < w) base += part[i];
-    total += part[i];
-  }
-  return base + sum - x;
-}
+};
 
-// Fills the plan; every workgroup of both launches does so for itself.
-__device__ __forceinline__ void make_plan(const DecodeArgs &a, Plan &p) {
-  const int t = threadIdx.x;
+// This workgroup's part of its line.
+struct Part {
+  int lo, hi, wg;
+};
+
+// Fills the plan and finds this workgroup's part of the line, and the entry it begins in.  Empty
+// parts have lo == hi.
+template <bool MANY>
+__device__ __forceinline__ Part make_plan(const DecodeArgs &a, Plan &p) {
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6;
   if (t < a.groups) {
     p.prefix[t] = 0x7FFFFFFF;
-    p.lead[t] = 0x7FFFFFFF;
+    p.lead[t] = kMaxList - 1;
     p.live[t] = 0;
   }
-  __syncthreads();
   int len = 0, g = 0;
   if (t < a.batch) {
     g = a.group[t];
     if (a.slot[t] >= 0) len = min(max(a.len[a.slot[t]], 0), a.max_pages << a.page_shift);
     p.len[t] = len;
-    if (len > 0) {
-      atomicMin(&p.prefix[g], max(len - a.nq, 0));
-      atomicMin(&p.lead[g], t);
-      atomicAdd(&p.live[g], 1);
-    }
   }
   __syncthreads();
-  int cost = 0, cost_many = 0;
+  if (len > 0) {
+    atomicMin(&p.prefix[g], max(len - a.nq, 0));
+    atomicMin(&p.lead[g], t);
+    atomicAdd(&p.live[g], 1);
+  }
+  __syncthreads();
+  int cost[3] = {0, 0, 0};                // groups of many rows, of few, own keys
   if (t < a.groups) {
     // one sequence alone has nothing to share
     const int keys = p.live[t] >= 2 ? min(p.prefix[t], a.prefix[t]) & ~15 : 0;
+    if (keys > 0) {
+      const bool many = is_many(a, t);
+      const int tiles = many ? many_tiles(group_rows(a, t)) : 1;
+      cost[many ? 0 : 1] = a.hkv * tiles * (tiles_of(keys) + kSegCost);
+    }
     p.prefix[t] = keys;
-    (is_many(a, t) ? cost_many : cost) = a.hkv * row_tiles(group_rows(a, t)) * tiles_of(keys);
-  }
-  int total_many, total_g, total;
-  const int at_many = scan256(cost_many, p.scan, total_many);   // (publishes p.prefix)
-  const int at_g = scan256(cost, p.scan, total_g);
-  cost = 0;
-  if (t < a.batch && len > 0)
-    cost = a.hkv * row_tiles(a.G * a.nq) * tiles_of(len - p.prefix[g]);
-  const int at_s = scan256(cost, p.scan, total);
-  p.cum_many[t] = at_many;
-  p.cum[t] = at_g;
-  p.cum[kMaxList + t] = total_g + at_s;
-  if (t == 0) {
-    p.cum_many[kMaxList] = total_many;
-    p.cum[2 * kMaxList] = total_g + total;
   }
   __syncthreads();
+  if (len > 0)
+    cost[2] = a.hkv * lean_tiles(a, a.G * a.nq) * (tiles_of(len - p.prefix[g]) + kSegCost);
+  int sum[3];
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    sum[i] = cost[i];
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int y = __shfl_up(sum[i], d);
+      if (lane >= d) sum[i] += y;
+    }
+    if (lane == 63) p.scan[i][w] = sum[i];
+  }
+  __syncthreads();
+  int total[3];
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    total[i] = 0;
+    sum[i] -= cost[i];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (j < w) sum[i] += p.scan[i][j];
+      total[i] += p.scan[i][j];
+    }
+  }
+  p.many[t] = sum[0];
+  p.lean[t] = sum[1];
+  p.lean[kMaxList + t] = total[1] + sum[2];
+  if (t == 0) {
+    p.many[kMaxList] = total[0];
+    p.lean[2 * kMaxList] = total[1] + total[2];
+  }
+  // Workgroups of one XCD (every eighth) take neighbouring parts of the line, which share keys.
+  Part r;
+  const int places = MANY ? total[0] : total[1] + total[2];
+  const int wgs = min(a.wgs, places);
+  r.wg = blockIdx.x;
+  if (wgs == a.wgs) r.wg = (r.wg & 7) * (a.wgs / 8) + (r.wg >> 3);
+  r.lo = r.hi = 0;
+  if (r.wg < wgs) {
+    const Cut cut(places, wgs);
+    r.lo = cut.begin(r.wg);
+    r.hi = cut.begin(r.wg + 1);
+    if (MANY) {
+      if (sum[0] <= r.lo && r.lo < sum[0] + cost[0]) p.first = t;
+    } else {
+      if (sum[1] <= r.lo && r.lo < sum[1] + cost[1]) p.first = t;
+      const int own = total[1] + sum[2];
+      if (own <= r.lo && r.lo < own + cost[2]) p.first = kMaxList + t;
+    }
+  }
+  __syncthreads();
+  r.lo = __builtin_amdgcn_readfirstlane(r.lo);
+  r.hi = __builtin_amdgcn_readfirstlane(r.hi);
+  r.wg = __builtin_amdgcn_readfirstlane(r.wg);
+  return r;
 }
 
-// The line of `total` tiles cut for `wgs` workgroups: [first, first of the next).
-__device__ __forceinline__ int cut(int64_t total, int wgs, int w) {
-  return (int)(total * w / wgs);
-}
-// The workgroup that has tile x.
-__device__ __forceinline__ int owner(int64_t total, int wgs, int x) {
-  return (int)((((int64_t)x + 1) * wgs - 1) / total);
+// What the joining launch needs of the plan, written by one workgroup of decode_lean.
+__device__ __forceinline__ void publish(const DecodeArgs &a, const Plan &p) {
+  const int t = threadIdx.x;
+  DecodeJoin &j = *a.join;
+  if (t < a.batch) {
+    j.len[t] = p.len[t];
+    j.own[t] = p.lean[kMaxList + t];
+  }
+  if (t < a.groups) {
+    j.prefix[t] = p.prefix[t];
+    j.shared[t] = is_many(a, t) ? p.many[t] : p.lean[t];
+  }
+  if (t == 0) {
+    j.total_many = p.many[kMaxList];
+    j.total_lean = p.lean[2 * kMaxList];
+  }
 }
 
-// A run of tiles of one segment in one workgroup.
+// A run of tiles of one segment in one workgroup; every field is wave-uniform.
 struct Piece {
-  int end;              // first place of the line past it
+  int entry;            // of the plan
+  int end;              // place of the line where the segment ends
   int row;              // cache slot whose pages are read
   int head;             // KV head
-  int t0, t1, n;        // tiles [t0, t1) of the segment's n
-  int key0, limit;      // first key, and the first one past the segment
+  int t0, t1;           // tiles [t0, t1); t0 == t1: none
+  int key0, limit;      // the segment's keys: first, and first one past
   int row0, rows;       // rows of this row tile: row0 .. row0 + rows - 1 of the segment's
   int token0;           // query token of the segment's first row
   int vis;              // keys that the first query of a sequence sees
-  int shared;           // a group's prefix
   int slot;             // partial result
   int whole;            // the piece is all that its rows have
 };
 
+// The piece at place x < hi of the line, which lies in entry `e` or a later one.
 template <bool MANY>
-__device__ __forceinline__ Piece piece_at(const DecodeArgs &a, const Plan &p, int x, int hi,
-                                          int wg) {
-  const int *cum = MANY ? p.cum_many : p.cum;
-  int lo = 0, up = MANY ? kMaxList : 2 * kMaxList;   // cum[lo] <= x < cum[up]
-  while (up - lo > 1) {
-    const int mid = (lo + up) / 2;
-    if (cum[mid] <= x) lo = mid;
-    else up = mid;
-  }
-  lo = __builtin_amdgcn_readfirstlane(lo);
+__device__ __forceinline__ Piece piece_at(const DecodeArgs &a, const Plan &p, int e, int x,
+                                          int hi, int wg) {
+  const int *starts = MANY ? p.many : p.lean;
+  while (starts[e + 1] <= x) ++e;
   Piece r;
-  r.shared = MANY || lo < kMaxList;
-  const int e = r.shared ? lo : lo - kMaxList;
-  const int g = r.shared ? e : a.group[e];
-  const int prefix = p.prefix[g];
-  int rows, base;
-  if (r.shared) {
-    r.row = a.slot[min(p.lead[e], kMaxList - 1)];
+  r.entry = __builtin_amdgcn_readfirstlane(e);
+  const bool shared = MANY || r.entry < kMaxList;
+  const int b = r.entry - kMaxList;
+  const int g = shared ? r.entry : a.group[b];
+  const int prefix = __builtin_amdgcn_readfirstlane(p.prefix[g]);
+  int rows, base, tiles, whole = 0;
+  if (shared) {
+    r.row = a.slot[__builtin_amdgcn_readfirstlane(p.lead[g])];
     r.key0 = 0;
     r.limit = r.vis = prefix;
-    rows = group_rows(a, e);
-    r.token0 = a.start[e] * a.nq;
-    base = prefix_base(a, e, MANY);
+    rows = group_rows(a, g);
+    tiles = MANY ? many_tiles(rows) : 1;
+    r.token0 = a.start[g] * a.nq;
+    base = prefix_base(a, g, MANY);
   } else {
-    r.row = a.slot[e];
+    r.row = a.slot[b];
     r.key0 = prefix;
-    r.limit = p.len[e];
+    r.limit = __builtin_amdgcn_readfirstlane(p.len[b]);
     r.vis = r.limit - a.nq + 1;
     rows = a.G * a.nq;
-    r.token0 = e * a.nq;
-    base = e * a.hkv * row_tiles(rows);
+    tiles = lean_tiles(a, rows);
+    r.token0 = b * a.nq;
+    base = b * a.hkv * tiles;
+    whole = prefix == 0;
   }
-  r.n = tiles_of(r.limit - r.key0);
-  const int rt = row_tiles(rows);
-  const int off = x - cum[lo];
-  const int seg = off / r.n;               // (KV head, row tile) of the segment
-  r.head = seg / rt;
-  r.row0 = (seg - r.head * rt) * kDecodeRows;
-  r.rows = min(rows - r.row0, kDecodeRows);
-  r.t0 = off - seg * r.n;
-  r.t1 = min(r.n, r.t0 + hi - x);
-  r.end = x + r.t1 - r.t0;
+  const int n = tiles_of(r.limit - r.key0);
+  const int start = __builtin_amdgcn_readfirstlane(starts[r.entry]);
+  const int seg = (x - start) / (n + kSegCost);         // (KV head, row tile) of the entry
+  const int at = start + seg * (n + kSegCost) + kSegCost;   // place of its first tile
+  const int per = MANY ? kDecodeRows : a.tile_rows;
+  r.head = seg / tiles;
+  r.row0 = (seg - r.head * tiles) * per;
+  r.rows = min(rows - r.row0, per);
+  r.t0 = max(x - at, 0);
+  r.t1 = max(min(hi - at, n), r.t0);
+  r.end = at + n;
   r.slot = wg + base + seg;
-  r.whole = !r.shared && prefix == 0 && r.t0 == 0 && r.t1 == r.n;
+  r.whole = whole && r.t0 == 0 && r.t1 == n;
   return r;
-}
-
-__device__ __forceinline__ Piece uniform(const Piece &r) {
-  Piece u;
-  u.end = __builtin_amdgcn_readfirstlane(r.end);
-  u.row = __builtin_amdgcn_readfirstlane(r.row);
-  u.head = __builtin_amdgcn_readfirstlane(r.head);
-  u.t0 = __builtin_amdgcn_readfirstlane(r.t0);
-  u.t1 = __builtin_amdgcn_readfirstlane(r.t1);
-  u.n = __builtin_amdgcn_readfirstlane(r.n);
-  u.key0 = __builtin_amdgcn_readfirstlane(r.key0);
-  u.limit = __builtin_amdgcn_readfirstlane(r.limit);
-  u.row0 = __builtin_amdgcn_readfirstlane(r.row0);
-  u.rows = __builtin_amdgcn_readfirstlane(r.rows);
-  u.token0 = __builtin_amdgcn_readfirstlane(r.token0);
-  u.vis = __builtin_amdgcn_readfirstlane(r.vis);
-  u.shared = __builtin_amdgcn_readfirstlane(r.shared);
-  u.slot = __builtin_amdgcn_readfirstlane(r.slot);
-  u.whole = __builtin_amdgcn_readfirstlane(r.whole);
-  return u;
 }
 
 template <int D>
 struct DecGeo {
   static constexpr int OCC = D == 64 ? 3 : 2;      // workgroups per CU = waves per SIMD
   static constexpr int RB = 2 * D;                 // bytes per key row
-  static constexpr int BYTES = kKeys * RB;         // a tile of K or of V
-  static constexpr int DMA = BYTES / 4 / 1024;     // 1 KB copies per wave and tile
-  static constexpr int CPR = RB / 16;
+  static constexpr int STEP = 16 * RB;             // bytes of 16 keys, of K or of V
+  static constexpr int DMA = STEP / 1024;          // 1 KB copies of them
+  static constexpr int CPR = RB / 16;              // 16-byte chunks per key row
   static constexpr int RPI = 1024 / RB;            // key rows per copy
 };
 
-// MANY: the line of prefixes with more than kDecodeFew rows, every wave with rows of its own and
-// both 32-key halves of a tile under one update of the reference.  Otherwise halves are taken one
-// at a time, by different waves where there are rows for two of them or for one.
-template <int D, bool MANY>
-__global__ __launch_bounds__(kThreads)
-__attribute__((amdgpu_waves_per_eu(DecGeo<D>::OCC, DecGeo<D>::OCC)))
-void decode_fwd(DecodeArgs a) {
-  constexpr int NB = MANY ? 2 : 1;        // 32-key halves under one update
+// A wave's 16 keys of a tile, which always lie in one page, brought into LDS by DMA: K row-major
+// with 16-byte chunks swizzled as in the prefill, V^T in the fragment order of vt_unit.
+template <int D>
+struct Loader {
   using S = DecGeo<D>;
-  constexpr int KS = D / 16, DB = D / 32;
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * S::BYTES];   // [2 tiles][K, V]
-  __shared__ Plan plan;
-  __shared__ float2 s_ml[2][64];
-  __shared__ Piece s_next;
-  __shared__ int s_odd[2][4];             // per tile buffer: a wave's keys hold such a value
-  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-  const int lr = lane & 31, lh = lane >> 5;
-  const float c = a.scale_log2;
-  const float lazy_raw = fminf(kLazy / c, 3.0e38f);
-  make_plan(a, plan);
-  const int total =
-      __builtin_amdgcn_readfirstlane(MANY ? plan.cum_many[kMaxList] : plan.cum[2 * kMaxList]);
-  // workgroups of one XCD (every eighth) take neighbouring parts of the line, which share keys;
-  // with fewer tiles than workgroups, one tile each
-  const int wgs = min(a.wgs, total);
-  int wg = blockIdx.x;
-  if (wgs == a.wgs) wg = (wg & 7) * (a.wgs / 8) + (wg >> 3);
-  if (wg >= wgs) return;
-  const int hi = cut(total, wgs, wg + 1);
-
-  // DMA offsets of this wave's 16 keys: K rows with swizzled chunks, V^T in fragment order
-  uint32_t koff[S::DMA];
+  uint32_t koff[S::DMA], voff;
+  int w;
+  __device__ __forceinline__ Loader(int w, int lane) : w(w) {
 #pragma unroll
-  for (int i = 0; i < S::DMA; ++i) {
-    const int r = 16 * w + i * S::RPI + lane / S::CPR;
-    koff[i] = (i * S::RPI + lane / S::CPR) * S::RB + swz_k<D>(lane % S::CPR, r) * 16 - i * 1024;
+    for (int i = 0; i < S::DMA; ++i) {
+      const int r = i * S::RPI + lane / S::CPR;
+      koff[i] = r * S::RB + swz_k<D>(lane % S::CPR, r) * 16 - i * 1024;
+    }
+    const int d = 8 * (lane >> 4) + (lane & 7), half = ((lane >> 3) ^ (lane >> 4)) & 1;
+    voff = (2 * d + half) * 16;
   }
-  const int vd = 8 * (lane >> 4) + (lane & 7), vh = ((lane >> 3) ^ (lane >> 4)) & 1;
-  const uint32_t voff = (2 * vd + vh) * 16;
-  const uint32_t vaddr = 16 * vt_unit(lr, lh);
-  const int kr = (lr & ~12) | ((lr >> 1) & 4) | ((lr << 1) & 8);
-  uint32_t kaddr[KS];
-#pragma unroll
-  for (int k = 0; k < KS; ++k) kaddr[k] = kr * S::RB + swz_k<D>(2 * k + lh, kr) * 16;
-
-  // table entry of this wave's 16 keys of tile t; loaded a tile ahead and first looked at in
-  // `issue`, so that nothing waits for it
-  auto page_of = [&](const Piece &r, int t) {
+  // Table entry of the keys of tile t; loaded a tile ahead and first looked at in `issue`, so
+  // that nothing waits for it.
+  __device__ __forceinline__ int page(const DecodeArgs &a, const Piece &r, int t) const {
     const int key = min(r.key0 + kKeys * t + 16 * w, r.limit - 1);
     return a.table[(int64_t)r.row * a.max_pages + (key >> a.page_shift)];
-  };
-  auto issue = [&](const Piece &r, int t, int pg, int into) {
+  }
+  __device__ __forceinline__ void issue(const DecodeArgs &a, const Piece &r, int t, int pg,
+                                        uint8_t *k, uint8_t *v) const {
     const int key = r.key0 + kKeys * t + 16 * w;
     if (key >= r.limit) return;           // past the segment: those keys are masked
     pg = min(max(__builtin_amdgcn_readfirstlane(pg), 0), a.pages - 1);
     const int64_t off = ((((int64_t)pg * a.hkv + r.head) << a.page_shift) +
                          (key & ((1 << a.page_shift) - 1))) * D;
-    const __amdgpu_buffer_rsrc_t rk = uniform_rsrc(a.k + off, 16 * S::RB);
-    const __amdgpu_buffer_rsrc_t rv = uniform_rsrc(a.v + off, 16 * S::RB);
-    uint8_t *dst = lds + into * 2 * S::BYTES + w * 16 * S::RB;
-    dma_slots<0, S::DMA>(rk, (__attribute__((address_space(3))) void *)dst, koff);
-    dma_slots<0, S::DMA>(rv, (__attribute__((address_space(3))) void *)(dst + S::BYTES), voff);
-  };
-  auto barrier = [&]() {
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-  };
+    dma_slots<0, S::DMA>(uniform_rsrc(a.k + off, S::STEP),
+                         (__attribute__((address_space(3))) void *)k, koff);
+    dma_slots<0, S::DMA>(uniform_rsrc(a.v + off, S::STEP),
+                         (__attribute__((address_space(3))) void *)v, voff);
+  }
+};
 
-  Piece cur = uniform(piece_at<MANY>(a, plan, cut(total, wgs, wg), hi, wg));
-  int buf = 0;
-  issue(cur, cur.t0, page_of(cur, cur.t0), 0);
-  int page_next = page_of(cur, min(cur.t0 + 1, cur.t1 - 1));
-  while (true) {
-    // ---- rows of this wave, and the half of a tile that it takes (both with `four`)
-    const bool four = MANY || cur.rows > 64;
-    const int rb = four ? w : cur.rows > 32 ? w >> 1 : 0;
-    const bool active = four ? 32 * w < cur.rows : cur.rows > 32 || w < 2;
-    const int half = w & 1;
-    const int row = 32 * rb + lr;                       // within the row tile
-    const int srow = cur.row0 + min(row, cur.rows - 1); // within the segment
-    const int tok = srow / a.G;
-    const int kk = srow - tok * a.G;
-    const int64_t token = cur.token0 + tok;
-    bf16x8 qf[KS];
-    {
-      const uint16_t *qp = a.q + token * a.q_stride + (cur.head * a.G + kk) * D + 8 * lh;
+// 16 keys of V^T in LDS, of which some row does not see all.  Values past the segment may hold
+// anything, NaN among it, which a weight of zero would not cancel: they become zero.  So do
+// infinities and NaN of tokens that only later queries see; returns whether there were any, and the
+// rows that see them then take them separately.
+template <int D>
+__device__ __forceinline__ bool settle(uint8_t *v, int key0, int limit, int vis, int lane) {
+  bool odd = false;
+  for (int i = 0; i < 2 * D / 64; ++i) {
+    const int u = 64 * i + lane;          // unit (d, half), see Loader::voff
+    const int key = key0 + 8 * (((u >> 3) ^ (u >> 4)) & 1);
+    s16x8 x = *reinterpret_cast<const s16x8 *>(v + 16 * u);
 #pragma unroll
-      for (int k = 0; k < KS; ++k) qf[k] = *reinterpret_cast<const bf16x8 *>(qp + 16 * k);
+    for (int e = 0; e < 8; ++e) {
+      const bool out = key + e >= limit;
+      const bool late = key + e >= vis && (x[e] & 0x7F80) == 0x7F80;
+      odd |= late && !out;
+      if (out || late) x[e] = 0;
     }
+    *reinterpret_cast<s16x8 *>(v + 16 * u) = x;
+  }
+  return __ballot(odd) != 0;
+}
+
+// Workgroup barrier that orders LDS accesses only: it waits for no copy and no store in flight.
+__device__ __forceinline__ void wg_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// Largest x, and sum, over the four lanes that share lane % 16.
+__device__ __forceinline__ float quad_max(float x) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return wave_pair_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float quad_sum(float x) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return wave_pair_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+// ---- few rows: RT tiles of 16 query rows.  The four waves of a workgroup take 16 keys each of
+// every tile and need each other only at the end of a piece, where their results are joined in
+// LDS.  Per wave and step, on v_mfma_f32_16x16x32_bf16:
+//   S^T (16 keys x 16 rows) = K Q^T, D / 32 products; lane (row r = lane % 16, g = lane / 16) holds
+//   the scores of keys 4 g .. 4 g + 3;
+//   O^T += V^T P^T, D / 16 products.  The 32 places of a product's inner dimension are the 16 keys
+//   twice: a weight is the sum of two bf16 numbers (error 2^-17), the second one in places where
+//   V^T is repeated.  That costs no product, and the keys' bytes bound the kernel anyway.
+template <int D, int RT>
+__global__ __launch_bounds__(kThreads)
+__attribute__((amdgpu_waves_per_eu(DecGeo<D>::OCC, DecGeo<D>::OCC)))
+void decode_lean(DecodeArgs a) {
+  using S = DecGeo<D>;
+  constexpr int KS = D / 32, DB = D / 16;
+  // [wave][2 steps][K, V]; at the end of a piece a wave's last step holds its O (16 x D floats)
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[4][2][2 * S::STEP];
+  __shared__ Plan plan;
+  __shared__ float2 s_ml[4][16];
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int r16 = lane & 15, g4 = lane >> 4;
+  const float c = a.scale_log2;
+  const float lazy_raw = fminf(kLazy / c, 3.0e38f);
+  const Part part = make_plan<false>(a, plan);
+  if (blockIdx.x == 0) publish(a, plan);
+  if (part.lo == part.hi) return;
+  const Loader<D> load(w, lane);
+  uint32_t kaddr[KS];                     // this lane's K fragments: key r16, chunks 4 k + g4
+#pragma unroll
+  for (int k = 0; k < KS; ++k) kaddr[k] = r16 * S::RB + swz_k<D>(4 * k + g4, r16) * 16;
+  const uint32_t vaddr = S::STEP + 16 * vt_unit(r16, g4 >> 1) + 8 * (g4 & 1);
+
+  Piece cur = piece_at<false>(a, plan, plan.first, part.lo, part.hi, part.wg);
+  if (cur.t0 == cur.t1) return;           // the part ends before the segment's first tile
+  int buf = 0;
+  load.issue(a, cur, cur.t0, load.page(a, cur, cur.t0), lds[w][0], lds[w][0] + S::STEP);
+  int page_next = load.page(a, cur, min(cur.t0 + 1, cur.t1 - 1));
+  while (true) {
+    // ---- this lane's rows (16 i + r16), their queries and how many keys they see
+    bf16x8 qf[RT][KS];
+    int lim[RT];
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+      const int srow = cur.row0 + min(16 * i + r16, cur.rows - 1);
+      const int tok = srow / a.G;
+      lim[i] = cur.entry < kMaxList ? cur.limit : cur.vis + tok;
+      const uint16_t *qp = a.q + (int64_t)(cur.token0 + tok) * a.q_stride +
+                           (cur.head * a.G + srow - tok * a.G) * D + 8 * g4;
+#pragma unroll
+      for (int k = 0; k < KS; ++k) qf[i][k] = *reinterpret_cast<const bf16x8 *>(qp + 32 * k);
+    }
+    // the next piece, if this part of the line goes on past the segment
+    Piece nxt;
+    nxt.t0 = nxt.t1 = 0;
+    int page_piece = 0;
+    if (cur.end < part.hi) {
+      nxt = piece_at<false>(a, plan, cur.entry, cur.end, part.hi, part.wg);
+      page_piece = load.page(a, nxt, nxt.t0);
+    }
+    const bool more = nxt.t0 < nxt.t1;
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+      for (int k = 0; k < KS; ++k) asm volatile("" : "+v"(qf[i][k]));
+    f32x4 oacc[RT][DB];
+    float m_ref[RT], mc[RT], m_trig[RT], l_run[RT];
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db) oacc[i][db] = f32x4{};
+      m_ref[i] = m_trig[i] = -INFINITY;
+      mc[i] = l_run[i] = 0.f;
+    }
+
+    for (int t = cur.t0; t < cur.t1; ++t) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's keys are here
+      uint8_t *next = lds[w][buf ^ 1];
+      if (t + 1 < cur.t1) {
+        load.issue(a, cur, t + 1, page_next, next, next + S::STEP);
+        page_next = load.page(a, cur, min(t + 2, cur.t1 - 1));
+      } else if (more) {
+        load.issue(a, nxt, nxt.t0, page_piece, next, next + S::STEP);
+        page_next = load.page(a, nxt, min(nxt.t0 + 1, nxt.t1 - 1));
+      }
+      uint8_t *step = lds[w][buf];
+      buf ^= 1;
+      const int k0 = cur.key0 + kKeys * t + 16 * w;
+      if (k0 >= cur.limit) continue;
+      const bool edge = k0 + 16 > cur.vis;
+      bool odd = false;
+      if (edge) odd = settle<D>(step + S::STEP, k0, cur.limit, cur.vis, lane);
+      bf16x8 kf[KS];
+#pragma unroll
+      for (int k = 0; k < KS; ++k) kf[k] = *reinterpret_cast<const bf16x8 *>(step + kaddr[k]);
+      bf16x8 pf[RT];
+#pragma unroll
+      for (int i = 0; i < RT; ++i) {
+        f32x4 s = f32x4{};
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+          s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[k], qf[i][k], s, 0, 0, 0);
+        // (Not only on an edge: with a branch around these few instructions the compiler leaves
+        // out the wait between the product and what reads it on the other path.)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[e] = k0 + 4 * g4 + e < lim[i] ? s[e] : -INFINITY;
+        const float mt = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+        // the reference moves only when a score rises 2^kLazy above it in weight
+        if (__ballot(mt > m_trig[i])) {
+          const float m_new = fmaxf(m_ref[i], quad_max(mt));
+          const float f =
+              m_ref[i] == m_new ? 1.f : __builtin_amdgcn_exp2f((m_ref[i] - m_new) * c);
+          l_run[i] *= f;
+#pragma unroll
+          for (int db = 0; db < DB; ++db) oacc[i][db] *= f;
+          m_ref[i] = m_new;
+          const bool none = m_new == -INFINITY;
+          mc[i] = none ? 0.f : m_new * c;
+          m_trig[i] = none ? -INFINITY : m_new + lazy_raw;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float wt = __builtin_amdgcn_exp2f(fmaf(s[e], c, -mc[i]));
+          const __bf16 top = (__bf16)wt;
+          pf[i][e] = top;
+          pf[i][4 + e] = (__bf16)(wt - (float)top);
+        }
+        const bf16x8 pair[1] = {pf[i]};
+        l_run[i] = sum_weights(pair, l_run[i]);
+      }
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const bf16x4 v = *reinterpret_cast<const bf16x4 *>(step + vaddr + 512 * db);
+        const bf16x8 vf = __builtin_shufflevector(v, v, 0, 1, 2, 3, 0, 1, 2, 3);
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+          oacc[i][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[i], oacc[i][db], 0, 0, 0);
+      }
+      if (odd) {                          // the values that settle took out
+        for (int key = max(cur.vis, k0); key < min(cur.limit, k0 + 16); ++key) {
+          const int pg = min(max(a.table[(int64_t)cur.row * a.max_pages + (key >> a.page_shift)],
+                                 0), a.pages - 1);
+          const uint16_t *vp =
+              a.v + ((((int64_t)pg * a.hkv + cur.head) << a.page_shift) +
+                     (key & ((1 << a.page_shift) - 1) & ~15)) * D + (key & 15) + 64 * g4;
+#pragma unroll
+          for (int i = 0; i < RT; ++i) {
+            float wt = 0.f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (k0 + 4 * g4 + e == key) wt = (float)pf[i][e] + (float)pf[i][4 + e];
+            wt = quad_sum(wt);
+            if (key >= lim[i]) continue;
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const uint32_t x = vp[16 * (16 * db + e)];
+                if ((x & 0x7F80) == 0x7F80)
+                  oacc[i][db][e] = fmaf(wt, __uint_as_float(x << 16), oacc[i][db][e]);
+              }
+          }
+        }
+      }
+    }
+
+    // ---- the waves' results joined: each leaves O in its last step's LDS, 16-byte chunks of a row
+    // swizzled by the row; thread (row tid / 16, i = tid % 16) sums chunks i, i + 16
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+      if (16 * i >= cur.rows) break;
+      if (i) wg_barrier();
+      float *box = reinterpret_cast<float *>(lds[w][buf ^ 1]);
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+        *reinterpret_cast<f32x4 *>(box + r16 * D + 4 * ((4 * db + g4) ^ r16)) = oacc[i][db];
+      const float l = quad_sum(l_run[i]);
+      if (g4 == 0) s_ml[w][r16] = make_float2(m_ref[i], l);
+      wg_barrier();
+      const int row = tid >> 4, ch = tid & 15;
+      if (16 * i + row < cur.rows) {
+        float2 ml[4];
+        float m = -INFINITY, l_tot = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          ml[j] = s_ml[j][row];
+          m = fmaxf(m, ml[j].x);
+        }
+        f32x4 sum[D / 64];
+#pragma unroll
+        for (int q = 0; q < D / 64; ++q) sum[q] = f32x4{};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float f = ml[j].y == 0.f ? 0.f : __builtin_amdgcn_exp2f((ml[j].x - m) * c);
+          l_tot = fmaf(f, ml[j].y, l_tot);
+          const float *from = reinterpret_cast<const float *>(lds[j][buf ^ 1]) + row * D;
+#pragma unroll
+          for (int q = 0; q < D / 64; ++q) {
+            const f32x4 x = *reinterpret_cast<const f32x4 *>(from + 4 * ((ch + 16 * q) ^ row));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[q][e] = fmaf(f, x[e], sum[q][e]);
+          }
+        }
+        const int srow = cur.row0 + 16 * i + row;
+        if (cur.whole) {
+          const int tok = srow / a.G;
+          const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;
+          uint16_t *op = a.o + ((int64_t)(cur.token0 + tok) * a.hq + cur.head * a.G + srow -
+                                tok * a.G) * D + 4 * ch;
+#pragma unroll
+          for (int q = 0; q < D / 64; ++q) {
+            bf16x4 o;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = (__bf16)(sum[q][e] * inv);
+            *reinterpret_cast<bf16x4 *>(op + 64 * q) = o;
+          }
+        } else {
+          float *to = (cur.entry < kMaxList ? a.part_few : a.part_own) +
+                      (int64_t)cur.slot * a.tile_rows * (D + 2);
+          const int at = 16 * i + row;
+          if (ch == 0)
+            *reinterpret_cast<float2 *>(to + a.tile_rows * D + 2 * at) = make_float2(m, l_tot);
+#pragma unroll
+          for (int q = 0; q < D / 64; ++q)
+            *reinterpret_cast<f32x4 *>(to + at * D + 4 * ch + 64 * q) = sum[q];
+        }
+      }
+    }
+    if (!more) return;
+    wg_barrier();                         // read before the next copy arrives there
+    cur = nxt;
+  }
+}
+
+// ---- many rows: tiles of 128, 32 per wave.  The 64 keys of a tile go through LDS (double
+// buffered, each wave bringing 16) and are read by all four waves; the products are those of the
+// prefill, on v_mfma_f32_32x32x16_bf16: S^T = K Q^T with K rows permuted so that a lane's scores
+// are the consecutive keys that P^T of O^T += V^T P^T needs, one update of the reference for 64
+// keys.  A weight is one bf16 number, as there, its error 2^-8 in O and in the sum alike.  All rows
+// see all keys of a prefix.
+template <int D>
+__global__ __launch_bounds__(kThreads)
+__attribute__((amdgpu_waves_per_eu(DecGeo<D>::OCC, DecGeo<D>::OCC)))
+void decode_many(DecodeArgs a) {
+  using S = DecGeo<D>;
+  constexpr int KS = D / 16, DB = D / 32, TILE = 4 * S::STEP;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[2][2 * TILE];   // [2 tiles][K, V]
+  __shared__ Plan plan;
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int lr = lane & 31, lh = lane >> 5;
+  const float c = a.scale_log2;
+  const float lazy_raw = fminf(kLazy / c, 3.0e38f);
+  const Part part = make_plan<true>(a, plan);
+  if (part.lo == part.hi) return;
+  const Loader<D> load(w, lane);
+  auto issue = [&](const Piece &r, int t, int pg, int into) {
+    uint8_t *k = lds[into] + w * S::STEP;
+    load.issue(a, r, t, pg, k, k + TILE);
+  };
+  const int kr = (lr & ~12) | ((lr >> 1) & 4) | ((lr << 1) & 8);
+  uint32_t kaddr[KS];
+#pragma unroll
+  for (int k = 0; k < KS; ++k) kaddr[k] = kr * S::RB + swz_k<D>(2 * k + lh, kr) * 16;
+  const uint32_t vaddr = TILE + 16 * vt_unit(lr, lh);
+
+  Piece cur = piece_at<true>(a, plan, plan.first, part.lo, part.hi, part.wg);
+  if (cur.t0 == cur.t1) return;
+  int buf = 0;
+  issue(cur, cur.t0, load.page(a, cur, cur.t0), 0);
+  int page_next = load.page(a, cur, min(cur.t0 + 1, cur.t1 - 1));
+  while (true) {
+    const bool active = 32 * w < cur.rows;
+    const int row = 32 * w + lr;
+    const int srow = cur.row0 + min(row, cur.rows - 1);
+    const int tok = srow / a.G;
+    const uint16_t *qp = a.q + (int64_t)(cur.token0 + tok) * a.q_stride +
+                         (cur.head * a.G + srow - tok * a.G) * D + 8 * lh;
+    bf16x8 qf[KS];
+#pragma unroll
+    for (int k = 0; k < KS; ++k) qf[k] = *reinterpret_cast<const bf16x8 *>(qp + 16 * k);
 #pragma unroll
     for (int k = 0; k < KS; ++k) asm volatile("" : "+v"(qf[k]));
-    const int lim = cur.shared ? cur.limit : cur.vis + tok;   // keys that this lane's row sees
     f32x16 oacc[DB];
 #pragma unroll
     for (int i = 0; i < DB; ++i) oacc[i] = f32x16{};
     float m_ref = -INFINITY, mc = 0.f, m_trig = -INFINITY, l_run = 0.f;
-    const bool more = cur.end < hi;
-    if (more) {                           // published by the first tile's barrier
-      const Piece nxt = piece_at<MANY>(a, plan, cur.end, hi, wg);
-      if (tid == 0) s_next = nxt;
-    }
+    Piece nxt;
+    nxt.t0 = nxt.t1 = 0;
+    if (cur.end < part.hi) nxt = piece_at<true>(a, plan, cur.entry, cur.end, part.hi, part.wg);
+    const bool more = nxt.t0 < nxt.t1;
 
-    // NB 32-key halves of the tile in `buf`, from half h0 on
-    auto compute = [&](int h0, int k0) {
-      const uint8_t *ks = lds + buf * 2 * S::BYTES + h0 * 32 * S::RB;
-      const uint8_t *vs = lds + (buf * 2 + 1) * S::BYTES + h0 * 32 * S::RB + vaddr;
-      k0 += 32 * h0;
-      f32x16 sacc[NB];
+    for (int t = cur.t0; t < cur.t1; ++t) {
+      const int k0 = cur.key0 + kKeys * t;
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's part of tile t is here
+      const bool edge = k0 + kKeys > cur.limit;
+      if (edge)
+        settle<D>(lds[buf] + TILE + w * S::STEP, k0 + 16 * w, cur.limit, cur.limit, lane);
+      wg_barrier();                                      // ... and every wave's
+      if (t + 1 < cur.t1) {
+        issue(cur, t + 1, page_next, buf ^ 1);
+        page_next = load.page(a, cur, min(t + 2, cur.t1 - 1));
+      } else if (more) {
+        issue(nxt, nxt.t0, load.page(a, nxt, nxt.t0), buf ^ 1);
+        page_next = load.page(a, nxt, min(nxt.t0 + 1, nxt.t1 - 1));
+      }
+      const uint8_t *tile = lds[buf];
+      buf ^= 1;
+      if (!active) continue;
+      f32x16 sacc[2];
 #pragma unroll
-      for (int b = 0; b < NB; ++b) {
+      for (int b = 0; b < 2; ++b) {
         bf16x8 kf[KS];
 #pragma unroll
         for (int k = 0; k < KS; ++k)
-          kf[k] = *reinterpret_cast<const bf16x8 *>(ks + kaddr[k] + b * 32 * S::RB);
+          kf[k] = *reinterpret_cast<const bf16x8 *>(tile + kaddr[k] + b * 32 * S::RB);
         sacc[b] = f32x16{};
 #pragma unroll
         for (int k = 0; k < KS; ++k)
           sacc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k], qf[k], sacc[b], 0, 0, 0);
       }
-      const bool edge = k0 + 32 * NB > cur.vis;         // some row does not see every key
       if (edge) {
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+        for (int b = 0; b < 2; ++b)
 #pragma unroll
           for (int v = 0; v < 16; ++v)
-            if (k0 + 32 * b + 16 * (v >> 3) + 8 * lh + (v & 7) >= lim) sacc[b][v] = -INFINITY;
+            if (k0 + 32 * b + 16 * (v >> 3) + 8 * lh + (v & 7) >= cur.limit)
+              sacc[b][v] = -INFINITY;
       }
       float mt = -INFINITY;
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
+      for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int v = 0; v < 16; ++v) mt = fmaxf(mt, sacc[b][v]);
-      // the reference moves only when a score rises 2^kLazy above it in weight
       if (__ballot(mt > m_trig)) {
         const float m_new = fmaxf(m_ref, wave_pair_max(mt));
-        const float a2 = m_ref == m_new ? 1.f : __builtin_amdgcn_exp2f((m_ref - m_new) * c);
-        l_run *= a2;
+        const float f = m_ref == m_new ? 1.f : __builtin_amdgcn_exp2f((m_ref - m_new) * c);
+        l_run *= f;
 #pragma unroll
-        for (int i = 0; i < DB; ++i) oacc[i] *= a2;
+        for (int i = 0; i < DB; ++i) oacc[i] *= f;
         m_ref = m_new;
         const bool none = m_new == -INFINITY;
         mc = none ? 0.f : m_new * c;
         m_trig = none ? -INFINITY : m_new + lazy_raw;
       }
-      // Weights: with few rows the keys' bytes bound the kernel, and a weight is the sum of two
-      // bf16 numbers, its error 2^-17; with many the products do, and it is one, as in the prefill,
-      // its error 2^-8 in O and in the sum alike.
-      bf16x8 pf[2 * NB], pl[2 * NB];
+      bf16x8 pf[4];
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
+      for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const float wt = __builtin_amdgcn_exp2f(fmaf(sacc[b][v], c, -mc));
-          const __bf16 top = (__bf16)wt;
-          pf[2 * b + (v >> 3)][v & 7] = top;
-          if constexpr (!MANY) pl[v >> 3][v & 7] = (__bf16)(wt - (float)top);
-        }
+        for (int v = 0; v < 16; ++v)
+          pf[2 * b + (v >> 3)][v & 7] = (__bf16)__builtin_amdgcn_exp2f(fmaf(sacc[b][v], c, -mc));
       l_run = sum_weights(pf, l_run);
-      if constexpr (!MANY) l_run = sum_weights(pl, l_run);
 #pragma unroll
-      for (int t = 0; t < 2 * NB; ++t)
+      for (int t4 = 0; t4 < 4; ++t4)
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
-          const bf16x8 vf = *reinterpret_cast<const bf16x8 *>(vs + db * 1024 + t * 32 * D);
-          oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[t], oacc[db], 0, 0, 0);
-          if constexpr (!MANY)
-            oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pl[t], oacc[db], 0, 0, 0);
+          const bf16x8 vf =
+              *reinterpret_cast<const bf16x8 *>(tile + vaddr + db * 1024 + t4 * S::STEP);
+          oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[t4], oacc[db], 0, 0, 0);
         }
-      if (!MANY && edge && (s_odd[buf][0] | s_odd[buf][1] | s_odd[buf][2] | s_odd[buf][3])) {
-        // the values that settle_edge took out, for the rows that see them
-        const int32_t *table = a.table + (int64_t)cur.row * a.max_pages;
-        for (int key = max(cur.vis, k0); key < min(cur.limit, k0 + 32 * NB); ++key) {
-          float wt = 0.f;
-#pragma unroll
-          for (int t = 0; t < 2 * NB; ++t)
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (k0 + 16 * t + 8 * lh + e == key) wt = (float)pf[t][e];
-          wt = wave_pair_sum(wt);
-          if (key >= lim) continue;
-          const int pg = min(max(table[key >> a.page_shift], 0), a.pages - 1);
-          const uint16_t *vp = a.v + ((((int64_t)pg * a.hkv + cur.head) << a.page_shift) +
-                                      (key & ((1 << a.page_shift) - 1) & ~15)) * D + (key & 15);
-#pragma unroll
-          for (int db = 0; db < DB; ++db)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) {
-              const uint32_t x = vp[16 * (32 * db + 8 * (v >> 2) + 4 * lh + (v & 3))];
-              if ((x & 0x7F80) == 0x7F80) oacc[db][v] = fmaf(wt, __uint_as_float(x << 16), oacc[db][v]);
-            }
-        }
-      }
-    };
-    // This wave's 16 keys of a tile that some row does not see whole, before the others read
-    // them.  Values past the segment may hold anything, NaN among it, which a weight of zero
-    // would not cancel: they become zero.  So do infinities and NaN of tokens that only later
-    // queries see; the rows that see them take them separately (s_odd).
-    auto settle_edge = [&](int k0) {
-      uint8_t *vs = lds + (buf * 2 + 1) * S::BYTES + w * 32 * D;
-      bool odd = false;
-      for (int i = 0; i < 2 * D / 64; ++i) {
-        const int u = 64 * i + lane;      // unit (d, vh) of the step, see voff
-        const int key = k0 + 16 * w + 8 * (((u >> 3) ^ (u >> 4)) & 1);
-        s16x8 x = *reinterpret_cast<const s16x8 *>(vs + 16 * u);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const bool out = key + e >= cur.limit;
-          const bool late = key + e >= cur.vis && (x[e] & 0x7F80) == 0x7F80;
-          odd |= late && !out;
-          if (out || late) x[e] = 0;
-        }
-        *reinterpret_cast<s16x8 *>(vs + 16 * u) = x;
-      }
-      const bool any = __ballot(odd) != 0;
-      if (lane == 0) s_odd[buf][w] = any;
-    };
-
-    for (int t = cur.t0; t < cur.t1; ++t) {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's part of tile t is here
-      const int k0 = cur.key0 + kKeys * t;
-      if (k0 + kKeys > cur.vis) settle_edge(k0);
-      barrier();                                         // ... and every wave's
-      if (t + 1 < cur.t1) {
-        issue(cur, t + 1, page_next, buf ^ 1);
-        page_next = page_of(cur, min(t + 2, cur.t1 - 1));
-      } else if (more) {
-        const Piece nxt = uniform(s_next);
-        issue(nxt, nxt.t0, page_of(nxt, nxt.t0), buf ^ 1);
-        page_next = page_of(nxt, min(nxt.t0 + 1, nxt.t1 - 1));
-      }
-      if constexpr (MANY) {
-        if (active) compute(0, k0);
-      } else if (active) {
-        for (int h = four ? 0 : half; h < (four ? 2 : half + 1); ++h)
-          if (k0 + 32 * h < cur.limit) compute(h, k0);
-      }
-      buf ^= 1;
     }
 
-    // ---- the two key halves of a row joined in LDS (in the tile just used)
-    float l_tot = wave_pair_sum(l_run);
-    if (!MANY && !four) {
-      barrier();
-      float *box = reinterpret_cast<float *>(lds + (buf ^ 1) * 2 * S::BYTES) +
-                   (w >> 1) * 64 * 16 * DB;
-      if (active && half == 1) {
-#pragma unroll
-        for (int i = 0; i < DB; ++i)
-#pragma unroll
-          for (int v = 0; v < 16; ++v) box[(16 * i + v) * 64 + lane] = oacc[i][v];
-        s_ml[w >> 1][lane] = make_float2(m_ref, l_tot);
-      }
-      barrier();
-      if (active && half == 0) {
-        const float2 other = s_ml[w >> 1][lane];
-        const float m_new = fmaxf(m_ref, other.x);
-        const float f0 = m_ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m_ref - m_new) * c);
-        const float f1 =
-            other.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((other.x - m_new) * c);
-#pragma unroll
-        for (int i = 0; i < DB; ++i)
-#pragma unroll
-          for (int v = 0; v < 16; ++v)
-            oacc[i][v] = fmaf(f1, box[(16 * i + v) * 64 + lane], f0 * oacc[i][v]);
-        l_tot = f0 * l_tot + f1 * other.y;
-        m_ref = m_new;
-      }
-    }
     // ---- lane holds row `row`, d = 32 db + 8 (v / 4) + 4 lh + v % 4
-    if (active && (four || half == 0) && row < cur.rows) {
-      if (cur.whole) {
-        const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;
-        uint16_t *op = a.o + (token * a.hq + cur.head * a.G + kk) * D + 4 * lh;
+    const float l = wave_pair_sum(l_run);
+    if (row < cur.rows) {
+      float *to = a.part_many + (int64_t)cur.slot * kDecodeRows * (D + 2);
+      if (lh == 0)
+        *reinterpret_cast<float2 *>(to + kDecodeRows * D + 2 * row) = make_float2(m_ref, l);
+      to += row * D + 4 * lh;
 #pragma unroll
-        for (int db = 0; db < DB; ++db)
+      for (int db = 0; db < DB; ++db)
 #pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            bf16x4 ov;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) ov[e] = (__bf16)(oacc[db][4 * g + e] * inv);
-            *reinterpret_cast<bf16x4 *>(op + 32 * db + 8 * g) = ov;
-          }
-      } else {
-        const int slot_rows =
-            MANY ? kDecodeRows : cur.shared ? kDecodeFew : min(a.G * a.nq, kDecodeRows);
-        float *to = (MANY ? a.part_many : cur.shared ? a.part_few : a.part_own) +
-                    (int64_t)cur.slot * slot_rows * (D + 2);
-        if (lh == 0) *reinterpret_cast<float2 *>(to + slot_rows * D + 2 * row) =
-            make_float2(m_ref, l_tot);
-        to += row * D + 4 * lh;
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-          for (int g = 0; g < 4; ++g)
-            *reinterpret_cast<float4 *>(to + 32 * db + 8 * g) =
-                make_float4(oacc[db][4 * g], oacc[db][4 * g + 1], oacc[db][4 * g + 2],
-                            oacc[db][4 * g + 3]);
-      }
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<float4 *>(to + 32 * db + 8 * g) =
+              make_float4(oacc[db][4 * g], oacc[db][4 * g + 1], oacc[db][4 * g + 2],
+                          oacc[db][4 * g + 3]);
     }
     if (!more) return;
-    cur = uniform(s_next);
-    barrier();                            // read by all before it is written again
+    cur = nxt;
   }
 }
 
-// Joins the pieces of every row: one wave per row, D / 64 elements per lane; lane i first takes
-// the reference and weight sum of piece i.
-template <int D>
+// ---- Joins the pieces of a row: WPR waves, each with every 64 / (D / 4) * WPR-th group of pieces,
+// D / 4 lanes to a piece, 16 bytes each.
+template <int D, int WPR>
 __global__ __launch_bounds__(kThreads) void decode_join(DecodeArgs a) {
-  __shared__ Plan plan;
-  make_plan(a, plan);
-  const int lane = threadIdx.x & 63;
-  const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (id >= (int64_t)a.batch * a.nq * a.hq) return;
+  constexpr int LPP = D / 4;              // lanes per piece
+  constexpr int PPW = 64 / LPP;           // pieces at once in a wave
+  __shared__ f32x4 s_sum[4][LPP];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, part = w % WPR;
+  const int64_t id = (int64_t)blockIdx.x * (4 / WPR) + w / WPR;
+  if (WPR == 1 && id >= (int64_t)a.batch * a.nq * a.hq) return;
   const int token = (int)(id / a.hq), qh = (int)(id - (int64_t)token * a.hq);
-  const int b = token / a.nq, head = qh / a.G, kk = qh - head * a.G;
-  const int g = a.group[b], prefix = plan.prefix[g], len = plan.len[b];
+  const int b = token / a.nq, t = token - b * a.nq, head = qh / a.G, kk = qh - head * a.G;
+  const int g = a.group[b];
+  const DecodeJoin &j = *a.join;
+  const int prefix = j.prefix[g], len = j.len[b];
   uint16_t *op = a.o + id * D;
-  constexpr int E = D / 64;
   const float c = a.scale_log2;
-  if (len == 0) {
-#pragma unroll
-    for (int e = 0; e < E; ++e) op[lane * E + e] = 0;
-    return;
-  }
   const bool many = is_many(a, g);
-  // segment of the row and its pieces, for the prefix (kind 0) and its own keys (1)
-  int first[2], count[2], row[2];
-  int64_t slot[2];
+  // pieces of the row's two segments: the prefix (0) and its own keys (1)
+  int count[2] = {0, 0}, stride[2], ml_at[2];
+  const float *from[2] = {a.part_own, a.part_own};
 #pragma unroll
   for (int kind = 0; kind < 2; ++kind) {
-    const int rows = kind == 0 ? group_rows(a, g) : a.G * a.nq;
-    const int r = kind == 0 ? ((b - a.start[g]) * a.nq + token - b * a.nq) * a.G + kk
-                            : (token - b * a.nq) * a.G + kk;
-    const int n = tiles_of(kind == 0 ? prefix : len - prefix);
-    const int rt = row_tiles(rows), seg = head * rt + r / kDecodeRows;
     const bool line = kind == 0 && many;
-    const int total = line ? plan.cum_many[kMaxList] : plan.cum[2 * kMaxList];
-    const int wgs = min(a.wgs, total);
-    const int x =
-        (line ? plan.cum_many[g] : plan.cum[kind == 0 ? g : kMaxList + b]) + seg * n;
-    first[kind] = n ? owner(total, wgs, x) : 0;
-    count[kind] = n ? owner(total, wgs, x + n - 1) - first[kind] + 1 : 0;
-    row[kind] = r % kDecodeRows;
-    slot[kind] = (kind == 0 ? prefix_base(a, g, many) : b * a.hkv * rt) + seg;
+    const int r = ((kind == 0 ? b - a.start[g] : 0) * a.nq + t) * a.G + kk;
+    const int per = line ? kDecodeRows : a.tile_rows;
+    const int tiles = line ? many_tiles(group_rows(a, g))
+                           : kind == 0 ? 1 : lean_tiles(a, a.G * a.nq);
+    const int n = len == 0 ? 0 : tiles_of(kind == 0 ? prefix : len - prefix);
+    stride[kind] = per * (D + 2);
+    const int row = r % per;
+    ml_at[kind] = per * D + 2 * row - row * D;
+    if (n == 0) continue;
+    const int seg = head * tiles + r / per;
+    const int at = (kind == 0 ? j.shared[g] : j.own[b]) + seg * (n + kSegCost) + kSegCost;
+    const int total = line ? j.total_many : j.total_lean;
+    const Cut cut(total, min(a.wgs, total));
+    const int first = cut.owner(at);
+    count[kind] = cut.owner(at + n - 1) - first + 1;
+    const int base = kind == 0 ? prefix_base(a, g, many) : b * a.hkv * tiles;
+    from[kind] = (line ? a.part_many : kind == 0 ? a.part_few : a.part_own) +
+                 (int64_t)(base + seg + first) * stride[kind] + row * D;
   }
-  if (prefix == 0 && count[1] == 1) return;       // finished by its workgroup
-  const int own_rows = min(a.G * a.nq, kDecodeRows);
   const int n = count[0] + count[1];
-  // partial i of the row: its floats, and its reference and weight sum
-  auto part = [&](int i, const float *&ml) {
-    const int kind = i >= count[0];
-    const int slot_rows = kind ? own_rows : many ? kDecodeRows : kDecodeFew;
-    const float *base = (kind ? a.part_own : many ? a.part_many : a.part_few) +
-                        (slot[kind] + first[kind] + (kind ? i - count[0] : i)) * slot_rows * (D + 2);
-    ml = base + slot_rows * D + 2 * row[kind];
-    return base + row[kind] * D;
+  if (prefix == 0 && n == 1) return;      // finished by its workgroup
+  auto piece = [&](int i) {
+    return i < count[0] ? from[0] + (int64_t)i * stride[0]
+                        : from[1] + (int64_t)(i - count[0]) * stride[1];
   };
-  float m = -INFINITY, l = 0.f, acc[E] = {};
+  float m = -INFINITY, l = 0.f;
+  f32x4 acc = f32x4{};
   for (int i0 = 0; i0 < n; i0 += 64) {
     const int k = min(64, n - i0);
     float2 ml = make_float2(-INFINITY, 0.f);
-    if (lane < k) {
-      const float *at;
-      part(i0 + lane, at);
-      ml = *reinterpret_cast<const float2 *>(at);
-    }
+    if (lane < k)
+      ml = *reinterpret_cast<const float2 *>(piece(i0 + lane) +
+                                             ml_at[i0 + lane < count[0] ? 0 : 1]);
     float top = fmaxf(m, ml.x);
 #pragma unroll
     for (int d = 32; d > 0; d /= 2) top = fmaxf(top, __shfl_xor(top, d));
     const float old = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - top) * c);
-    const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ml.x - top) * c);
+    // (a sum of 0: no key seen; a NaN has to come through, whatever its reference)
+    const float f = ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f((ml.x - top) * c);
     float sum = f * ml.y;
 #pragma unroll
     for (int d = 32; d > 0; d /= 2) sum += __shfl_xor(sum, d);
     l = l * old + sum;
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] *= old;
+    for (int e = 0; e < 4; ++e) acc[e] *= old;
     m = top;
-    for (int i = 0; i < k; ++i) {
-      const float *unused;
-      const float *at = part(i0 + i, unused) + lane * E;
-      const float fi = __shfl(f, i);
+    constexpr int U = 4;                  // loads in flight
+    for (int i = part * PPW; i < k; i += U * WPR * PPW) {
+      f32x4 x[U];
+      float fi[U];
 #pragma unroll
-      for (int e = 0; e < E; ++e) acc[e] = fmaf(fi, at[e], acc[e]);
+      for (int u = 0; u < U; ++u) {
+        const int at = i + u * WPR * PPW + lane / LPP;
+        fi[u] = __shfl(f, at & 63);
+        if (at >= k) fi[u] = 0.f;
+        x[u] = *reinterpret_cast<const f32x4 *>(piece(i0 + min(at, k - 1)) + 4 * (lane % LPP));
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (fi[u] != 0.f) acc[e] = fmaf(fi[u], x[u][e], acc[e]);
+    }
+  }
+#pragma unroll
+  for (int d = LPP; d < 64; d *= 2)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], d);
+  if constexpr (WPR > 1) {
+    if (lane < LPP) s_sum[w][lane] = acc;
+    __syncthreads();
+    if (part != 0) return;
+    if (lane < LPP) {
+      acc = f32x4{};
+#pragma unroll
+      for (int i = 0; i < WPR; ++i) acc += s_sum[w + i][lane];
     }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
+  if (lane < LPP) {
+    bf16x4 o;
 #pragma unroll
-  for (int e = 0; e < E; ++e)
-    op[lane * E + e] = __builtin_bit_cast(uint16_t, (__bf16)(acc[e] * inv));
+    for (int e = 0; e < 4; ++e) o[e] = (__bf16)(acc[e] * inv);
+    *reinterpret_cast<bf16x4 *>(op + 4 * lane) = o;
+  }
 }
 
 template <int D>
 hipError_t launch(const DecodeArgs &a, hipStream_t s) {
+  hipError_t e = hipSuccess;
   if (a.any_many) {
-    decode_fwd<D, true><<<a.wgs, kThreads, 0, s>>>(a);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+    decode_many<D><<<a.wgs, kThreads, 0, s>>>(a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  decode_fwd<D, false><<<a.wgs, kThreads, 0, s>>>(a);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  const int64_t rows = (int64_t)a.batch * a.nq * a.hq;
-  decode_join<D><<<(int)((rows + 3) / 4), kThreads, 0, s>>>(a);
+  if (a.tile_rows == 16) decode_lean<D, 1><<<a.wgs, kThreads, 0, s>>>(a);
+  else decode_lean<D, 2><<<a.wgs, kThreads, 0, s>>>(a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  const int rows = a.batch * a.nq * a.hq;
+  if (rows <= 2048) decode_join<D, 4><<<rows, kThreads, 0, s>>>(a);
+  else decode_join<D, 1><<<(rows + 3) / 4, kThreads, 0, s>>>(a);
   return hipGetLastError();
 }
 

@@ -183,6 +183,13 @@ struct ForkArgs {
   int32_t dst[FP_MAX_CACHE_LIST];
 };
 
+// What the joining launch of decode_attn knows of the call's plan (workspace).
+struct DecodeJoin {
+  int32_t len[FP_MAX_CACHE_LIST], own[FP_MAX_CACHE_LIST];        // per sequence
+  int32_t prefix[FP_MAX_CACHE_LIST], shared[FP_MAX_CACHE_LIST];  // per group
+  int32_t total_lean, total_many;
+};
+
 struct DecodeArgs {
   const uint16_t *k, *v;       // pools of the layer
   const int32_t *len, *table;
@@ -191,7 +198,9 @@ struct DecodeArgs {
   int64_t q_stride;
   // partial results of key ranges: prefixes with many and with few rows, sequences' own keys
   float *part_many, *part_few, *part_own;
+  DecodeJoin *join;
   int32_t any_many;            // some group's prefix has more than kDecodeFew rows
+  int32_t tile_rows;           // query rows of a unit of the other work: 16 or 32
   int32_t pages, hkv, page_shift, max_pages;
   int32_t G, hq, nq, batch, groups;
   int32_t wgs;                 // workgroups that the key ranges are divided among
@@ -202,10 +211,10 @@ struct DecodeArgs {
   uint8_t group[FP_MAX_CACHE_LIST];        // per sequence
 };
 
-// Query rows of one unit of decoding work: 4 waves of 32.
+// Query rows of one unit of work on prefixes with many rows: 4 waves of 32.
 constexpr int kDecodeRows = 128;
 // Rows up to which a prefix is read like a sequence's own keys.
-constexpr int kDecodeFew = 64;
+constexpr int kDecodeFew = 32;
 // Workgroups that fp_decode_attn divides its keys among: every one resident, two (head dim 128)
 // or three (64) on each of 256 CUs.
 constexpr int decode_wgs(int d) { return d == 64 ? 768 : 512; }

@@ -129,7 +129,8 @@ class Scene:
         return q, o
 
 
-HEADS = [(4, 1, 128), (2, 2, 64), (16, 1, 64), (7, 1, 128), (8, 2, 64), (48, 1, 128)]
+HEADS = [(4, 1, 128), (2, 2, 64), (16, 1, 64), (7, 1, 128), (8, 2, 64), (48, 1, 128),
+         (17, 1, 64), (33, 1, 128)]
 
 
 @pytest.mark.parametrize("hq,hkv,d", HEADS)
@@ -244,6 +245,22 @@ def test_odd_keys_of_later_tokens(pattern):
     for b, (k, v) in enumerate(s.seqs):
         want, mass = attend(floats(q[b * 4:b * 4 + 3]), floats(k[:-1]), floats(v[:-1]), 0.125)
         assert np.all(np.abs(got[b, :3] - want) <= tolerance(want, mass))
+
+
+@pytest.mark.parametrize("pattern", [INF, NAN])
+@pytest.mark.parametrize("n", [1, 3, 200])
+def test_odd_keys_come_through(pattern, n):
+    """A visible key that is NaN, or whose score is +inf, makes its queries NaN, whether it is
+    the only one of its range of keys or not; other sequences and KV heads stay as they are."""
+    s = Scene([(48, [n, 20]), (0, [n])], 4, 2, 64, 16, seed=n)
+    q = bits(np.abs(floats(s.queries(1))) + 0.1)
+    for b in (0, 2):
+        k = np.array(s.seqs[b][0][-1])
+        k[0, 3] = pattern
+        s.put(b, len(s.seqs[b][0]) - 1, k=k)
+    o = s.fpx.decode_attn(_dev(q), s.cache(), 0, s.batch(1))
+    assert bool(torch.isnan(o[[0, 2]][:, :2].float()).all())
+    s.check(q, o, 1)
 
 
 def test_scores_of_minus_infinity():
