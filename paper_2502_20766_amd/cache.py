@@ -19,7 +19,7 @@ import ctypes
 
 import numpy as np
 
-from . import FpCache, FpDecode, _check, _check_tensor, _stream_ptr, _workspace, lib
+from . import FP_OK, FpCache, FpDecode, _check, _check_tensor, _workspace, lib
 
 CACHE_FULL, CACHE_TOO_LONG, CACHE_SHARED = 1, 2, 4
 MAX_CACHE_LIST = 256
@@ -37,8 +37,34 @@ class CacheError(RuntimeError):
         super().__init__("; ".join(names) or f"error bits {bits}")
 
 
+# These calls are made several times a layer and step, so the host's share of one counts: lists go
+# to the library as the bytes of int32 arrays, tensors as plain addresses.
+
+_torch = None
+
+
+def _t():
+    """torch, which importing this package does not load."""
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
+
+def _stream(stream):
+    """The raw handle of `stream` or of the current stream."""
+    if stream is not None:
+        return stream.cuda_stream
+    c = _t()._C
+    return c._cuda_getCurrentRawStream(c._cuda_getDevice())
+
+
 def _ints(x, name, n=None):
     """x as a contiguous int32 host array of n elements."""
+    if (type(x) is np.ndarray and x.dtype == np.int32 and x.ndim == 1
+            and x.flags.c_contiguous and (n is None or x.size == n)):
+        return x
     a = np.ascontiguousarray(x if isinstance(x, np.ndarray) else list(x))
     if a.dtype != np.int32:
         if a.size and not np.issubdtype(a.dtype, np.integer):
@@ -52,8 +78,9 @@ def _ints(x, name, n=None):
     return a
 
 
-def _ptr(a):
-    return ctypes.c_void_p(a.ctypes.data)
+def _call(status, what):
+    if status != FP_OK:
+        _check(status, what)
 
 
 class Cache:
@@ -120,7 +147,7 @@ def _cache_workspace(cache, workspace, stream):
 
 def cache_init(cache: Cache, stream=None):
     """Every slot empty, every page free."""
-    _check(lib().fp_cache_init(cache.ref, _stream_ptr(stream)), "fp_cache_init")
+    _call(lib().fp_cache_init(cache.ref, _stream(stream)), "fp_cache_init")
 
 
 def cache_reserve(cache: Cache, slots, counts, workspace=None, stream=None):
@@ -128,23 +155,22 @@ def cache_reserve(cache: Cache, slots, counts, workspace=None, stream=None):
     layers.  A shared last page that is not full is copied first.  If pages run out or a slot
     would grow past max_pages nothing changes, and Cache.check raises."""
     slots = _ints(slots, "slots")
-    counts = (np.full(slots.size, counts, np.int32) if np.ndim(counts) == 0
-              else _ints(counts, "counts", slots.size))
+    n = slots.size
+    counts = (np.full(n, counts, np.int32) if isinstance(counts, (int, np.integer))
+              else _ints(counts, "counts", n))
     ws = _cache_workspace(cache, workspace, stream)
-    _check(lib().fp_cache_reserve(cache.ref, slots.size, _ptr(slots), _ptr(counts),
-                                  ctypes.c_void_p(ws.data_ptr()), ws.numel(),
-                                  _stream_ptr(stream)), "fp_cache_reserve")
+    _call(lib().fp_cache_reserve(cache.ref, n, slots.tobytes(), counts.tobytes(), ws.data_ptr(),
+                                 ws.numel(), _stream(stream)), "fp_cache_reserve")
 
 
 def _check_rows(x, name, heads, d):
-    """A [T, heads, d] bf16 tensor whose rows are contiguous, any stride between them."""
-    import torch
-    if not (x.is_cuda and x.dtype == torch.bfloat16 and x.dim() == 3
-            and tuple(x.shape[1:]) == (heads, d)
-            and (x.shape[0] == 0 or (x.stride(2) == 1 and x.stride(1) == d))):
+    """The stride between rows of a [T, heads, d] bf16 tensor whose rows are contiguous."""
+    shape, stride = x.shape, x.stride()
+    if not (x.is_cuda and x.dtype == _t().bfloat16 and len(shape) == 3 and shape[1] == heads
+            and shape[2] == d and (shape[0] == 0 or (stride[2] == 1 and stride[1] == d))):
         raise ValueError(f"{name} must be a bf16 CUDA tensor [T, {heads}, {d}] with contiguous "
                          "rows")
-    return x.stride(0) if x.shape[0] > 1 else heads * d
+    return stride[0] if shape[0] > 1 else heads * d
 
 
 def cache_write(cache: Cache, layer, k, v, slots, cu_seqlens, stream=None):
@@ -152,45 +178,43 @@ def cache_write(cache: Cache, layer, k, v, slots, cu_seqlens, stream=None):
     slots[i].  k, v: [T, Hkv, d] bf16, rows contiguous (slices of a fused projection do)."""
     slots = _ints(slots, "slots")
     cu = _ints(cu_seqlens, "cu_seqlens", slots.size + 1)
-    ks = _check_rows(k, "k", cache.c.num_kv_heads, cache.c.head_dim)
-    vs = _check_rows(v, "v", cache.c.num_kv_heads, cache.c.head_dim)
-    if k.shape[0] != cu[-1] or v.shape[0] != cu[-1]:
-        raise ValueError(f"k and v have {k.shape[0]} and {v.shape[0]} rows; cu_seqlens ends "
-                         f"at {cu[-1]}")
-    _check(lib().fp_cache_write(cache.ref, int(layer), slots.size, _ptr(slots), _ptr(cu),
-                                ctypes.c_void_p(k.data_ptr()), ks,
-                                ctypes.c_void_p(v.data_ptr()), vs, _stream_ptr(stream)),
-           "fp_cache_write")
+    heads, d = cache.c.num_kv_heads, cache.c.head_dim
+    ks, vs = _check_rows(k, "k", heads, d), _check_rows(v, "v", heads, d)
+    if not len(k) == len(v) == cu[-1]:
+        raise ValueError(f"k and v have {len(k)} and {len(v)} rows; cu_seqlens ends at {cu[-1]}")
+    _call(lib().fp_cache_write(cache.ref, layer, slots.size, slots.tobytes(), cu.tobytes(),
+                               k.data_ptr(), ks, v.data_ptr(), vs, _stream(stream)),
+          "fp_cache_write")
 
 
 def cache_fork(cache: Cache, src, dst, stream=None):
     """dst[i] becomes a copy of src[i] that shares its pages; what it held is given back."""
     src = _ints(src, "src")
     dst = _ints(dst, "dst", src.size)
-    _check(lib().fp_cache_fork(cache.ref, src.size, _ptr(src), _ptr(dst), _stream_ptr(stream)),
-           "fp_cache_fork")
+    _call(lib().fp_cache_fork(cache.ref, src.size, src.tobytes(), dst.tobytes(),
+                              _stream(stream)), "fp_cache_fork")
 
 
 def cache_truncate(cache: Cache, slots, lens, stream=None):
     """slots[i] keeps its first lens[i] tokens (drafts that were not accepted, for one)."""
     slots = _ints(slots, "slots")
     lens = _ints(lens, "lens", slots.size)
-    _check(lib().fp_cache_truncate(cache.ref, slots.size, _ptr(slots), _ptr(lens),
-                                   _stream_ptr(stream)), "fp_cache_truncate")
+    _call(lib().fp_cache_truncate(cache.ref, slots.size, slots.tobytes(), lens.tobytes(),
+                                  _stream(stream)), "fp_cache_truncate")
 
 
 def cache_free(cache: Cache, slots, stream=None):
     """The slots become empty; their pages are free once no other slot holds them."""
     slots = _ints(slots, "slots")
-    _check(lib().fp_cache_truncate(cache.ref, slots.size, _ptr(slots), None,
-                                   _stream_ptr(stream)), "fp_cache_truncate")
+    _call(lib().fp_cache_truncate(cache.ref, slots.size, slots.tobytes(), None,
+                                  _stream(stream)), "fp_cache_truncate")
 
 
 def cache_compact(cache: Cache, workspace=None, stream=None):
     """The pages in use become pages 0 .. state[0]-1, in every layer and table."""
     ws = _cache_workspace(cache, workspace, stream)
-    _check(lib().fp_cache_compact(cache.ref, ctypes.c_void_p(ws.data_ptr()), ws.numel(),
-                                  _stream_ptr(stream)), "fp_cache_compact")
+    _call(lib().fp_cache_compact(cache.ref, ws.data_ptr(), ws.numel(), _stream(stream)),
+          "fp_cache_compact")
 
 
 class DecodeBatch:
@@ -200,18 +224,20 @@ class DecodeBatch:
 
     def __init__(self, slots, num_q_heads, queries=1, group_start=None, prefix_lens=None,
                  softmax_scale=0.0):
-        self.slots = _ints(slots, "slots")
+        # copies: the structure keeps their addresses
+        self.slots = _ints(slots, "slots").copy()
         self.group_start = self.prefix_lens = None
         if (group_start is None) != (prefix_lens is None):
             raise ValueError("group_start and prefix_lens come together")
-        self.c = FpDecode(self.slots.size, _ptr(self.slots), int(num_q_heads), int(queries), 0,
-                          None, None, float(softmax_scale))
+        self.c = FpDecode(self.slots.size, self.slots.ctypes.data, int(num_q_heads),
+                          int(queries), 0, None, None, float(softmax_scale))
         if group_start is not None:
-            self.prefix_lens = _ints(prefix_lens, "prefix_lens")
-            self.group_start = _ints(group_start, "group_start", self.prefix_lens.size + 1)
+            self.prefix_lens = _ints(prefix_lens, "prefix_lens").copy()
+            self.group_start = _ints(group_start, "group_start",
+                                     self.prefix_lens.size + 1).copy()
             self.c.groups = self.prefix_lens.size
-            self.c.group_start = _ptr(self.group_start)
-            self.c.prefix_lens = _ptr(self.prefix_lens)
+            self.c.group_start = self.group_start.ctypes.data
+            self.c.prefix_lens = self.prefix_lens.ctypes.data
         self.ref = ctypes.byref(self.c)
 
 
@@ -227,20 +253,19 @@ def decode_attn(q, cache: Cache, layer, batch: DecodeBatch, out=None, workspace=
                 stream=None):
     """Attention of the batch's query tokens over their sequences.  q: [batch * queries, Hq, d]
     bf16, rows contiguous, sequence by sequence; returns o of the same shape."""
-    import torch
     T, hq, d = batch.c.batch * batch.c.queries, batch.c.num_q_heads, cache.c.head_dim
     stride = _check_rows(q, "q", hq, d)
-    if q.shape[0] != T:
-        raise ValueError(f"q has {q.shape[0]} rows; the batch has {T} query tokens")
+    if len(q) != T:
+        raise ValueError(f"q has {len(q)} rows; the batch has {T} query tokens")
     if out is None:
-        out = _workspace(2 * T * hq * d, q.device, stream).view(torch.bfloat16).view(T, hq, d)
-    _check_tensor(out, "out", 3)
-    if tuple(out.shape) != (T, hq, d):
-        raise ValueError(f"out has shape {tuple(out.shape)}; the batch needs {(T, hq, d)}")
+        out = _workspace(2 * T * hq * d, q.device, stream).view(_t().bfloat16).view(T, hq, d)
+    else:
+        _check_tensor(out, "out", 3)
+        if out.shape != (T, hq, d):
+            raise ValueError(f"out has shape {tuple(out.shape)}; the batch needs {(T, hq, d)}")
     if workspace is None:
         workspace = _workspace(decode_workspace_size(cache, batch), q.device, stream)
-    _check(lib().fp_decode_attn(cache.ref, batch.ref, int(layer), ctypes.c_void_p(q.data_ptr()),
-                                stride, ctypes.c_void_p(out.data_ptr()),
-                                ctypes.c_void_p(workspace.data_ptr()), workspace.numel(),
-                                _stream_ptr(stream)), "fp_decode_attn")
+    _call(lib().fp_decode_attn(cache.ref, batch.ref, layer, q.data_ptr(), stride,
+                               out.data_ptr(), workspace.data_ptr(), workspace.numel(),
+                               _stream(stream)), "fp_decode_attn")
     return out

@@ -13,13 +13,14 @@ namespace {
 constexpr int kPlanThreads = 1024;   // the single workgroup that hands out pages
 constexpr int kCopyUnits = 1024;     // 16-byte units of a page copied by one workgroup at a time
 constexpr int kCopyGrid = 2048;      // workgroups of a copy whose length the host cannot know
+constexpr int kBatch = kForkChildren;   // table rows that one thread takes a place of
 
 struct __attribute__((aligned(16))) Unit {
   uint32_t x[4];
 };
 
-// Exclusive prefix sum over the workgroup (kPlanThreads threads) and the total; `part` is
-// 17 ints of LDS.
+// Exclusive prefix sum over the workgroup (kPlanThreads threads) and the total; `part` is an int
+// of LDS per wave.
 __device__ __forceinline__ int block_scan(int x, int *part, int &total) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   int sum = x;
@@ -31,28 +32,25 @@ __device__ __forceinline__ int block_scan(int x, int *part, int &total) {
   __syncthreads();                   // earlier reads of `part` are done
   if (lane == 63) part[w] = sum;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    int run = 0;
-    for (int i = 0; i < kPlanThreads / 64; ++i) {
-      const int y = part[i];
-      part[i] = run;
-      run += y;
-    }
-    part[kPlanThreads / 64] = run;
+  int base = 0;
+  total = 0;
+#pragma unroll
+  for (int i = 0; i < kPlanThreads / 64; ++i) {
+    const int y = part[i];
+    if (i < w) base += y;
+    total += y;
   }
-  __syncthreads();
-  total = part[kPlanThreads / 64];
-  return part[w] + sum - x;
+  return base + sum - x;
 }
 
 __device__ __forceinline__ int pages_of(int tokens, int shift) {
   return (int)(((unsigned)tokens + (1u << shift) - 1) >> shift);
 }
 
-// One holder less of page p; its bit is cleared when it was the last.  Returns 1 then.
-__device__ __forceinline__ int drop_page(const CacheView &c, int p) {
-  if ((unsigned)p >= (unsigned)c.pages) return 0;
-  if (atomicSub(c.ref + p, 1) != 1) return 0;
+// n holders less of page p; its bit is cleared when they were the last.  Returns 1 then.
+__device__ __forceinline__ int drop_page(const CacheView &c, int p, int n) {
+  if (n == 0 || (unsigned)p >= (unsigned)c.pages) return 0;
+  if (atomicSub(c.ref + p, n) != n) return 0;
   atomicAnd(c.used + (p >> 6), ~(1ull << (p & 63)));
   return 1;
 }
@@ -81,7 +79,7 @@ __global__ __launch_bounds__(256) void cache_init(CacheView c) {
 // Latency bound (one workgroup, a chain of about six loads).
 __global__ __launch_bounds__(kPlanThreads) void cache_reserve(CacheView c, CacheList l,
                                                               PageCopies w) {
-  __shared__ int part[kPlanThreads / 64 + 1];
+  __shared__ int part[kPlanThreads / 64];
   __shared__ int s_slot[FP_MAX_CACHE_LIST], s_held[FP_MAX_CACHE_LIST];
   __shared__ int s_begin[FP_MAX_CACHE_LIST + 1], s_tail[FP_MAX_CACHE_LIST];
   __shared__ int s_copy[FP_MAX_CACHE_LIST];      // index of the slot's copy, or -1
@@ -164,7 +162,7 @@ __global__ __launch_bounds__(kPlanThreads) void cache_reserve(CacheView c, Cache
     s_free[tid] = fr;
     __syncthreads();
     const int lane = tid & 63;
-    for (int i = tid >> 6; i < kPlanThreads; i += kPlanThreads / 64) {
+    for (int i = tid >> 6; i < min(kPlanThreads, c.words - w0); i += kPlanThreads / 64) {
       const unsigned long long f = s_free[i];
       const int first = s_base[i];
       if (f == 0 || first >= total) continue;
@@ -190,34 +188,36 @@ __global__ __launch_bounds__(kPlanThreads) void cache_reserve(CacheView c, Cache
   }
 }
 
-// Part `part` (kCopyUnits 16-byte units) of page copy `i` in one layer of K or V; jobs are
-// numbered part fastest.  Plain 16-byte loads and stores, four in flight per thread.
-__device__ __forceinline__ void copy_job(const CacheView &c, const PageCopies &w, int64_t job,
-                                         int units, int parts) {
-  const int part = (int)(job % parts);
-  int64_t r = job / parts;
-  const int kv = (int)(r & 1);
-  r >>= 1;
-  const int layer = (int)(r % c.layers), i = (int)(r / c.layers);
-  if ((unsigned)w.src[i] >= (unsigned)c.pages || (unsigned)w.dst[i] >= (unsigned)c.pages) return;
-  uint16_t *pool = (kv ? c.v : c.k) + (int64_t)layer * c.pages * units * 8;
-  const Unit *from = (const Unit *)pool + (int64_t)w.src[i] * units;
-  Unit *to = (Unit *)pool + (int64_t)w.dst[i] * units;
-  const int u0 = part * kCopyUnits + threadIdx.x;
-  Unit x[kCopyUnits / 256];
-#pragma unroll
-  for (int j = 0; j < kCopyUnits / 256; ++j)
-    if (u0 + 256 * j < units) x[j] = from[u0 + 256 * j];
-#pragma unroll
-  for (int j = 0; j < kCopyUnits / 256; ++j)
-    if (u0 + 256 * j < units) to[u0 + 256 * j] = x[j];
-}
-
+// The page copies of a list in every layer.  blockIdx.x is a part (kCopyUnits 16-byte units) of a
+// page of K or V in one layer, blockIdx.y and every gridDim.y-th after it a copy.  Plain 16-byte
+// loads and stores, four in flight per thread.
 __device__ __forceinline__ void copy_pages(const CacheView &c, const PageCopies &w) {
   const int units = c.hkv * c.page * c.d / 8;
   const int parts = (units + kCopyUnits - 1) / kCopyUnits;
-  const int64_t jobs = (int64_t)w.count[0] * c.layers * 2 * parts;
-  for (int64_t job = blockIdx.x; job < jobs; job += gridDim.x) copy_job(c, w, job, units, parts);
+  const int pool = blockIdx.x / parts;                   // layer and K or V
+  uint16_t *base = (pool & 1 ? c.v : c.k) + (int64_t)(pool >> 1) * c.pages * units * 8;
+  const int u0 = (blockIdx.x - pool * parts) * kCopyUnits + threadIdx.x;
+  const int n = w.count[0];
+  for (int i = blockIdx.y; i < n; i += gridDim.y) {
+    const int src = w.src[i], dst = w.dst[i];
+    if ((unsigned)src >= (unsigned)c.pages || (unsigned)dst >= (unsigned)c.pages) continue;
+    const Unit *from = (const Unit *)base + (int64_t)src * units;
+    Unit *to = (Unit *)base + (int64_t)dst * units;
+    Unit x[kCopyUnits / 256];
+#pragma unroll
+    for (int j = 0; j < kCopyUnits / 256; ++j)
+      if (u0 + 256 * j < units) x[j] = from[u0 + 256 * j];
+#pragma unroll
+    for (int j = 0; j < kCopyUnits / 256; ++j)
+      if (u0 + 256 * j < units) to[u0 + 256 * j] = x[j];
+  }
+}
+
+dim3 copy_grid(const CacheView &c, int most) {
+  const int units = c.hkv * c.page * c.d / 8;
+  const int64_t x = (int64_t)c.layers * 2 * ((units + kCopyUnits - 1) / kCopyUnits);
+  const int64_t y = x < kCopyGrid ? (kCopyGrid + x - 1) / x : 1;
+  return dim3((unsigned)x, (unsigned)(y < most ? y : most));
 }
 
 __global__ __launch_bounds__(256) void cache_copy(CacheView c, PageCopies w) { copy_pages(c, w); }
@@ -230,14 +230,15 @@ template <int D>
 __global__ __launch_bounds__(256) void cache_write(CacheView c, WriteArgs a) {
   constexpr int CPR = D / 8;                 // 16-byte chunks per row
   __shared__ __attribute__((aligned(16))) uint16_t tile[64][D + 8];
-  int i = 0, hi = a.list.n;                  // the slot whose blocks hold blockIdx.x
-  while (hi - i > 1) {
-    const int mid = (i + hi) / 2;
-    if (a.blk[mid] <= (int)blockIdx.x) i = mid;
-    else hi = mid;
-  }
-  if (c.state[1] & (FP_CACHE_FULL | FP_CACHE_TOO_LONG)) return;
+  __shared__ int s_i;
   const int h = blockIdx.y, tid = threadIdx.x;
+  // the slot whose blocks hold blockIdx.x: one thread's
+  if (tid < a.list.n && a.blk[tid] <= (int)blockIdx.x && (int)blockIdx.x < a.blk[tid + 1])
+    s_i = tid;
+  const int error = c.state[1];
+  __syncthreads();
+  const int i = __builtin_amdgcn_readfirstlane(s_i);
+  if (error & (FP_CACHE_FULL | FP_CACHE_TOO_LONG)) return;
   const int row0 = a.list.num[i], n = a.list.num[i + 1] - row0;
   const int slot = a.list.slot[i];
   const int len = min(c.len[slot], c.max_pages << c.page_shift);
@@ -291,53 +292,80 @@ __global__ __launch_bounds__(256) void cache_write(CacheView c, WriteArgs a) {
   }
 }
 
-// ---- fork: a thread takes one place of the source's table to its copies.  The source keeps its
-// pages throughout, so a page is never free in between, whatever the order of the counts.
+// ---- fork: a thread takes one place of the source's table to kBatch of its copies.  The source
+// keeps its pages throughout, so a page is never free in between, whatever the order of the counts.
+// Copies of one source, and what they held before (often the same pages), share their atomics.
 __global__ __launch_bounds__(256) void cache_fork(CacheView c, ForkArgs a) {
-  if (c.state[1] != 0) return;
   const int item = blockIdx.y, j = blockIdx.x * 256 + threadIdx.x;
   const int src = a.src[item], first = a.first[item], n = a.first[item + 1] - first;
+  if (c.state[1] != 0) return;
   int gone = 0;
   if (j < c.max_pages) {
     const int p = c.table[(int64_t)src * c.max_pages + j];
-    int more = 0;
-    for (int i = 0; i < n; ++i) {
-      int32_t *to = c.table + (int64_t)a.dst[first + i] * c.max_pages + j;
-      const int old = *to;
-      if (old == p) continue;
-      *to = p;
+    int old[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i)
+      old[i] = i < n ? c.table[(int64_t)a.dst[first + i] * c.max_pages + j] : p;
+    int more = 0, run = -1, less = 0;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      if (old[i] == p) continue;
+      c.table[(int64_t)a.dst[first + i] * c.max_pages + j] = p;
       ++more;
-      if (old >= 0) gone += drop_page(c, old);
+      if (old[i] != run) {
+        gone += drop_page(c, run, less);
+        run = old[i];
+        less = 0;
+      }
+      ++less;
     }
+    gone += drop_page(c, run, less);
     if (more && (unsigned)p < (unsigned)c.pages) atomicAdd(c.ref + p, more);
   }
   count_freed(c, gone);
   if (blockIdx.x == 0 && threadIdx.x < n) c.len[a.dst[first + threadIdx.x]] = c.len[src];
 }
 
-// ---- truncate: a thread gives back one place of a slot's table
+// ---- truncate: a thread gives back one place of the tables of kBatch slots; neighbours in the list
+// that hold the same page share an atomic
 __global__ __launch_bounds__(256) void cache_truncate(CacheView c, CacheList l) {
-  if (c.state[1] != 0) return;
-  const int slot = l.slot[blockIdx.y], keep = l.num[blockIdx.y];
+  const int first = blockIdx.y * kBatch, n = min(l.n - first, kBatch);
   const int j = blockIdx.x * 256 + threadIdx.x;
+  if (c.state[1] != 0) return;
   int gone = 0;
-  if (j < c.max_pages && j >= pages_of(keep, c.page_shift)) {
-    int32_t *at = c.table + (int64_t)slot * c.max_pages + j;
-    const int p = *at;
-    if (p >= 0) {
-      *at = -1;
-      gone = drop_page(c, p);
+  if (j < c.max_pages) {
+    int old[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i)
+      old[i] = i < n && j >= pages_of(l.num[first + i], c.page_shift)
+                   ? c.table[(int64_t)l.slot[first + i] * c.max_pages + j]
+                   : -1;
+    int run = -1, less = 0;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      if (old[i] < 0) continue;
+      c.table[(int64_t)l.slot[first + i] * c.max_pages + j] = -1;
+      if (old[i] != run) {
+        gone += drop_page(c, run, less);
+        run = old[i];
+        less = 0;
+      }
+      ++less;
     }
+    gone += drop_page(c, run, less);
   }
   count_freed(c, gone);
-  if (j == 0) c.len[slot] = min(c.len[slot], keep);
+  if (blockIdx.x == 0 && threadIdx.x < n) {
+    int32_t *len = c.len + l.slot[first + threadIdx.x];
+    *len = min(*len, l.num[first + threadIdx.x]);
+  }
 }
 
 // ---- compact: one workgroup pairs holes with the pages behind them, a second launch copies the
 // pages and renames them in the tables.  Sources lie at or above state[0] and targets below, so
 // no copy reads what another writes.
 __global__ __launch_bounds__(kPlanThreads) void cache_compact_plan(CacheView c, PageCopies w) {
-  __shared__ int part[kPlanThreads / 64 + 1];
+  __shared__ int part[kPlanThreads / 64];
   __shared__ int s_base[kPlanThreads];
   __shared__ unsigned long long s_bits[kPlanThreads];
   const int tid = threadIdx.x, lane = tid & 63;
@@ -364,7 +392,7 @@ __global__ __launch_bounds__(kPlanThreads) void cache_compact_plan(CacheView c, 
       s_base[tid] = block_scan(__popcll(bits), part, found) + seen;
       s_bits[tid] = bits;
       __syncthreads();
-      for (int i = tid >> 6; i < kPlanThreads; i += kPlanThreads / 64) {
+      for (int i = tid >> 6; i < min(kPlanThreads, end_word - w0); i += kPlanThreads / 64) {
         const unsigned long long b = s_bits[i];
         if (!(b >> lane & 1)) continue;
         const int p = (w0 + i) * 64 + lane;
@@ -395,7 +423,8 @@ __global__ __launch_bounds__(kPlanThreads) void cache_compact_plan(CacheView c, 
 __global__ __launch_bounds__(256) void cache_compact_move(CacheView c, PageCopies w) {
   const int n = w.count[0], n_used = c.state[0];
   if (n == 0) return;
-  const int64_t me = (int64_t)blockIdx.x * 256 + threadIdx.x, all = (int64_t)gridDim.x * 256;
+  const int64_t me = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 256 + threadIdx.x;
+  const int64_t all = (int64_t)gridDim.x * gridDim.y * 256;
   for (int64_t i = me; i < n; i += all) {
     c.ref[w.dst[i]] = c.ref[w.src[i]];
     c.ref[w.src[i]] = 0;
@@ -419,9 +448,7 @@ hipError_t launch_cache_reserve(const CacheView &c, const CacheList &l, const Pa
   cache_reserve<<<1, kPlanThreads, 0, s>>>(c, l, w);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int64_t units = (int64_t)c.hkv * c.page * c.d / 8;
-  const int64_t most = (int64_t)l.n * c.layers * 2 * ((units + kCopyUnits - 1) / kCopyUnits);
-  cache_copy<<<(int)(most < kCopyGrid ? most : kCopyGrid), 256, 0, s>>>(c, w);
+  cache_copy<<<copy_grid(c, l.n), 256, 0, s>>>(c, w);
   return hipGetLastError();
 }
 
@@ -438,7 +465,8 @@ hipError_t launch_cache_fork(const CacheView &c, const ForkArgs &a, hipStream_t 
 }
 
 hipError_t launch_cache_truncate(const CacheView &c, const CacheList &l, hipStream_t s) {
-  cache_truncate<<<dim3((c.max_pages + 255) / 256, l.n), 256, 0, s>>>(c, l);
+  cache_truncate<<<dim3((c.max_pages + 255) / 256, (l.n + kBatch - 1) / kBatch), 256, 0, s>>>(c,
+                                                                                           l);
   return hipGetLastError();
 }
 
@@ -446,7 +474,7 @@ hipError_t launch_cache_compact(const CacheView &c, const PageCopies &w, hipStre
   cache_compact_plan<<<1, kPlanThreads, 0, s>>>(c, w);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  cache_compact_move<<<kCopyGrid, 256, 0, s>>>(c, w);
+  cache_compact_move<<<copy_grid(c, (c.pages + 1) / 2), 256, 0, s>>>(c, w);
   return hipGetLastError();
 }
 
