@@ -617,24 +617,13 @@ fp_status fp_cache_fork(const fp_cache *cache, int32_t n, const int32_t *src, co
   SlotSet seen;
   if ((st = check_slots(cache, n, dst, &seen)) != FP_OK) return st;
   if ((st = check_slots(cache, n, src, nullptr)) != FP_OK) return st;
-  for (int i = 0; i < n; ++i)
-    if (seen.has(src[i])) return FP_ERR_INVALID_ARG;
-  // destinations by source, at most kForkChildren to an item
   fp::ForkArgs a;
-  int16_t order[FP_MAX_CACHE_LIST];
-  for (int i = 0; i < n; ++i) order[i] = (int16_t)i;
-  std::stable_sort(order, order + n, [&](int x, int y) { return src[x] < src[y]; });
-  a.items = 0;
+  a.n = n;
   for (int i = 0; i < n; ++i) {
-    const int32_t s = src[order[i]];
-    if (a.items == 0 || a.src[a.items - 1] != s ||
-        i - a.first[a.items - 1] == fp::kForkChildren) {
-      a.src[a.items] = s;
-      a.first[a.items++] = i;
-    }
-    a.dst[i] = dst[order[i]];
+    if (seen.has(src[i])) return FP_ERR_INVALID_ARG;
+    a.src[i] = src[i];
+    a.dst[i] = dst[i];
   }
-  a.first[a.items] = n;
   const hipError_t e = fp::launch_cache_fork(c, a, (hipStream_t)stream);
   return e == hipSuccess ? FP_OK : hip_fail(e, "fp_cache_fork");
 }

@@ -13,7 +13,7 @@ namespace {
 constexpr int kPlanThreads = 1024;   // the single workgroup that hands out pages
 constexpr int kCopyUnits = 1024;     // 16-byte units of a page copied by one workgroup at a time
 constexpr int kCopyGrid = 2048;      // workgroups of a copy whose length the host cannot know
-constexpr int kBatch = kForkChildren;   // table rows that one thread takes a place of
+constexpr int kBatch = 16;           // table rows that one thread takes a place of
 
 struct __attribute__((aligned(16))) Unit {
   uint32_t x[4];
@@ -47,12 +47,28 @@ __device__ __forceinline__ int pages_of(int tokens, int shift) {
   return (int)(((unsigned)tokens + (1u << shift) - 1) >> shift);
 }
 
-// n holders less of page p; its bit is cleared when they were the last.  Returns 1 then.
-__device__ __forceinline__ int drop_page(const CacheView &c, int p, int n) {
-  if (n == 0 || (unsigned)p >= (unsigned)c.pages) return 0;
-  if (atomicSub(c.ref + p, n) != n) return 0;
-  atomicAnd(c.used + (p >> 6), ~(1ull << (p & 63)));
-  return 1;
+// One holder less of each page listed (-1: none) for kBatch entries of a thread; neighbours that
+// name the same page share an atomic, and all of a thread's are in flight together.  Bits of pages
+// without holders are cleared; returns how many there are.
+__device__ __forceinline__ int drop_pages(const CacheView &c, const int (&page)[kBatch]) {
+  int less[kBatch], before[kBatch], run = 0, gone = 0;
+#pragma unroll
+  for (int i = 0; i < kBatch; ++i) {
+    run = page[i] >= 0 && page[i] < c.pages ? run + 1 : 0;
+    const bool last = i + 1 == kBatch || page[i + 1] != page[i];
+    less[i] = last ? run : 0;
+    if (last) run = 0;
+  }
+#pragma unroll
+  for (int i = 0; i < kBatch; ++i)
+    if (less[i]) before[i] = atomicSub(c.ref + page[i], less[i]);
+#pragma unroll
+  for (int i = 0; i < kBatch; ++i)
+    if (less[i] && before[i] == less[i]) {
+      atomicAnd(c.used + (page[i] >> 6), ~(1ull << (page[i] & 63)));
+      ++gone;
+    }
+  return gone;
 }
 
 // state[0] less `gone` summed over the workgroup's waves.
@@ -292,42 +308,41 @@ __global__ __launch_bounds__(256) void cache_write(CacheView c, WriteArgs a) {
   }
 }
 
-// ---- fork: a thread takes one place of the source's table to kBatch of its copies.  The source
+// ---- fork: a thread takes one place of the tables of kBatch sources to their copies.  A source
 // keeps its pages throughout, so a page is never free in between, whatever the order of the counts.
-// Copies of one source, and what they held before (often the same pages), share their atomics.
+// Neighbours that share a page share its atomics: samples of one prompt hold mostly the same.
 __global__ __launch_bounds__(256) void cache_fork(CacheView c, ForkArgs a) {
-  const int item = blockIdx.y, j = blockIdx.x * 256 + threadIdx.x;
-  const int src = a.src[item], first = a.first[item], n = a.first[item + 1] - first;
+  const int first = blockIdx.y * kBatch, n = min(a.n - first, kBatch);
+  const int j = blockIdx.x * 256 + threadIdx.x;
   if (c.state[1] != 0) return;
   int gone = 0;
   if (j < c.max_pages) {
-    const int p = c.table[(int64_t)src * c.max_pages + j];
-    int old[kBatch];
-#pragma unroll
-    for (int i = 0; i < kBatch; ++i)
-      old[i] = i < n ? c.table[(int64_t)a.dst[first + i] * c.max_pages + j] : p;
-    int more = 0, run = -1, less = 0;
+    int now[kBatch], old[kBatch];
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
-      if (old[i] == p) continue;
-      c.table[(int64_t)a.dst[first + i] * c.max_pages + j] = p;
-      ++more;
-      if (old[i] != run) {
-        gone += drop_page(c, run, less);
-        run = old[i];
-        less = 0;
-      }
-      ++less;
+      now[i] = i < n ? c.table[(int64_t)a.src[first + i] * c.max_pages + j] : -1;
+      old[i] = i < n ? c.table[(int64_t)a.dst[first + i] * c.max_pages + j] : -1;
     }
-    gone += drop_page(c, run, less);
-    if (more && (unsigned)p < (unsigned)c.pages) atomicAdd(c.ref + p, more);
+    int more = 0;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const bool change = now[i] != old[i];
+      if (change) c.table[(int64_t)a.dst[first + i] * c.max_pages + j] = now[i];
+      else old[i] = -1;
+      more += change;
+      if (i + 1 == kBatch || now[i + 1] != now[i]) {
+        if (more && (unsigned)now[i] < (unsigned)c.pages) atomicAdd(c.ref + now[i], more);
+        more = 0;
+      }
+    }
+    gone = drop_pages(c, old);
   }
   count_freed(c, gone);
-  if (blockIdx.x == 0 && threadIdx.x < n) c.len[a.dst[first + threadIdx.x]] = c.len[src];
+  if (blockIdx.x == 0 && threadIdx.x < n)
+    c.len[a.dst[first + threadIdx.x]] = c.len[a.src[first + threadIdx.x]];
 }
 
-// ---- truncate: a thread gives back one place of the tables of kBatch slots; neighbours in the list
-// that hold the same page share an atomic
+// ---- truncate: a thread gives back one place of the tables of kBatch slots
 __global__ __launch_bounds__(256) void cache_truncate(CacheView c, CacheList l) {
   const int first = blockIdx.y * kBatch, n = min(l.n - first, kBatch);
   const int j = blockIdx.x * 256 + threadIdx.x;
@@ -340,19 +355,10 @@ __global__ __launch_bounds__(256) void cache_truncate(CacheView c, CacheList l) 
       old[i] = i < n && j >= pages_of(l.num[first + i], c.page_shift)
                    ? c.table[(int64_t)l.slot[first + i] * c.max_pages + j]
                    : -1;
-    int run = -1, less = 0;
 #pragma unroll
-    for (int i = 0; i < kBatch; ++i) {
-      if (old[i] < 0) continue;
-      c.table[(int64_t)l.slot[first + i] * c.max_pages + j] = -1;
-      if (old[i] != run) {
-        gone += drop_page(c, run, less);
-        run = old[i];
-        less = 0;
-      }
-      ++less;
-    }
-    gone += drop_page(c, run, less);
+    for (int i = 0; i < kBatch; ++i)
+      if (old[i] >= 0) c.table[(int64_t)l.slot[first + i] * c.max_pages + j] = -1;
+    gone = drop_pages(c, old);
   }
   count_freed(c, gone);
   if (blockIdx.x == 0 && threadIdx.x < n) {
@@ -460,7 +466,7 @@ hipError_t launch_cache_write(const CacheView &c, const WriteArgs &a, hipStream_
 }
 
 hipError_t launch_cache_fork(const CacheView &c, const ForkArgs &a, hipStream_t s) {
-  cache_fork<<<dim3((c.max_pages + 255) / 256, a.items), 256, 0, s>>>(c, a);
+  cache_fork<<<dim3((c.max_pages + 255) / 256, (a.n + kBatch - 1) / kBatch), 256, 0, s>>>(c, a);
   return hipGetLastError();
 }
 

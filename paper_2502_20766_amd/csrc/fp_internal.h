@@ -174,13 +174,9 @@ struct WriteArgs {
   int32_t layer;
 };
 
-// Forks of one source to at most kForkChildren slots, one workgroup column each.
-constexpr int kForkChildren = 16;
 struct ForkArgs {
-  int32_t items;
-  int32_t src[FP_MAX_CACHE_LIST];
-  int32_t first[FP_MAX_CACHE_LIST + 1];   // item -> its first entry of dst
-  int32_t dst[FP_MAX_CACHE_LIST];
+  int32_t n;
+  int32_t src[FP_MAX_CACHE_LIST], dst[FP_MAX_CACHE_LIST];
 };
 
 // What the joining launch of decode_attn knows of the call's plan (workspace).
