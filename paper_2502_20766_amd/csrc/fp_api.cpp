@@ -332,7 +332,7 @@ fp_status check_decode(const fp_cache *c, const fp_decode *b, DecodeDims *dm) {
       if (m > 1 && b->prefix_lens[g] > 0) {
         (m * dm->rows > fp::kDecodeFew ? dm->many : dm->few) = true;
         if (m * dm->rows > 16 && m * dm->rows <= fp::kDecodeFew) dm->tile_rows = 32;
-        cost += ((int64_t)m * dm->rows / fp::kDecodeRows + 1) *
+        cost += ((int64_t)m * dm->rows / 16 + 1) *
                 (std::min(most, ((int64_t)b->prefix_lens[g] + 63) / 64) + 8);
       }
     }
@@ -343,12 +343,14 @@ fp_status check_decode(const fp_cache *c, const fp_decode *b, DecodeDims *dm) {
   const size_t wgs = fp::decode_wgs(c->head_dim), row = 4 * (size_t)(c->head_dim + 2);
   const size_t own = wgs + (size_t)b->batch * c->num_kv_heads * dm->tiles;
   dm->bytes_own = align_up(own * dm->tile_rows * row);
-  const size_t few = wgs + (size_t)c->num_kv_heads * b->groups;
-  dm->bytes_few = dm->few ? align_up(few * dm->tile_rows * row) : 0;
-  // a group's row tiles start at (its first row) / kDecodeRows + its number
-  const size_t many = wgs + (size_t)c->num_kv_heads *
-                                ((size_t)b->batch * dm->rows / fp::kDecodeRows + b->groups + 1);
-  dm->bytes_many = dm->many ? align_up(many * fp::kDecodeRows * row) : 0;
+  // a group's row tiles start at (its first row) / (rows of a tile) + its number
+  auto prefixes = [&](bool any, int tile) -> size_t {
+    if (!any) return 0;
+    const size_t tiles = (size_t)b->batch * dm->rows / tile + b->groups + 1;
+    return align_up((wgs + c->num_kv_heads * tiles) * tile * row);
+  };
+  dm->bytes_few = prefixes(dm->few, dm->tile_rows);
+  dm->bytes_many = prefixes(dm->many, fp::kDecodeRows);
   return FP_OK;
 }
 

@@ -6,16 +6,18 @@
 //   O_R = sum w_j v_j,  l_R = sum w_j;   o = (sum_R 2^(m_R - M) O_R) / (sum_R 2^(m_R - M) l_R).
 // The ranges are cut as follows.  A segment is the work of one KV head and one tile of query rows
 // over one run of keys: the prefix of a group (rows: all query heads of the KV head, all queries,
-// all sequences of the group) or the rest of one sequence (rows: its own).  All segments, one
-// after the other in tiles of 64 keys, form a line that is cut into equal parts, one for each
-// resident workgroup, so every workgroup has the same work whatever the lengths.  A piece (the
-// part of a segment in one workgroup) leaves O_R, m_R and l_R in float32; a last launch joins the
-// pieces of each row in the order of the line.  A segment in one piece whose rows have no prefix
-// is finished on the spot.  Where the cuts fall follows from the lengths alone, so results do not
-// depend on timing.
+// all sequences of the group) or the rest of one sequence (rows: its own).  Segments, one after the
+// other in tiles of 64 keys, form a line that is cut into equal parts, one for each workgroup, so
+// every workgroup has the same work whatever the lengths.  A piece (the part of a segment in one
+// workgroup) leaves O_R, m_R and l_R in float32; a last launch joins the pieces of each row in the
+// order of the line.  A segment in one piece whose rows have no prefix is finished on the spot.
+// Where the cuts fall follows from the lengths alone, so results do not depend on timing.
 //
-// Segments with up to 32 rows are bound by the bytes of their keys, those with more by their
-// products, so there are two kernels, each with a line of its own (decode_lean, decode_many).
+// Segments with few rows are bound by the bytes of their keys, prefixes with many by their products,
+// so there are two ways to take a piece (lean_pieces, many_pieces) and two lines.  One launch takes
+// both: the resident workgroups are divided between the lines by their work, so that neither waits
+// for the other.  Workgroups that take the row tiles of one prefix go through the same keys side by
+// side (a cluster), so that those come from memory once.
 #include <type_traits>
 
 #include "fp_attn_dev.h"
@@ -36,6 +38,9 @@ constexpr int kSegCost = 2;
 
 static_assert(kThreads == kMaxList, "the plan has one thread per sequence");
 
+// Entries of the lean line: group g is entry g, sequence b is kOwn + b.
+constexpr int kOwn = kMaxList, kEnd = 2 * kMaxList;
+
 // The lines of a call.  Starts are the places where the segments of a group's prefix and of a
 // sequence's own keys begin; an entry without keys has the start of the next one.
 struct Plan {
@@ -43,9 +48,10 @@ struct Plan {
   int prefix[kMaxList];                   // per group: keys read once, a multiple of 16
   int lead[kMaxList];                     // per group: a sequence whose pages hold them
   int live[kMaxList];
-  int lean[2 * kMaxList + 1];             // starts: groups, then sequences at kMaxList + b
-  int many[kMaxList + 1];                 // starts of the groups that are on the other line
+  int many[kMaxList + 1];                 // line of many rows: groups, the end
+  int lean[2 * kMaxList + 1];             // the other: groups, sequences (from kOwn), the end
   int scan[3][4];
+  int rows_lo, rows_hi;                   // fewest and most row tiles of a group of many rows
   int first;                              // entry that this workgroup's part begins in
 };
 
@@ -55,12 +61,12 @@ __device__ __forceinline__ int group_rows(const DecodeArgs &a, int g) {
   return (a.start[g + 1] - a.start[g]) * a.nq * a.G;
 }
 
-// Groups whose prefix is on the line of many rows.
+// Groups whose prefix is taken as one of many rows.
 __device__ __forceinline__ bool is_many(const DecodeArgs &a, int g) {
   return group_rows(a, g) > kDecodeFew;
 }
 
-// Row tiles: kDecodeRows rows on the line of many, a.tile_rows (16 or 32) on the other.
+// Row tiles: of kDecodeRows rows for prefixes of many, of a.tile_rows (16 or 32) else.
 __device__ __forceinline__ int many_tiles(int rows) {
   return (rows + kDecodeRows - 1) / kDecodeRows;
 }
@@ -68,11 +74,10 @@ __device__ __forceinline__ int lean_tiles(const DecodeArgs &a, int rows) {
   return (rows + a.tile_rows - 1) / a.tile_rows;
 }
 
-// Number of the partial result of row tile 0 and KV head 0 of a prefix, less its workgroup's: the
-// tiles of a group of many rows start at (its first row) / kDecodeRows + its number; a prefix of
-// few rows is one tile.
+// Number of the partial result of row tile 0 and KV head 0 of a prefix, less its workgroup's: a
+// group's row tiles start at (its first row) / (rows of a tile) + its number.
 __device__ __forceinline__ int prefix_base(const DecodeArgs &a, int g, bool many) {
-  return (many ? a.start[g] * a.nq * a.G / kDecodeRows + g : g) * a.hkv;
+  return (a.start[g] * a.nq * a.G / (many ? kDecodeRows : a.tile_rows) + g) * a.hkv;
 }
 
 // A line of `total` places in `wgs` equal parts, the first total % wgs of them one place longer.
@@ -86,20 +91,44 @@ struct Cut {
   }
 };
 
-// This workgroup's part of its line.
-struct Part {
-  int lo, hi, wg;
+// How the workgroups are divided: `clusters` times `width` of them take the line of many rows, a
+// cluster one part of it and each of its workgroups one row tile; `lean` the other line.
+struct Shares {
+  int clusters, width, lean;
 };
 
-// Fills the plan and finds this workgroup's part of the line, and the entry it begins in.  Empty
-// parts have lo == hi.
-template <bool MANY>
+// This workgroup's part of its line.
+struct Part {
+  int many;             // which line
+  int lo, hi;           // places; lo == hi: none
+  int wg;               // number of the part
+  int tile;             // many: row tile, when the cluster has one for each
+};
+
+// Work of the lines (`many` per row tile) in shares of a.wgs workgroups.
+__device__ __forceinline__ Shares divide(int wgs, int many, int width, int lean) {
+  Shares r = {0, width, 0};
+  if (many > 0) {
+    const float work = (float)many * width;
+    const int most = (wgs - (lean > 0 ? 1 : 0)) / width;
+    r.clusters = (int)((float)wgs / width * (work / (work + lean)) + 0.5f);
+    r.clusters = max(1, min(min(r.clusters, most), many));
+  }
+  r.lean = min(wgs - r.clusters * width, lean);
+  return r;
+}
+
+// Fills the plan and finds this workgroup's part and the entry it begins in.
 __device__ __forceinline__ Part make_plan(const DecodeArgs &a, Plan &p) {
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
   if (t < a.groups) {
     p.prefix[t] = 0x7FFFFFFF;
     p.lead[t] = kMaxList - 1;
     p.live[t] = 0;
+  }
+  if (t == 0) {
+    p.rows_lo = 0x7FFFFFFF;
+    p.rows_hi = 0;
   }
   int len = 0, g = 0;
   if (t < a.batch) {
@@ -115,91 +144,107 @@ __device__ __forceinline__ Part make_plan(const DecodeArgs &a, Plan &p) {
   }
   __syncthreads();
   int cost[3] = {0, 0, 0};                // groups of many rows, of few, own keys
+  int tiles = 0;
   if (t < a.groups) {
     // one sequence alone has nothing to share
     const int keys = p.live[t] >= 2 ? min(p.prefix[t], a.prefix[t]) & ~15 : 0;
     if (keys > 0) {
       const bool many = is_many(a, t);
-      const int tiles = many ? many_tiles(group_rows(a, t)) : 1;
-      cost[many ? 0 : 1] = a.hkv * tiles * (tiles_of(keys) + kSegCost);
+      const int rows = group_rows(a, t);
+      tiles = many ? many_tiles(rows) : lean_tiles(a, rows);
+      cost[many ? 0 : 1] = a.hkv * (tiles_of(keys) + kSegCost);
+      if (many) {
+        atomicMin(&p.rows_lo, tiles);
+        atomicMax(&p.rows_hi, tiles);
+      }
     }
     p.prefix[t] = keys;
   }
   __syncthreads();
+  // a cluster per part where all prefixes have the same number of row tiles
+  const int width = p.rows_lo == p.rows_hi && p.rows_hi <= a.wgs / 4 ? p.rows_hi : 1;
+  if (width == 1) cost[0] *= tiles;
+  cost[1] *= tiles;
   if (len > 0)
     cost[2] = a.hkv * lean_tiles(a, a.G * a.nq) * (tiles_of(len - p.prefix[g]) + kSegCost);
-  int sum[3];
+  int start[3], total[3];
 #pragma unroll
   for (int i = 0; i < 3; ++i) {
-    sum[i] = cost[i];
+    start[i] = cost[i];
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
-      const int y = __shfl_up(sum[i], d);
-      if (lane >= d) sum[i] += y;
+      const int y = __shfl_up(start[i], d);
+      if (lane >= d) start[i] += y;
     }
-    if (lane == 63) p.scan[i][w] = sum[i];
+    if (lane == 63) p.scan[i][w] = start[i];
   }
   __syncthreads();
-  int total[3];
 #pragma unroll
   for (int i = 0; i < 3; ++i) {
+    start[i] -= cost[i];
     total[i] = 0;
-    sum[i] -= cost[i];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      if (j < w) sum[i] += p.scan[i][j];
+      if (j < w) start[i] += p.scan[i][j];
       total[i] += p.scan[i][j];
     }
   }
-  p.many[t] = sum[0];
-  p.lean[t] = sum[1];
-  p.lean[kMaxList + t] = total[1] + sum[2];
+  start[2] += total[1];
+  p.many[t] = start[0];
+  p.lean[t] = start[1];
+  p.lean[kOwn + t] = start[2];
+  const int places = total[1] + total[2];
   if (t == 0) {
     p.many[kMaxList] = total[0];
-    p.lean[2 * kMaxList] = total[1] + total[2];
+    p.lean[kEnd] = places;
   }
-  // Workgroups of one XCD (every eighth) take neighbouring parts of the line, which share keys.
-  Part r;
-  const int places = MANY ? total[0] : total[1] + total[2];
-  const int wgs = min(a.wgs, places);
-  r.wg = blockIdx.x;
-  if (wgs == a.wgs) r.wg = (r.wg & 7) * (a.wgs / 8) + (r.wg >> 3);
-  r.lo = r.hi = 0;
-  if (r.wg < wgs) {
-    const Cut cut(places, wgs);
+  const Shares sh = divide(a.wgs, total[0], width, places);
+  // Workgroups of one XCD (every eighth) take neighbouring parts, which share keys, unless there is
+  // not work for all.
+  const int crowd = sh.clusters * sh.width, used = crowd + sh.lean;
+  int wg = blockIdx.x;
+  if (8 * used > 7 * a.wgs) wg = (wg & 7) * (a.wgs / 8) + (wg >> 3);
+  Part r = {wg < crowd, 0, 0, 0, 0};
+  if (r.many) {
+    r.wg = wg / sh.width;
+    r.tile = wg - r.wg * sh.width;
+    const Cut cut(total[0], sh.clusters);
     r.lo = cut.begin(r.wg);
     r.hi = cut.begin(r.wg + 1);
-    if (MANY) {
-      if (sum[0] <= r.lo && r.lo < sum[0] + cost[0]) p.first = t;
-    } else {
-      if (sum[1] <= r.lo && r.lo < sum[1] + cost[1]) p.first = t;
-      const int own = total[1] + sum[2];
-      if (own <= r.lo && r.lo < own + cost[2]) p.first = kMaxList + t;
+    if (start[0] <= r.lo && r.lo < start[0] + cost[0]) p.first = t;
+  } else if (wg < used) {
+    r.wg = wg - crowd;
+    const Cut cut(places, sh.lean);
+    r.lo = cut.begin(r.wg);
+    r.hi = cut.begin(r.wg + 1);
+    if (start[1] <= r.lo && r.lo < start[1] + cost[1]) p.first = t;
+    if (start[2] <= r.lo && r.lo < start[2] + cost[2]) p.first = kOwn + t;
+  }
+  if (blockIdx.x == 0) {                  // what the joining launch needs of this
+    DecodeJoin &j = *a.join;
+    if (t < a.batch) {
+      j.len[t] = len;
+      j.own[t] = start[2];
+    }
+    if (t < a.groups) {
+      j.prefix[t] = p.prefix[t];
+      j.shared[t] = is_many(a, t) ? start[0] : start[1];
+    }
+    if (t == 0) {
+      j.places_many = total[0];
+      j.places_lean = places;
+      j.clusters = sh.clusters;
+      j.width = sh.width;
+      j.lean = sh.lean;
     }
   }
   __syncthreads();
+  r.many = __builtin_amdgcn_readfirstlane(r.many);
   r.lo = __builtin_amdgcn_readfirstlane(r.lo);
   r.hi = __builtin_amdgcn_readfirstlane(r.hi);
   r.wg = __builtin_amdgcn_readfirstlane(r.wg);
+  r.tile = sh.width > 1 ? __builtin_amdgcn_readfirstlane(r.tile) : -1;
   return r;
-}
-
-// What the joining launch needs of the plan, written by one workgroup of decode_lean.
-__device__ __forceinline__ void publish(const DecodeArgs &a, const Plan &p) {
-  const int t = threadIdx.x;
-  DecodeJoin &j = *a.join;
-  if (t < a.batch) {
-    j.len[t] = p.len[t];
-    j.own[t] = p.lean[kMaxList + t];
-  }
-  if (t < a.groups) {
-    j.prefix[t] = p.prefix[t];
-    j.shared[t] = is_many(a, t) ? p.many[t] : p.lean[t];
-  }
-  if (t == 0) {
-    j.total_many = p.many[kMaxList];
-    j.total_lean = p.lean[2 * kMaxList];
-  }
 }
 
 // A run of tiles of one segment in one workgroup; every field is wave-uniform.
@@ -217,25 +262,25 @@ struct Piece {
   int whole;            // the piece is all that its rows have
 };
 
-// The piece at place x < hi of the line, which lies in entry `e` or a later one.
+// The piece at place x of the workgroup's part, which lies in entry `e` or a later one.
 template <bool MANY>
 __device__ __forceinline__ Piece piece_at(const DecodeArgs &a, const Plan &p, int e, int x,
-                                          int hi, int wg) {
+                                          const Part &part) {
   const int *starts = MANY ? p.many : p.lean;
-  while (starts[e + 1] <= x) ++e;
+  while (starts[e + 1] <= x)
+    if (++e == a.groups && !MANY) e = kOwn;   // (the entries between are empty)
   Piece r;
   r.entry = __builtin_amdgcn_readfirstlane(e);
-  const bool shared = MANY || r.entry < kMaxList;
-  const int b = r.entry - kMaxList;
+  const bool shared = MANY || r.entry < kOwn;
+  const int b = r.entry - kOwn;
   const int g = shared ? r.entry : a.group[b];
   const int prefix = __builtin_amdgcn_readfirstlane(p.prefix[g]);
-  int rows, base, tiles, whole = 0;
+  int rows, base, whole = 0;
   if (shared) {
     r.row = a.slot[__builtin_amdgcn_readfirstlane(p.lead[g])];
     r.key0 = 0;
     r.limit = r.vis = prefix;
     rows = group_rows(a, g);
-    tiles = MANY ? many_tiles(rows) : 1;
     r.token0 = a.start[g] * a.nq;
     base = prefix_base(a, g, MANY);
   } else {
@@ -244,23 +289,25 @@ __device__ __forceinline__ Piece piece_at(const DecodeArgs &a, const Plan &p, in
     r.limit = __builtin_amdgcn_readfirstlane(p.len[b]);
     r.vis = r.limit - a.nq + 1;
     rows = a.G * a.nq;
-    tiles = lean_tiles(a, rows);
     r.token0 = b * a.nq;
-    base = b * a.hkv * tiles;
+    base = b * a.hkv * lean_tiles(a, rows);
     whole = prefix == 0;
   }
+  const bool cluster = MANY && part.tile >= 0;
+  const int tiles = cluster ? 1 : MANY ? many_tiles(rows) : lean_tiles(a, rows);
   const int n = tiles_of(r.limit - r.key0);
   const int start = __builtin_amdgcn_readfirstlane(starts[r.entry]);
   const int seg = (x - start) / (n + kSegCost);         // (KV head, row tile) of the entry
   const int at = start + seg * (n + kSegCost) + kSegCost;   // place of its first tile
   const int per = MANY ? kDecodeRows : a.tile_rows;
   r.head = seg / tiles;
-  r.row0 = (seg - r.head * tiles) * per;
+  r.row0 = (cluster ? part.tile : seg - r.head * tiles) * per;
   r.rows = min(rows - r.row0, per);
   r.t0 = max(x - at, 0);
-  r.t1 = max(min(hi - at, n), r.t0);
+  r.t1 = max(min(part.hi - at, n), r.t0);
   r.end = at + n;
-  r.slot = wg + base + seg;
+  r.slot = cluster ? (part.wg + g * a.hkv + seg) * many_tiles(rows) + part.tile
+                   : part.wg + base + seg;
   r.whole = whole && r.t0 == 0 && r.t1 == n;
   return r;
 }
@@ -334,6 +381,15 @@ __device__ __forceinline__ bool settle(uint8_t *v, int key0, int limit, int vis,
   return __ballot(odd) != 0;
 }
 
+// Waits for this wave's copies into LDS (and its other loads and stores).  The builtin, unlike the
+// same instruction in an asm statement, also tells the compiler, which would else wait for them
+// where their LDS is first read, after the next copies have been issued, and so for those too.
+__device__ __forceinline__ void wait_copies() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0F70);     // vmcnt(0)
+  asm volatile("" ::: "memory");
+}
+
 // Workgroup barrier that orders LDS accesses only: it waits for no copy and no store in flight.
 __device__ __forceinline__ void wg_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
@@ -360,32 +416,28 @@ __device__ __forceinline__ float quad_sum(float x) {
 //   twice: a weight is the sum of two bf16 numbers (error 2^-17), the second one in places where
 //   V^T is repeated.  That costs no product, and the keys' bytes bound the kernel anyway.
 template <int D, int RT>
-__global__ __launch_bounds__(kThreads)
-__attribute__((amdgpu_waves_per_eu(DecGeo<D>::OCC, DecGeo<D>::OCC)))
-void decode_lean(DecodeArgs a) {
+__device__ __forceinline__ void lean_pieces(const DecodeArgs &a, const Plan &plan, uint8_t *lds0,
+                                            uint8_t *lds1, float2 (*s_ml)[16],
+                                            const Part &part) {
   using S = DecGeo<D>;
   constexpr int KS = D / 32, DB = D / 16;
-  // [wave][2 steps][K, V]; at the end of a piece a wave's last step holds its O (16 x D floats)
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[4][2][2 * S::STEP];
-  __shared__ Plan plan;
-  __shared__ float2 s_ml[4][16];
+  // K and V of wave w's even (0) or odd steps; at the end of a piece the last one holds the wave's O
+  // (16 x D floats)
+  auto lds = [&](int w, int odd) { return (odd ? lds1 : lds0) + w * 2 * S::STEP; };
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int r16 = lane & 15, g4 = lane >> 4;
   const float c = a.scale_log2;
   const float lazy_raw = fminf(kLazy / c, 3.0e38f);
-  const Part part = make_plan<false>(a, plan);
-  if (blockIdx.x == 0) publish(a, plan);
-  if (part.lo == part.hi) return;
   const Loader<D> load(w, lane);
   uint32_t kaddr[KS];                     // this lane's K fragments: key r16, chunks 4 k + g4
 #pragma unroll
   for (int k = 0; k < KS; ++k) kaddr[k] = r16 * S::RB + swz_k<D>(4 * k + g4, r16) * 16;
   const uint32_t vaddr = S::STEP + 16 * vt_unit(r16, g4 >> 1) + 8 * (g4 & 1);
 
-  Piece cur = piece_at<false>(a, plan, plan.first, part.lo, part.hi, part.wg);
+  Piece cur = piece_at<false>(a, plan, plan.first, part.lo, part);
   if (cur.t0 == cur.t1) return;           // the part ends before the segment's first tile
   int buf = 0;
-  load.issue(a, cur, cur.t0, load.page(a, cur, cur.t0), lds[w][0], lds[w][0] + S::STEP);
+  load.issue(a, cur, cur.t0, load.page(a, cur, cur.t0), lds(w, 0), lds(w, 0) + S::STEP);
   int page_next = load.page(a, cur, min(cur.t0 + 1, cur.t1 - 1));
   while (true) {
     // ---- this lane's rows (16 i + r16), their queries and how many keys they see
@@ -395,7 +447,7 @@ void decode_lean(DecodeArgs a) {
     for (int i = 0; i < RT; ++i) {
       const int srow = cur.row0 + min(16 * i + r16, cur.rows - 1);
       const int tok = srow / a.G;
-      lim[i] = cur.entry < kMaxList ? cur.limit : cur.vis + tok;
+      lim[i] = cur.entry < kOwn ? cur.limit : cur.vis + tok;
       const uint16_t *qp = a.q + (int64_t)(cur.token0 + tok) * a.q_stride +
                            (cur.head * a.G + srow - tok * a.G) * D + 8 * g4;
 #pragma unroll
@@ -406,7 +458,7 @@ void decode_lean(DecodeArgs a) {
     nxt.t0 = nxt.t1 = 0;
     int page_piece = 0;
     if (cur.end < part.hi) {
-      nxt = piece_at<false>(a, plan, cur.entry, cur.end, part.hi, part.wg);
+      nxt = piece_at<false>(a, plan, cur.entry, cur.end, part);
       page_piece = load.page(a, nxt, nxt.t0);
     }
     const bool more = nxt.t0 < nxt.t1;
@@ -425,8 +477,8 @@ void decode_lean(DecodeArgs a) {
     }
 
     for (int t = cur.t0; t < cur.t1; ++t) {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's keys are here
-      uint8_t *next = lds[w][buf ^ 1];
+      wait_copies();                      // this wave's keys are here
+      uint8_t *next = lds(w, buf ^ 1);
       if (t + 1 < cur.t1) {
         load.issue(a, cur, t + 1, page_next, next, next + S::STEP);
         page_next = load.page(a, cur, min(t + 2, cur.t1 - 1));
@@ -434,7 +486,7 @@ void decode_lean(DecodeArgs a) {
         load.issue(a, nxt, nxt.t0, page_piece, next, next + S::STEP);
         page_next = load.page(a, nxt, min(nxt.t0 + 1, nxt.t1 - 1));
       }
-      uint8_t *step = lds[w][buf];
+      uint8_t *step = lds(w, buf);
       buf ^= 1;
       const int k0 = cur.key0 + kKeys * t + 16 * w;
       if (k0 >= cur.limit) continue;
@@ -521,7 +573,7 @@ void decode_lean(DecodeArgs a) {
     for (int i = 0; i < RT; ++i) {
       if (16 * i >= cur.rows) break;
       if (i) wg_barrier();
-      float *box = reinterpret_cast<float *>(lds[w][buf ^ 1]);
+      float *box = reinterpret_cast<float *>(lds(w, buf ^ 1));
 #pragma unroll
       for (int db = 0; db < DB; ++db)
         *reinterpret_cast<f32x4 *>(box + r16 * D + 4 * ((4 * db + g4) ^ r16)) = oacc[i][db];
@@ -544,7 +596,7 @@ void decode_lean(DecodeArgs a) {
         for (int j = 0; j < 4; ++j) {
           const float f = ml[j].y == 0.f ? 0.f : __builtin_amdgcn_exp2f((ml[j].x - m) * c);
           l_tot = fmaf(f, ml[j].y, l_tot);
-          const float *from = reinterpret_cast<const float *>(lds[j][buf ^ 1]) + row * D;
+          const float *from = reinterpret_cast<const float *>(lds(j, buf ^ 1)) + row * D;
 #pragma unroll
           for (int q = 0; q < D / 64; ++q) {
             const f32x4 x = *reinterpret_cast<const f32x4 *>(from + 4 * ((ch + 16 * q) ^ row));
@@ -566,7 +618,7 @@ void decode_lean(DecodeArgs a) {
             *reinterpret_cast<bf16x4 *>(op + 64 * q) = o;
           }
         } else {
-          float *to = (cur.entry < kMaxList ? a.part_few : a.part_own) +
+          float *to = (cur.entry < kOwn ? a.part_few : a.part_own) +
                       (int64_t)cur.slot * a.tile_rows * (D + 2);
           const int at = 16 * i + row;
           if (ch == 0)
@@ -590,22 +642,18 @@ void decode_lean(DecodeArgs a) {
 // keys.  A weight is one bf16 number, as there, its error 2^-8 in O and in the sum alike.  All rows
 // see all keys of a prefix.
 template <int D>
-__global__ __launch_bounds__(kThreads)
-__attribute__((amdgpu_waves_per_eu(DecGeo<D>::OCC, DecGeo<D>::OCC)))
-void decode_many(DecodeArgs a) {
+__device__ __forceinline__ void many_pieces(const DecodeArgs &a, const Plan &plan, uint8_t *lds0,
+                                            uint8_t *lds1, const Part &part) {
   using S = DecGeo<D>;
   constexpr int KS = D / 16, DB = D / 32, TILE = 4 * S::STEP;
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[2][2 * TILE];   // [2 tiles][K, V]
-  __shared__ Plan plan;
+  // K and V of even tiles in lds0, of odd ones in lds1
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int lr = lane & 31, lh = lane >> 5;
   const float c = a.scale_log2;
   const float lazy_raw = fminf(kLazy / c, 3.0e38f);
-  const Part part = make_plan<true>(a, plan);
-  if (part.lo == part.hi) return;
   const Loader<D> load(w, lane);
-  auto issue = [&](const Piece &r, int t, int pg, int into) {
-    uint8_t *k = lds[into] + w * S::STEP;
+  auto issue = [&](const Piece &r, int t, int pg, uint8_t *into) {
+    uint8_t *k = into + w * S::STEP;
     load.issue(a, r, t, pg, k, k + TILE);
   };
   const int kr = (lr & ~12) | ((lr >> 1) & 4) | ((lr << 1) & 8);
@@ -614,10 +662,10 @@ void decode_many(DecodeArgs a) {
   for (int k = 0; k < KS; ++k) kaddr[k] = kr * S::RB + swz_k<D>(2 * k + lh, kr) * 16;
   const uint32_t vaddr = TILE + 16 * vt_unit(lr, lh);
 
-  Piece cur = piece_at<true>(a, plan, plan.first, part.lo, part.hi, part.wg);
+  Piece cur = piece_at<true>(a, plan, plan.first, part.lo, part);
   if (cur.t0 == cur.t1) return;
-  int buf = 0;
-  issue(cur, cur.t0, load.page(a, cur, cur.t0), 0);
+  int odd = 0;
+  issue(cur, cur.t0, load.page(a, cur, cur.t0), lds0);
   int page_next = load.page(a, cur, min(cur.t0 + 1, cur.t1 - 1));
   while (true) {
     const bool active = 32 * w < cur.rows;
@@ -637,26 +685,24 @@ void decode_many(DecodeArgs a) {
     float m_ref = -INFINITY, mc = 0.f, m_trig = -INFINITY, l_run = 0.f;
     Piece nxt;
     nxt.t0 = nxt.t1 = 0;
-    if (cur.end < part.hi) nxt = piece_at<true>(a, plan, cur.entry, cur.end, part.hi, part.wg);
+    if (cur.end < part.hi) nxt = piece_at<true>(a, plan, cur.entry, cur.end, part);
     const bool more = nxt.t0 < nxt.t1;
 
-    for (int t = cur.t0; t < cur.t1; ++t) {
+    auto step = [&](uint8_t *tile, uint8_t *next, const int t) {
       const int k0 = cur.key0 + kKeys * t;
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's part of tile t is here
+      wait_copies();                                     // this wave's part of tile t is here
       const bool edge = k0 + kKeys > cur.limit;
       if (edge)
-        settle<D>(lds[buf] + TILE + w * S::STEP, k0 + 16 * w, cur.limit, cur.limit, lane);
+        settle<D>(tile + TILE + w * S::STEP, k0 + 16 * w, cur.limit, cur.limit, lane);
       wg_barrier();                                      // ... and every wave's
       if (t + 1 < cur.t1) {
-        issue(cur, t + 1, page_next, buf ^ 1);
+        issue(cur, t + 1, page_next, next);
         page_next = load.page(a, cur, min(t + 2, cur.t1 - 1));
       } else if (more) {
-        issue(nxt, nxt.t0, load.page(a, nxt, nxt.t0), buf ^ 1);
+        issue(nxt, nxt.t0, load.page(a, nxt, nxt.t0), next);
         page_next = load.page(a, nxt, min(nxt.t0 + 1, nxt.t1 - 1));
       }
-      const uint8_t *tile = lds[buf];
-      buf ^= 1;
-      if (!active) continue;
+      if (!active) return;
       f32x16 sacc[2];
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
@@ -708,6 +754,11 @@ void decode_many(DecodeArgs a) {
               *reinterpret_cast<const bf16x8 *>(tile + vaddr + db * 1024 + t4 * S::STEP);
           oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[t4], oacc[db], 0, 0, 0);
         }
+    };
+    for (int t = cur.t0; t < cur.t1; ++t) {
+      if (odd == 0) step(lds0, lds1, t);
+      else step(lds1, lds0, t);
+      odd ^= 1;
     }
 
     // ---- lane holds row `row`, d = 32 db + 8 (v / 4) + 4 lh + v % 4
@@ -728,6 +779,22 @@ void decode_many(DecodeArgs a) {
     if (!more) return;
     cur = nxt;
   }
+}
+
+// RT: row tiles of 16 of a piece with few rows.  MANY: the batch may have prefixes with many.
+template <int D, int RT, bool MANY>
+__global__ __launch_bounds__(kThreads)
+__attribute__((amdgpu_waves_per_eu(DecGeo<D>::OCC, DecGeo<D>::OCC)))
+void decode_fwd(DecodeArgs a) {
+  // two arrays, so that the compiler sees that reads of one do not wait for copies into the other
+  __shared__ __attribute__((aligned(1024))) uint8_t lds0[8 * DecGeo<D>::STEP];
+  __shared__ __attribute__((aligned(1024))) uint8_t lds1[8 * DecGeo<D>::STEP];
+  __shared__ Plan plan;
+  __shared__ float2 s_ml[4][16];
+  const Part part = make_plan(a, plan);
+  if (part.lo == part.hi) return;
+  if (MANY && part.many) many_pieces<D>(a, plan, lds0, lds1, part);
+  else lean_pieces<D, RT>(a, plan, lds0, lds1, s_ml, part);
 }
 
 // ---- Joins the pieces of a row: WPR waves, each with every 64 / (D / 4) * WPR-th group of pieces,
@@ -753,25 +820,27 @@ __global__ __launch_bounds__(kThreads) void decode_join(DecodeArgs a) {
   const float *from[2] = {a.part_own, a.part_own};
 #pragma unroll
   for (int kind = 0; kind < 2; ++kind) {
-    const bool line = kind == 0 && many;
+    const bool wide = kind == 0 && many;
     const int r = ((kind == 0 ? b - a.start[g] : 0) * a.nq + t) * a.G + kk;
-    const int per = line ? kDecodeRows : a.tile_rows;
-    const int tiles = line ? many_tiles(group_rows(a, g))
-                           : kind == 0 ? 1 : lean_tiles(a, a.G * a.nq);
+    const int per = wide ? kDecodeRows : a.tile_rows;
+    const int rows = kind == 0 ? group_rows(a, g) : a.G * a.nq;
+    const int width = wide ? j.width : 1;
+    const int tiles = width > 1 ? 1 : wide ? many_tiles(rows) : lean_tiles(a, rows);
     const int n = len == 0 ? 0 : tiles_of(kind == 0 ? prefix : len - prefix);
-    stride[kind] = per * (D + 2);
+    stride[kind] = width * per * (D + 2);
     const int row = r % per;
     ml_at[kind] = per * D + 2 * row - row * D;
     if (n == 0) continue;
-    const int seg = head * tiles + r / per;
+    const int seg = head * tiles + (width > 1 ? 0 : r / per);
     const int at = (kind == 0 ? j.shared[g] : j.own[b]) + seg * (n + kSegCost) + kSegCost;
-    const int total = line ? j.total_many : j.total_lean;
-    const Cut cut(total, min(a.wgs, total));
+    const Cut cut(wide ? j.places_many : j.places_lean, wide ? j.clusters : j.lean);
     const int first = cut.owner(at);
     count[kind] = cut.owner(at + n - 1) - first + 1;
-    const int base = kind == 0 ? prefix_base(a, g, many) : b * a.hkv * tiles;
-    from[kind] = (line ? a.part_many : kind == 0 ? a.part_few : a.part_own) +
-                 (int64_t)(base + seg + first) * stride[kind] + row * D;
+    const int base = width > 1 ? g * a.hkv
+                               : kind == 0 ? prefix_base(a, g, many) : b * a.hkv * tiles;
+    const int slot = (first + base + seg) * width + (width > 1 ? r / per : 0);
+    from[kind] = (wide ? a.part_many : kind == 0 ? a.part_few : a.part_own) +
+                 (int64_t)slot * per * (D + 2) + row * D;
   }
   const int n = count[0] + count[1];
   if (prefix == 0 && n == 1) return;      // finished by its workgroup
@@ -843,14 +912,12 @@ __global__ __launch_bounds__(kThreads) void decode_join(DecodeArgs a) {
 
 template <int D>
 hipError_t launch(const DecodeArgs &a, hipStream_t s) {
-  hipError_t e = hipSuccess;
-  if (a.any_many) {
-    decode_many<D><<<a.wgs, kThreads, 0, s>>>(a);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-  }
-  if (a.tile_rows == 16) decode_lean<D, 1><<<a.wgs, kThreads, 0, s>>>(a);
-  else decode_lean<D, 2><<<a.wgs, kThreads, 0, s>>>(a);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
+  if (a.any_many && a.tile_rows == 16) decode_fwd<D, 1, true><<<a.wgs, kThreads, 0, s>>>(a);
+  else if (a.any_many) decode_fwd<D, 2, true><<<a.wgs, kThreads, 0, s>>>(a);
+  else if (a.tile_rows == 16) decode_fwd<D, 1, false><<<a.wgs, kThreads, 0, s>>>(a);
+  else decode_fwd<D, 2, false><<<a.wgs, kThreads, 0, s>>>(a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
   const int rows = a.batch * a.nq * a.hq;
   if (rows <= 2048) decode_join<D, 4><<<rows, kThreads, 0, s>>>(a);
   else decode_join<D, 1><<<(rows + 3) / 4, kThreads, 0, s>>>(a);

@@ -183,7 +183,8 @@ struct ForkArgs {
 struct DecodeJoin {
   int32_t len[FP_MAX_CACHE_LIST], own[FP_MAX_CACHE_LIST];        // per sequence
   int32_t prefix[FP_MAX_CACHE_LIST], shared[FP_MAX_CACHE_LIST];  // per group
-  int32_t total_lean, total_many;
+  int32_t places_many, places_lean;
+  int32_t clusters, width, lean;
 };
 
 struct DecodeArgs {
