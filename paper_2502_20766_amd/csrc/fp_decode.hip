@@ -755,11 +755,15 @@ __device__ __forceinline__ void many_pieces(const DecodeArgs &a, const Plan &pla
           oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[t4], oacc[db], 0, 0, 0);
         }
     };
-    for (int t = cur.t0; t < cur.t1; ++t) {
-      if (odd == 0) step(lds0, lds1, t);
-      else step(lds1, lds0, t);
-      odd ^= 1;
+    // (in pairs: a branch on the buffer in every step would move O from register to register)
+    int t = cur.t0;
+    if (odd) step(lds1, lds0, t++);
+    for (; t + 2 <= cur.t1; t += 2) {
+      step(lds0, lds1, t);
+      step(lds1, lds0, t + 1);
     }
+    odd = t < cur.t1;
+    if (odd) step(lds0, lds1, t);
 
     // ---- lane holds row `row`, d = 32 db + 8 (v / 4) + 4 lh + v % 4
     const float l = wave_pair_sum(l_run);
