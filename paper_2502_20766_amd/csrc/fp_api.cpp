@@ -698,6 +698,7 @@ fp_status fp_decode_attn(const fp_cache *cache, const fp_decode *batch, int32_t 
   a.part_many = (float *)part;
   a.part_few = (float *)(part + dm.bytes_many);
   a.part_own = (float *)(part + dm.bytes_many + dm.bytes_few);
+  a.any_prefix = dm.many || dm.few;
   a.any_many = dm.many;
   a.tile_rows = dm.tile_rows;
   a.pages = c.pages;

@@ -91,6 +91,17 @@ struct Cut {
   }
 };
 
+// Inclusive prefix sum over the wave: within rows of 16 lanes, then the rows' sums handed on.
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // row_shr 1
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast 15 to rows 1, 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast 31 to rows 2, 3
+  return x;
+}
+
 // How the workgroups are divided: `clusters` times `width` of them take the line of many rows, a
 // cluster one part of it and each of its workgroups one row tile; `lean` the other line.
 struct Shares {
@@ -121,33 +132,34 @@ __device__ __forceinline__ Shares divide(int wgs, int many, int width, int lean)
 // Fills the plan and finds this workgroup's part and the entry it begins in.
 __device__ __forceinline__ Part make_plan(const DecodeArgs &a, Plan &p) {
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
-  if (t < a.groups) {
-    p.prefix[t] = 0x7FFFFFFF;
-    p.lead[t] = kMaxList - 1;
-    p.live[t] = 0;
-  }
-  if (t == 0) {
-    p.rows_lo = 0x7FFFFFFF;
-    p.rows_hi = 0;
-  }
   int len = 0, g = 0;
   if (t < a.batch) {
     g = a.group[t];
     if (a.slot[t] >= 0) len = min(max(a.len[a.slot[t]], 0), a.max_pages << a.page_shift);
     p.len[t] = len;
   }
-  __syncthreads();
-  if (len > 0) {
-    atomicMin(&p.prefix[g], max(len - a.nq, 0));
-    atomicMin(&p.lead[g], t);
-    atomicAdd(&p.live[g], 1);
-  }
-  __syncthreads();
   int cost[3] = {0, 0, 0};                // groups of many rows, of few, own keys
-  int tiles = 0;
-  if (t < a.groups) {
+  int width = 1, keys = 0;
+  if (a.any_prefix) {
+    if (t < a.groups) {
+      p.prefix[t] = 0x7FFFFFFF;
+      p.lead[t] = kMaxList - 1;
+      p.live[t] = 0;
+    }
+    if (t == 0) {
+      p.rows_lo = 0x7FFFFFFF;
+      p.rows_hi = 0;
+    }
+    __syncthreads();
+    if (len > 0) {
+      atomicMin(&p.prefix[g], max(len - a.nq, 0));
+      atomicMin(&p.lead[g], t);
+      atomicAdd(&p.live[g], 1);
+    }
+    __syncthreads();
+    int tiles = 0;
     // one sequence alone has nothing to share
-    const int keys = p.live[t] >= 2 ? min(p.prefix[t], a.prefix[t]) & ~15 : 0;
+    if (t < a.groups && p.live[t] >= 2) keys = min(p.prefix[t], a.prefix[t]) & ~15;
     if (keys > 0) {
       const bool many = is_many(a, t);
       const int rows = group_rows(a, t);
@@ -158,24 +170,22 @@ __device__ __forceinline__ Part make_plan(const DecodeArgs &a, Plan &p) {
         atomicMax(&p.rows_hi, tiles);
       }
     }
-    p.prefix[t] = keys;
+    if (t < a.groups) p.prefix[t] = keys;
+    __syncthreads();
+    // a cluster per part where all prefixes have the same number of row tiles
+    if (p.rows_lo == p.rows_hi && p.rows_hi <= a.wgs / 4) width = p.rows_hi;
+    else cost[0] *= tiles;
+    cost[1] *= tiles;
+  } else if (t < a.groups) {
+    p.prefix[t] = 0;
   }
-  __syncthreads();
-  // a cluster per part where all prefixes have the same number of row tiles
-  const int width = p.rows_lo == p.rows_hi && p.rows_hi <= a.wgs / 4 ? p.rows_hi : 1;
-  if (width == 1) cost[0] *= tiles;
-  cost[1] *= tiles;
   if (len > 0)
-    cost[2] = a.hkv * lean_tiles(a, a.G * a.nq) * (tiles_of(len - p.prefix[g]) + kSegCost);
+    cost[2] = a.hkv * lean_tiles(a, a.G * a.nq) *
+              (tiles_of(len - (a.any_prefix ? p.prefix[g] : 0)) + kSegCost);
   int start[3], total[3];
 #pragma unroll
   for (int i = 0; i < 3; ++i) {
-    start[i] = cost[i];
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const int y = __shfl_up(start[i], d);
-      if (lane >= d) start[i] += y;
-    }
+    start[i] = wave_scan(cost[i]);
     if (lane == 63) p.scan[i][w] = start[i];
   }
   __syncthreads();
@@ -227,7 +237,7 @@ __device__ __forceinline__ Part make_plan(const DecodeArgs &a, Plan &p) {
       j.own[t] = start[2];
     }
     if (t < a.groups) {
-      j.prefix[t] = p.prefix[t];
+      j.prefix[t] = keys;
       j.shared[t] = is_many(a, t) ? start[0] : start[1];
     }
     if (t == 0) {
@@ -880,7 +890,7 @@ __global__ __launch_bounds__(kThreads) void decode_join(DecodeArgs a) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int at = i + u * WPR * PPW + lane / LPP;
-        fi[u] = __shfl(f, at & 63);
+        fi[u] = __shfl(f, at & 63);       // (by all lanes)
         if (at >= k) fi[u] = 0.f;
         x[u] = *reinterpret_cast<const f32x4 *>(piece(i0 + min(at, k - 1)) + 4 * (lane % LPP));
       }

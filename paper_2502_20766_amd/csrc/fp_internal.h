@@ -196,7 +196,8 @@ struct DecodeArgs {
   // partial results of key ranges: prefixes with many and with few rows, sequences' own keys
   float *part_many, *part_few, *part_own;
   DecodeJoin *join;
-  int32_t any_many;            // some group's prefix has more than kDecodeFew rows
+  int32_t any_prefix;          // some group may share a prefix
+  int32_t any_many;            // ... with more than kDecodeFew rows
   int32_t tile_rows;           // query rows of a unit of the other work: 16 or 32
   int32_t pages, hkv, page_shift, max_pages;
   int32_t G, hq, nq, batch, groups;
