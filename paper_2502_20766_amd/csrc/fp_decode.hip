@@ -933,7 +933,7 @@ hipError_t launch(const DecodeArgs &a, hipStream_t s) {
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int rows = a.batch * a.nq * a.hq;
-  if (rows <= 2048) decode_join<D, 4><<<rows, kThreads, 0, s>>>(a);
+  if (rows <= 512) decode_join<D, 4><<<rows, kThreads, 0, s>>>(a);
   else decode_join<D, 1><<<(rows + 3) / 4, kThreads, 0, s>>>(a);
   return hipGetLastError();
 }
