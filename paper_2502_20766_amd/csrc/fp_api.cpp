@@ -600,6 +600,7 @@ fp_status fp_cache_write(const fp_cache *cache, int32_t layer, int32_t n, const 
   if (!k || !v || !aligned16(k) || !aligned16(v) || k_stride < row || v_stride < row ||
       k_stride % 8 || v_stride % 8)
     return FP_ERR_INVALID_ARG;
+  if (blocks * cache->num_kv_heads >= (1 << 24)) return FP_ERR_UNSUPPORTED;   // grid size
   a.list.num[n] = cu[n];
   a.blk[n] = (int32_t)blocks;
   a.k = (const uint16_t *)k;

@@ -13,7 +13,10 @@ namespace {
 constexpr int kPlanThreads = 1024;   // the single workgroup that hands out pages
 constexpr int kCopyUnits = 1024;     // 16-byte units of a page copied by one workgroup at a time
 constexpr int kCopyGrid = 2048;      // workgroups of a copy whose length the host cannot know
-constexpr int kBatch = 16;           // table rows that one thread takes a place of
+// Table rows that one thread takes a place of in fork and truncate: long lists (samples of one
+// prompt, which share most pages) share atomics, short ones are spread over more threads.  Eight
+// slots at 16 rows a thread took 6.6 and 5.5 us; 100 slots at 4 took more atomics than memory likes.
+constexpr int kFewRows = 4, kManyRows = 16, kShortList = 32;
 
 // 16 bytes as a vector: arrays of a struct of four words were kept in scratch memory, which cost a
 // short copy 13 us.
@@ -47,9 +50,10 @@ __device__ __forceinline__ int pages_of(int tokens, int shift) {
   return (int)(((unsigned)tokens + (1u << shift) - 1) >> shift);
 }
 
-// One holder less of each page listed (-1: none) for kBatch entries of a thread; neighbours that
+// One holder less of each page listed (-1: none) for the entries of a thread; neighbours that
 // name the same page share an atomic, and all of a thread's are in flight together.  Bits of pages
 // without holders are cleared; returns how many there are.
+template <int kBatch>
 __device__ __forceinline__ int drop_pages(const CacheView &c, const int (&page)[kBatch]) {
   int less[kBatch], before[kBatch], run = 0, gone = 0;
 #pragma unroll
@@ -246,11 +250,11 @@ template <int D>
 __global__ __launch_bounds__(256) void cache_write(CacheView c, WriteArgs a) {
   constexpr int CPR = D / 8;                 // 16-byte chunks per row
   __shared__ __attribute__((aligned(16))) uint16_t tile[64][D + 8];
-  __shared__ int s_i;
-  const int h = blockIdx.y, tid = threadIdx.x;
-  // the slot whose blocks hold blockIdx.x: one thread's
-  if (tid < a.list.n && a.blk[tid] <= (int)blockIdx.x && (int)blockIdx.x < a.blk[tid + 1])
-    s_i = tid;
+  __shared__ int s_i, s_page[4];
+  // neighbouring workgroups take the KV heads of the same rows
+  const int blk = blockIdx.x / c.hkv, h = blockIdx.x - blk * c.hkv, tid = threadIdx.x;
+  // the slot whose blocks hold this one: one thread's
+  if (tid < a.list.n && a.blk[tid] <= blk && blk < a.blk[tid + 1]) s_i = tid;
   const int error = c.state[1];
   __syncthreads();
   const int i = __builtin_amdgcn_readfirstlane(s_i);
@@ -259,39 +263,52 @@ __global__ __launch_bounds__(256) void cache_write(CacheView c, WriteArgs a) {
   const int slot = a.list.slot[i];
   const int len = min(c.len[slot], c.max_pages << c.page_shift);
   const int start = len - n;                 // position of the first row
-  const int p0 = (max(start, 0) & ~63) + 64 * ((int)blockIdx.x - a.blk[i]);
+  const int p0 = (max(start, 0) & ~63) + 64 * (blk - a.blk[i]);
   const int lo = max(start, p0), end = min(len, p0 + 64);
   if (lo >= end) return;
-  const int32_t *table = c.table + (int64_t)slot * c.max_pages;
-  // page of position t, or -1 when it is not this slot's alone
-  auto page_at = [&](int t) {
-    const int p = table[t >> c.page_shift];
-    if ((unsigned)p >= (unsigned)c.pages || c.ref[p] != 1) return -1;
-    return p;
-  };
   auto tile_of = [&](int p, int t) {         // element offset of position t's 16-token step
     return ((((int64_t)a.layer * c.pages + p) * c.hkv + h) << c.page_shift) * D +
            (int64_t)(t & (c.page - 1) & ~15) * D;
   };
-  for (int u = tid; u < 64 * CPR; u += 256) {
-    const int r = u / CPR, ch = u % CPR, t = p0 + r;
+  Unit kx[64 * CPR / 256], vx[64 * CPR / 256];
+#pragma unroll
+  for (int i = 0; i < 64 * CPR / 256; ++i) {
+    const int u = tid + 256 * i, r = u / CPR, ch = u % CPR, t = p0 + r;
     if (t < lo || t >= end) continue;
     const int64_t row = row0 + (t - start);
-    const Unit kx = *(const Unit *)(a.k + row * a.k_stride + h * D + ch * 8);
-    const Unit vx = *(const Unit *)(a.v + row * a.v_stride + h * D + ch * 8);
-    *(Unit *)&tile[r][ch * 8] = vx;
-    const int p = page_at(t);
-    if (p >= 0)
-      *(Unit *)(c.k + tile_of(p, t) + (t & 15) * D + ch * 8) = kx;
-    else if (ch == 0)
-      atomicOr(c.state + 1, FP_CACHE_SHARED);
+    kx[i] = *(const Unit *)(a.k + row * a.k_stride + h * D + ch * 8);
+    vx[i] = *(const Unit *)(a.v + row * a.v_stride + h * D + ch * 8);
+  }
+  // pages of the four 16-token steps, or -1 for one that is not this slot's alone
+  if (tid < 4) {
+    const int t = p0 + 16 * tid;
+    int p = -1;
+    if (t < end && t + 16 > lo) {
+      p = c.table[(int64_t)slot * c.max_pages + (t >> c.page_shift)];
+      if ((unsigned)p >= (unsigned)c.pages || c.ref[p] != 1) {
+        p = -1;
+        atomicOr(c.state + 1, FP_CACHE_SHARED);
+      }
+    }
+    s_page[tid] = p;
+  }
+#pragma unroll
+  for (int i = 0; i < 64 * CPR / 256; ++i) {
+    const int u = tid + 256 * i, r = u / CPR, ch = u % CPR, t = p0 + r;
+    if (t >= lo && t < end) *(Unit *)&tile[r][ch * 8] = vx[i];
   }
   __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 64 * CPR / 256; ++i) {
+    const int u = tid + 256 * i, r = u / CPR, ch = u % CPR, t = p0 + r, p = s_page[r >> 4];
+    if (t < lo || t >= end || p < 0) continue;
+    *(Unit *)(c.k + tile_of(p, t) + (t & 15) * D + ch * 8) = kx[i];
+  }
   for (int u = tid; u < 8 * D; u += 256) {   // 8 half steps x D
     const int half = u & 1, d = (u >> 1) % D, step = (u >> 1) / D;
     const int r = 16 * step + 8 * half, t = p0 + r;
     if (t + 8 <= lo || t >= end) continue;
-    const int p = page_at(t);
+    const int p = s_page[step];
     if (p < 0) continue;
     uint16_t *to = c.v + tile_of(p, t) + d * 16 + 8 * half;
     if (t >= lo && t + 8 <= end) {
@@ -311,6 +328,7 @@ __global__ __launch_bounds__(256) void cache_write(CacheView c, WriteArgs a) {
 // ---- fork: a thread takes one place of the tables of kBatch sources to their copies.  A source
 // keeps its pages throughout, so a page is never free in between, whatever the order of the counts.
 // Neighbours that share a page share its atomics: samples of one prompt hold mostly the same.
+template <int kBatch>
 __global__ __launch_bounds__(256) void cache_fork(CacheView c, ForkArgs a) {
   const int first = blockIdx.y * kBatch, n = min(a.n - first, kBatch);
   const int j = blockIdx.x * 256 + threadIdx.x;
@@ -343,6 +361,7 @@ __global__ __launch_bounds__(256) void cache_fork(CacheView c, ForkArgs a) {
 }
 
 // ---- truncate: a thread gives back one place of the tables of kBatch slots
+template <int kBatch>
 __global__ __launch_bounds__(256) void cache_truncate(CacheView c, CacheList l) {
   const int first = blockIdx.y * kBatch, n = min(l.n - first, kBatch);
   const int j = blockIdx.x * 256 + threadIdx.x;
@@ -459,20 +478,30 @@ hipError_t launch_cache_reserve(const CacheView &c, const CacheList &l, const Pa
 }
 
 hipError_t launch_cache_write(const CacheView &c, const WriteArgs &a, hipStream_t s) {
-  const dim3 grid(a.blk[a.list.n], c.hkv);
+  const int grid = a.blk[a.list.n] * c.hkv;
   if (c.d == 64) cache_write<64><<<grid, 256, 0, s>>>(c, a);
   else cache_write<128><<<grid, 256, 0, s>>>(c, a);
   return hipGetLastError();
 }
 
+// Workgroups of fork and truncate: 256 places of the tables, `rows` slots of the list.
+static dim3 table_grid(const CacheView &c, int n, int rows) {
+  return dim3((c.max_pages + 255) / 256, (n + rows - 1) / rows);
+}
+
 hipError_t launch_cache_fork(const CacheView &c, const ForkArgs &a, hipStream_t s) {
-  cache_fork<<<dim3((c.max_pages + 255) / 256, (a.n + kBatch - 1) / kBatch), 256, 0, s>>>(c, a);
+  if (a.n <= kShortList)
+    cache_fork<kFewRows><<<table_grid(c, a.n, kFewRows), 256, 0, s>>>(c, a);
+  else
+    cache_fork<kManyRows><<<table_grid(c, a.n, kManyRows), 256, 0, s>>>(c, a);
   return hipGetLastError();
 }
 
 hipError_t launch_cache_truncate(const CacheView &c, const CacheList &l, hipStream_t s) {
-  cache_truncate<<<dim3((c.max_pages + 255) / 256, (l.n + kBatch - 1) / kBatch), 256, 0, s>>>(c,
-                                                                                           l);
+  if (l.n <= kShortList)
+    cache_truncate<kFewRows><<<table_grid(c, l.n, kFewRows), 256, 0, s>>>(c, l);
+  else
+    cache_truncate<kManyRows><<<table_grid(c, l.n, kManyRows), 256, 0, s>>>(c, l);
   return hipGetLastError();
 }
 
