@@ -40,24 +40,21 @@ class CacheError(RuntimeError):
 # These calls are made several times a layer and step, so the host's share of one counts: lists go
 # to the library as the bytes of int32 arrays, tensors as plain addresses.
 
-_torch = None
+_bf16 = _device = _raw_stream = None
 
 
-def _t():
-    """torch, which importing this package does not load."""
-    global _torch
-    if _torch is None:
-        import torch
-        _torch = torch
-    return _torch
+def _load_torch():
+    """torch's parts that the calls use; importing this package does not load it."""
+    global _bf16, _device, _raw_stream
+    import torch
+    torch.cuda.init()
+    _bf16 = torch.bfloat16
+    _device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 
 
 def _stream(stream):
     """The raw handle of `stream` or of the current stream."""
-    if stream is not None:
-        return stream.cuda_stream
-    c = _t()._C
-    return c._cuda_getCurrentRawStream(c._cuda_getDevice())
+    return _raw_stream(_device()) if stream is None else stream.cuda_stream
 
 
 def _ints(x, name, n=None):
@@ -112,7 +109,10 @@ class Cache:
             _check_tensor(x, name, len(shape), dtype)
             if tuple(x.shape) != tuple(shape):
                 raise ValueError(f"{name} has shape {tuple(x.shape)}; the cache needs {shape}")
+        if _bf16 is None:
+            _load_torch()
         self.k, self.v, self.meta = k, v, meta
+        self.heads, self.head_dim = int(num_kv_heads), int(head_dim)
         self.c.k, self.c.v, self.c.meta = k.data_ptr(), v.data_ptr(), meta.data_ptr()
         words = 2 * -(-int(num_pages) // 64)
         sizes = [8, words, int(num_slots), int(num_pages), int(num_slots) * int(max_pages)]
@@ -164,13 +164,13 @@ def cache_reserve(cache: Cache, slots, counts, workspace=None, stream=None):
 
 
 def _check_rows(x, name, heads, d):
-    """The stride between rows of a [T, heads, d] bf16 tensor whose rows are contiguous."""
+    """Rows, and the stride between them, of a [T, heads, d] bf16 tensor with contiguous rows."""
     shape, stride = x.shape, x.stride()
-    if not (x.is_cuda and x.dtype == _t().bfloat16 and len(shape) == 3 and shape[1] == heads
-            and shape[2] == d and (shape[0] == 0 or (stride[2] == 1 and stride[1] == d))):
-        raise ValueError(f"{name} must be a bf16 CUDA tensor [T, {heads}, {d}] with contiguous "
-                         "rows")
-    return stride[0] if shape[0] > 1 else heads * d
+    if len(shape) == 3 and x.is_cuda and x.dtype is _bf16:
+        n, h, e = shape
+        if h == heads and e == d and (n == 0 or (stride[2] == 1 and stride[1] == d)):
+            return n, stride[0] if n > 1 else heads * d
+    raise ValueError(f"{name} must be a bf16 CUDA tensor [T, {heads}, {d}] with contiguous rows")
 
 
 def cache_write(cache: Cache, layer, k, v, slots, cu_seqlens, stream=None):
@@ -178,10 +178,10 @@ def cache_write(cache: Cache, layer, k, v, slots, cu_seqlens, stream=None):
     slots[i].  k, v: [T, Hkv, d] bf16, rows contiguous (slices of a fused projection do)."""
     slots = _ints(slots, "slots")
     cu = _ints(cu_seqlens, "cu_seqlens", slots.size + 1)
-    heads, d = cache.c.num_kv_heads, cache.c.head_dim
-    ks, vs = _check_rows(k, "k", heads, d), _check_rows(v, "v", heads, d)
-    if not len(k) == len(v) == cu[-1]:
-        raise ValueError(f"k and v have {len(k)} and {len(v)} rows; cu_seqlens ends at {cu[-1]}")
+    nk, ks = _check_rows(k, "k", cache.heads, cache.head_dim)
+    nv, vs = _check_rows(v, "v", cache.heads, cache.head_dim)
+    if not nk == nv == cu[-1]:
+        raise ValueError(f"k and v have {nk} and {nv} rows; cu_seqlens ends at {cu[-1]}")
     _call(lib().fp_cache_write(cache.ref, layer, slots.size, slots.tobytes(), cu.tobytes(),
                                k.data_ptr(), ks, v.data_ptr(), vs, _stream(stream)),
           "fp_cache_write")
@@ -239,6 +239,7 @@ class DecodeBatch:
             self.c.group_start = self.group_start.ctypes.data
             self.c.prefix_lens = self.prefix_lens.ctypes.data
         self.ref = ctypes.byref(self.c)
+        self.rows, self.heads = self.c.batch * self.c.queries, self.c.num_q_heads
 
 
 def decode_workspace_size(cache: Cache, batch: DecodeBatch) -> int:
@@ -253,12 +254,12 @@ def decode_attn(q, cache: Cache, layer, batch: DecodeBatch, out=None, workspace=
                 stream=None):
     """Attention of the batch's query tokens over their sequences.  q: [batch * queries, Hq, d]
     bf16, rows contiguous, sequence by sequence; returns o of the same shape."""
-    T, hq, d = batch.c.batch * batch.c.queries, batch.c.num_q_heads, cache.c.head_dim
-    stride = _check_rows(q, "q", hq, d)
-    if len(q) != T:
-        raise ValueError(f"q has {len(q)} rows; the batch has {T} query tokens")
+    T, hq, d = batch.rows, batch.heads, cache.head_dim
+    n, stride = _check_rows(q, "q", hq, d)
+    if n != T:
+        raise ValueError(f"q has {n} rows; the batch has {T} query tokens")
     if out is None:
-        out = _workspace(2 * T * hq * d, q.device, stream).view(_t().bfloat16).view(T, hq, d)
+        out = _workspace(2 * T * hq * d, q.device, stream).view(_bf16).view(T, hq, d)
     else:
         _check_tensor(out, "out", 3)
         if out.shape != (T, hq, d):
