@@ -201,8 +201,8 @@ fp_status fp_sparse_attn_noalloc(const fp_shape *shape, const void *q, const voi
  *
  * What only the device knows cannot be refused by the host.  A reserve that finds too few pages
  * or too short a table row changes nothing and sets an error bit in state[1]; while a bit is set
- * every call that changes the cache does nothing.  The caller reads the word when it synchronises
- * anyway and clears it by storing 0. */
+ * reserve, fork, truncate and compact do nothing, and after a failed reserve write does nothing
+ * either.  The caller reads the word when it synchronises anyway and clears it by storing 0. */
 #define FP_CACHE_FULL 1       /* fp_cache_reserve: fewer free pages than the call needs        */
 #define FP_CACHE_TOO_LONG 2   /* fp_cache_reserve: a slot would pass max_pages pages           */
 #define FP_CACHE_SHARED 4     /* fp_cache_write: tokens on a page that is not the slot's alone */
@@ -247,7 +247,8 @@ fp_status fp_cache_reserve(const fp_cache *cache, int32_t n, const int32_t *slot
 /* Keys and values of one layer for the last cu[i+1] - cu[i] tokens of slots[i] (HOST arrays,
  * cu [n+1], cu[0] = 0, non-decreasing): rows cu[i] .. cu[i+1]-1 of k and v, each [Hkv][d] bf16
  * contiguous, k_stride and v_stride elements from one token to the next (>= Hkv * d, a multiple
- * of 8; pointers 16-byte aligned).  Rows beyond a slot's length are left out. */
+ * of 8; pointers 16-byte aligned).  Rows beyond a slot's length are left out.  Takes up to 2^24
+ * pieces of 64 tokens and one KV head. */
 fp_status fp_cache_write(const fp_cache *cache, int32_t layer, int32_t n, const int32_t *slots,
                          const int32_t *cu, const void *k, int64_t k_stride, const void *v,
                          int64_t v_stride, void *stream);

@@ -130,6 +130,13 @@ def test_write_of_nothing_touches_no_device(lib):
                               None, 128, None, 128, None) == fpx.FP_OK
 
 
+def test_write_of_too_much(lib):
+    """More (64 tokens, KV head) pieces than one launch takes."""
+    cu = _i32(0, 1 << 30)
+    assert lib.fp_cache_write(ctypes.byref(_cache()), 0, 1, _p(_i32(0)), _p(cu), 4096, 128, 4096,
+                              128, None) == UNSUPPORTED
+
+
 def _batch(slots=(0, 1, -1, 1), hq=4, queries=1, start=None, prefix=None, scale=0.0):
     return fpx.DecodeBatch(slots, hq, queries, start, prefix, scale)
 

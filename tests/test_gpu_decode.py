@@ -163,6 +163,21 @@ def test_rows_of_a_group(nq, count):
     Scene([(333, own)], 4, 2, 64, 64, seed=count + nq).run(nq)
 
 
+@pytest.mark.parametrize("sizes", [(40, 40), (40, 100), (33, 33, 33), (90, 2, 90), (65, 7, 1, 33)])
+@pytest.mark.parametrize("prefix", [70, 900])
+def test_row_tiles_of_several_groups(sizes, prefix):
+    """Groups with as many row tiles as each other (taken side by side) and with others, beside
+    groups of few rows and sequences of their own."""
+    groups = [(prefix + 50 * i, [1 + (11 * j) % 40 for j in range(n)])
+              for i, n in enumerate(sizes)]
+    Scene(groups, 4, 1, 128, 32, seed=sum(sizes)).run()
+    Scene(groups, 8, 2, 64, 64, seed=sum(sizes)).run()
+
+
+def test_a_long_prefix_of_many_rows():
+    Scene([(40000, [3, 200] * 40)], 4, 1, 128, 128, seed=21).run()
+
+
 @pytest.mark.parametrize("d", [64, 128])
 def test_several_groups(d):
     groups = [(200, [3, 70]), (0, [5, 100, 1]), (77, [30]), (1000, [20, None, 64, 21]),
