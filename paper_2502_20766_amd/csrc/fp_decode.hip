@@ -230,15 +230,14 @@ __device__ __forceinline__ Part make_plan(const DecodeArgs &a, Plan &p) {
     if (start[1] <= r.lo && r.lo < start[1] + cost[1]) p.first = t;
     if (start[2] <= r.lo && r.lo < start[2] + cost[2]) p.first = kOwn + t;
   }
+  __syncthreads();
   if (blockIdx.x == 0) {                  // what the joining launch needs of this
     DecodeJoin &j = *a.join;
     if (t < a.batch) {
-      j.len[t] = len;
-      j.own[t] = start[2];
-    }
-    if (t < a.groups) {
-      j.prefix[t] = keys;
-      j.shared[t] = is_many(a, t) ? start[0] : start[1];
+      const int prefix = len > 0 ? p.prefix[g] : 0;
+      const bool many = is_many(a, g);
+      j.seq[t] = make_int4(len, prefix, start[2], many ? p.many[g] : p.lean[g]);
+      j.group[t] = make_int4(g, a.start[g], group_rows(a, g), many);
     }
     if (t == 0) {
       j.places_many = total[0];
@@ -248,7 +247,6 @@ __device__ __forceinline__ Part make_plan(const DecodeArgs &a, Plan &p) {
       j.lean = sh.lean;
     }
   }
-  __syncthreads();
   r.many = __builtin_amdgcn_readfirstlane(r.many);
   r.lo = __builtin_amdgcn_readfirstlane(r.lo);
   r.hi = __builtin_amdgcn_readfirstlane(r.hi);
@@ -823,38 +821,43 @@ __global__ __launch_bounds__(kThreads) void decode_join(DecodeArgs a) {
   if (WPR == 1 && id >= (int64_t)a.batch * a.nq * a.hq) return;
   const int token = (int)(id / a.hq), qh = (int)(id - (int64_t)token * a.hq);
   const int b = token / a.nq, t = token - b * a.nq, head = qh / a.G, kk = qh - head * a.G;
-  const int g = a.group[b];
   const DecodeJoin &j = *a.join;
-  const int prefix = j.prefix[g], len = j.len[b];
+  const int4 seq = j.seq[b];              // tokens, prefix, places of own keys and of the prefix
+  const int len = seq.x, prefix = seq.y;
   uint16_t *op = a.o + id * D;
   const float c = a.scale_log2;
-  const bool many = is_many(a, g);
-  // pieces of the row's two segments: the prefix (0) and its own keys (1)
-  int count[2] = {0, 0}, stride[2], ml_at[2];
+  // pieces of the row's two segments: its own keys (1) and the prefix (0)
+  int count[2] = {0, 0}, stride[2] = {0, 0}, ml_at[2] = {0, 0};
   const float *from[2] = {a.part_own, a.part_own};
-#pragma unroll
-  for (int kind = 0; kind < 2; ++kind) {
-    const bool wide = kind == 0 && many;
-    const int r = ((kind == 0 ? b - a.start[g] : 0) * a.nq + t) * a.G + kk;
-    const int per = wide ? kDecodeRows : a.tile_rows;
-    const int rows = kind == 0 ? group_rows(a, g) : a.G * a.nq;
-    const int width = wide ? j.width : 1;
-    const int tiles = width > 1 ? 1 : wide ? many_tiles(rows) : lean_tiles(a, rows);
-    const int n = len == 0 ? 0 : tiles_of(kind == 0 ? prefix : len - prefix);
-    stride[kind] = width * per * (D + 2);
-    const int row = r % per;
-    ml_at[kind] = per * D + 2 * row - row * D;
-    if (n == 0) continue;
-    const int seg = head * tiles + (width > 1 ? 0 : r / per);
-    const int at = (kind == 0 ? j.shared[g] : j.own[b]) + seg * (n + kSegCost) + kSegCost;
-    const Cut cut(wide ? j.places_many : j.places_lean, wide ? j.clusters : j.lean);
+  if (len > 0) {
+    const int per = a.tile_rows, r = t * a.G + kk, row = r % per;
+    const int tiles = lean_tiles(a, a.G * a.nq), n = tiles_of(len - prefix);
+    const int seg = head * tiles + r / per;
+    const int at = seq.z + seg * (n + kSegCost) + kSegCost;
+    const Cut cut(j.places_lean, j.lean);
     const int first = cut.owner(at);
-    count[kind] = cut.owner(at + n - 1) - first + 1;
-    const int base = width > 1 ? g * a.hkv
-                               : kind == 0 ? prefix_base(a, g, many) : b * a.hkv * tiles;
-    const int slot = (first + base + seg) * width + (width > 1 ? r / per : 0);
-    from[kind] = (wide ? a.part_many : kind == 0 ? a.part_few : a.part_own) +
-                 (int64_t)slot * per * (D + 2) + row * D;
+    count[1] = cut.owner(at + n - 1) - first + 1;
+    stride[1] = per * (D + 2);
+    ml_at[1] = per * D + 2 * row - row * D;
+    from[1] = a.part_own + (int64_t)(first + b * a.hkv * tiles + seg) * stride[1] + row * D;
+  }
+  if (prefix > 0) {
+    const int4 grp = j.group[b];          // group, its first sequence, its rows, whether many
+    const int g = grp.x, many = grp.w;
+    const int per = many ? kDecodeRows : a.tile_rows, width = many ? j.width : 1;
+    const int r = ((b - grp.y) * a.nq + t) * a.G + kk, tile = r / per, row = r - tile * per;
+    const int tiles = width > 1 ? 1 : many ? many_tiles(grp.z) : lean_tiles(a, grp.z);
+    const int n = tiles_of(prefix);
+    const int seg = head * tiles + (width > 1 ? 0 : tile);
+    const int at = seq.w + seg * (n + kSegCost) + kSegCost;
+    const Cut cut(many ? j.places_many : j.places_lean, many ? j.clusters : j.lean);
+    const int first = cut.owner(at);
+    count[0] = cut.owner(at + n - 1) - first + 1;
+    stride[0] = width * per * (D + 2);
+    ml_at[0] = per * D + 2 * row - row * D;
+    const int base = width > 1 ? g * a.hkv : prefix_base(a, g, many);
+    const int slot = (first + base + seg) * width + (width > 1 ? tile : 0);
+    from[0] = (many ? a.part_many : a.part_few) + (int64_t)slot * per * (D + 2) + row * D;
   }
   const int n = count[0] + count[1];
   if (prefix == 0 && n == 1) return;      // finished by its workgroup

@@ -181,8 +181,9 @@ struct ForkArgs {
 
 // What the joining launch of decode_attn knows of the call's plan (workspace).
 struct DecodeJoin {
-  int32_t len[FP_MAX_CACHE_LIST], own[FP_MAX_CACHE_LIST];        // per sequence
-  int32_t prefix[FP_MAX_CACHE_LIST], shared[FP_MAX_CACHE_LIST];  // per group
+  int4 seq[FP_MAX_CACHE_LIST];     // per sequence: tokens, keys of the prefix, places of its own
+                                   // keys and of the prefix
+  int4 group[FP_MAX_CACHE_LIST];   // per sequence: group, its first sequence, its rows, many or not
   int32_t places_many, places_lean;
   int32_t clusters, width, lean;
 };
