@@ -1,23 +1,24 @@
-// Attention of the next tokens over a paged cache: o = softmax(c q K^T) V for the last `queries`
-// tokens of every sequence of a batch, with the keys and values that a group of sequences shares
-// at its start read once for the whole group.
+// Attention of the next tokens over a paged cache: o = softmax(c q K^T) V for the last
+// `queries` tokens of every sequence of a batch, with the keys and values that a group of
+// sequences shares at its start read once for the whole group.
 //
 // Split softmax: over a range R of keys, with reference m and weights w_j = exp2(s_j - m),
 //   O_R = sum w_j v_j,  l_R = sum w_j;   o = (sum_R 2^(m_R - M) O_R) / (sum_R 2^(m_R - M) l_R).
-// The ranges are cut as follows.  A segment is the work of one KV head and one tile of query rows
-// over one run of keys: the prefix of a group (rows: all query heads of the KV head, all queries,
-// all sequences of the group) or the rest of one sequence (rows: its own).  Segments, one after the
-// other in tiles of 64 keys, form a line that is cut into equal parts, one for each workgroup, so
-// every workgroup has the same work whatever the lengths.  A piece (the part of a segment in one
-// workgroup) leaves O_R, m_R and l_R in float32; a last launch joins the pieces of each row in the
-// order of the line.  A segment in one piece whose rows have no prefix is finished on the spot.
-// Where the cuts fall follows from the lengths alone, so results do not depend on timing.
+// The ranges are cut as follows.  A segment is the work of one KV head and one tile of query
+// rows over one run of keys: the prefix of a group (rows: all query heads of the KV head, all
+// queries, all sequences of the group) or the rest of one sequence (rows: its own).  Segments,
+// one after the other in tiles of 64 keys, form a line that is cut into equal parts, one for
+// each workgroup, so every workgroup has the same work whatever the lengths.  A piece (the part
+// of a segment in one workgroup) leaves O_R, m_R and l_R in float32; a last launch joins the
+// pieces of each row in the order of the line.  A segment in one piece whose rows have no
+// prefix is finished on the spot. Where the cuts fall follows from the lengths alone, so
+// results do not depend on timing.
 //
-// Segments with few rows are bound by the bytes of their keys, prefixes with many by their products,
-// so there are two ways to take a piece (lean_pieces, many_pieces) and two lines.  One launch takes
-// both: the resident workgroups are divided between the lines by their work, so that neither waits
-// for the other.  Workgroups that take the row tiles of one prefix go through the same keys side by
-// side (a cluster), so that those come from memory once.
+// Segments with few rows are bound by the bytes of their keys, prefixes with many by their
+// products, so there are two ways to take a piece (lean_pieces, many_pieces) and two lines.
+// One launch takes both: the resident workgroups are divided between the lines by their work,
+// so that neither waits for the other.  Workgroups that take the row tiles of one prefix go
+// through the same keys side by side (a cluster), so that those come from memory once.
 #include <type_traits>
 
 #include "fp_attn_dev.h"
@@ -32,8 +33,10 @@ constexpr int kKeys = 64;                 // keys per tile
 constexpr int kThreads = 256;
 constexpr int kMaxList = FP_MAX_CACHE_LIST;
 constexpr float kLazy = 8.f;              // rise (log2 units) that moves a row's reference
-// Places of the line, beside its tiles, that a segment takes: starting and ending a piece costs a
-// workgroup about as much as this many tiles.
+// Places of the line, beside its tiles, that a segment takes: starting and ending a piece costs
+// a workgroup about as much as this many tiles.  At 1, 2, 3, 4, 6: 64 sequences of 3 to 32000
+// tokens 100, 95, 93, 94, 94 us; 16 samples of 32k 30.6, 31.2, 32.3, 32.6, 33.2; 256 samples of
+// 128k (best of 20) 749, 579, 583, 589, 610.
 constexpr int kSegCost = 2;
 
 static_assert(kThreads == kMaxList, "the plan has one thread per sequence");
@@ -80,7 +83,8 @@ __device__ __forceinline__ int prefix_base(const DecodeArgs &a, int g, bool many
   return (a.start[g] * a.nq * a.G / (many ? kDecodeRows : a.tile_rows) + g) * a.hkv;
 }
 
-// A line of `total` places in `wgs` equal parts, the first total % wgs of them one place longer.
+// A line of `total` places in `wgs` equal parts, the first total % wgs of them one place
+// longer.
 struct Cut {
   int per, rem;
   __device__ __forceinline__ Cut(int total, int wgs) : per(total / wgs), rem(total % wgs) {}
@@ -102,8 +106,8 @@ __device__ __forceinline__ int wave_scan(int x) {
   return x;
 }
 
-// How the workgroups are divided: `clusters` times `width` of them take the line of many rows, a
-// cluster one part of it and each of its workgroups one row tile; `lean` the other line.
+// How the workgroups are divided: `clusters` times `width` of them take the line of many rows,
+// a cluster one part of it and each of its workgroups one row tile; `lean` the other line.
 struct Shares {
   int clusters, width, lean;
 };
@@ -209,8 +213,8 @@ __device__ __forceinline__ Part make_plan(const DecodeArgs &a, Plan &p) {
     p.lean[kEnd] = places;
   }
   const Shares sh = divide(a.wgs, total[0], width, places);
-  // Workgroups of one XCD (every eighth) take neighbouring parts, which share keys, unless there is
-  // not work for all.
+  // Workgroups of one XCD (every eighth) take neighbouring parts, which share keys, unless
+  // there is not work for all.
   const int crowd = sh.clusters * sh.width, used = crowd + sh.lean;
   int wg = blockIdx.x;
   if (8 * used > 7 * a.wgs) wg = (wg & 7) * (a.wgs / 8) + (wg >> 3);
@@ -330,8 +334,9 @@ struct DecGeo {
   static constexpr int RPI = 1024 / RB;            // key rows per copy
 };
 
-// A wave's 16 keys of a tile, which always lie in one page, brought into LDS by DMA: K row-major
-// with 16-byte chunks swizzled as in the prefill, V^T in the fragment order of vt_unit.
+// A wave's 16 keys of a tile, which always lie in one page, brought into LDS by DMA: K
+// row-major with 16-byte chunks swizzled as in the prefill, V^T in the fragment order of
+// vt_unit.
 template <int D>
 struct Loader {
   using S = DecGeo<D>;
@@ -368,8 +373,8 @@ struct Loader {
 
 // 16 keys of V^T in LDS, of which some row does not see all.  Values past the segment may hold
 // anything, NaN among it, which a weight of zero would not cancel: they become zero.  So do
-// infinities and NaN of tokens that only later queries see; returns whether there were any, and the
-// rows that see them then take them separately.
+// infinities and NaN of tokens that only later queries see; returns whether there were any, and
+// the rows that see them then take them separately.
 template <int D>
 __device__ __forceinline__ bool settle(uint8_t *v, int key0, int limit, int vis, int lane) {
   bool odd = false;
@@ -389,9 +394,10 @@ __device__ __forceinline__ bool settle(uint8_t *v, int key0, int limit, int vis,
   return __ballot(odd) != 0;
 }
 
-// Waits for this wave's copies into LDS (and its other loads and stores).  The builtin, unlike the
-// same instruction in an asm statement, also tells the compiler, which would else wait for them
-// where their LDS is first read, after the next copies have been issued, and so for those too.
+// Waits for this wave's copies into LDS (and its other loads and stores).  The builtin, unlike
+// the same instruction in an asm statement, also tells the compiler, which would else wait for
+// them where their LDS is first read, after the next copies have been issued, and so for those
+// too.
 __device__ __forceinline__ void wait_copies() {
   asm volatile("" ::: "memory");
   __builtin_amdgcn_s_waitcnt(0x0F70);     // vmcnt(0)
@@ -423,14 +429,19 @@ __device__ __forceinline__ float quad_sum(float x) {
 //   O^T += V^T P^T, D / 16 products.  The 32 places of a product's inner dimension are the 16 keys
 //   twice: a weight is the sum of two bf16 numbers (error 2^-17), the second one in places where
 //   V^T is repeated.  That costs no product, and the keys' bytes bound the kernel anyway.
+// Measured: 64 sequences of 3 to 32000 tokens, 32 query and 8 KV heads of 128, 507 MB of keys
+// and values in 93 us, 5.4 TB/s (a copy of 1 GiB moves 5.1); pages of 16 and of 64 tokens the
+// same.  With 32-row products instead (one wave 32 keys, weights in one piece, joined in pairs)
+// the same bytes took 189 us.  256 sequences of 100 tokens, two tiles a segment: 27 us for 105
+// MB.
 template <int D, int RT>
 __device__ __forceinline__ void lean_pieces(const DecodeArgs &a, const Plan &plan, uint8_t *lds0,
                                             uint8_t *lds1, float2 (*s_ml)[16],
                                             const Part &part) {
   using S = DecGeo<D>;
   constexpr int KS = D / 32, DB = D / 16;
-  // K and V of wave w's even (0) or odd steps; at the end of a piece the last one holds the wave's O
-  // (16 x D floats)
+  // K and V of wave w's even (0) or odd steps; at the end of a piece the last one holds the
+  // wave's O (16 x D floats)
   auto lds = [&](int w, int odd) { return (odd ? lds1 : lds0) + w * 2 * S::STEP; };
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int r16 = lane & 15, g4 = lane >> 4;
@@ -644,11 +655,15 @@ __device__ __forceinline__ void lean_pieces(const DecodeArgs &a, const Plan &pla
 }
 
 // ---- many rows: tiles of 128, 32 per wave.  The 64 keys of a tile go through LDS (double
-// buffered, each wave bringing 16) and are read by all four waves; the products are those of the
-// prefill, on v_mfma_f32_32x32x16_bf16: S^T = K Q^T with K rows permuted so that a lane's scores
-// are the consecutive keys that P^T of O^T += V^T P^T needs, one update of the reference for 64
-// keys.  A weight is one bf16 number, as there, its error 2^-8 in O and in the sum alike.  All rows
-// see all keys of a prefix.
+// buffered, each wave bringing 16) and are read by all four waves; the products are those of
+// the prefill, on v_mfma_f32_32x32x16_bf16: S^T = K Q^T with K rows permuted so that a lane's
+// scores are the consecutive keys that P^T of O^T += V^T P^T needs, one update of the reference
+// for 64 keys.  A weight is one bf16 number, as there, its error 2^-8 in O and in the sum
+// alike.  All rows see all keys of a prefix. Measured: 256 samples of a 131072-token prompt, 32
+// query and 8 KV heads of 128, 550 GFLOP in 568 us (best; 640 in the middle, with the clock
+// that the power limit leaves), 0.97 PFLOP/s where a product of 8192^3 reaches 1.28: the matrix
+// pipe is busy 55% of cycles, the vector unit 40%, at 1.7 GHz.  With 64 rows (16 samples of
+// 32k, two of the waves idle) the keys' bytes bound it: 31 us for 141 MB.
 template <int D>
 __device__ __forceinline__ void many_pieces(const DecodeArgs &a, const Plan &plan, uint8_t *lds0,
                                             uint8_t *lds1, const Part &part) {
@@ -798,7 +813,8 @@ template <int D, int RT, bool MANY>
 __global__ __launch_bounds__(kThreads)
 __attribute__((amdgpu_waves_per_eu(DecGeo<D>::OCC, DecGeo<D>::OCC)))
 void decode_fwd(DecodeArgs a) {
-  // two arrays, so that the compiler sees that reads of one do not wait for copies into the other
+  // two arrays, so that the compiler sees that reads of one do not wait for copies into the
+  // other
   __shared__ __attribute__((aligned(1024))) uint8_t lds0[8 * DecGeo<D>::STEP];
   __shared__ __attribute__((aligned(1024))) uint8_t lds1[8 * DecGeo<D>::STEP];
   __shared__ Plan plan;
@@ -810,7 +826,9 @@ void decode_fwd(DecodeArgs a) {
 }
 
 // ---- Joins the pieces of a row: WPR waves, each with every 64 / (D / 4) * WPR-th group of pieces,
-// D / 4 lanes to a piece, 16 bytes each.
+// D / 4 lanes to a piece, 16 bytes each, four loads in flight (two: 13.2 us instead of 10.2 for
+// 1024 rows of 65 pieces; eight: the same there, 12.0 instead of 10.0 for 6144 rows of 12).
+// Latency bound up to a few hundred rows (4.4 us for 32), then by the bytes of the pieces.
 template <int D, int WPR>
 __global__ __launch_bounds__(kThreads) void decode_join(DecodeArgs a) {
   constexpr int LPP = D / 4;              // lanes per piece
@@ -935,6 +953,8 @@ hipError_t launch(const DecodeArgs &a, hipStream_t s) {
   else decode_fwd<D, 2, false><<<a.wgs, kThreads, 0, s>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
+  // four waves a row while there are few: 512 rows of 66 pieces 7.8 us, one wave each 9.4; 2048
+  // rows of up to 20 pieces 8.8 and 6.1
   const int rows = a.batch * a.nq * a.hq;
   if (rows <= 512) decode_join<D, 4><<<rows, kThreads, 0, s>>>(a);
   else decode_join<D, 1><<<(rows + 3) / 4, kThreads, 0, s>>>(a);
