@@ -78,7 +78,8 @@ __device__ __forceinline__ int lean_tiles(const DecodeArgs &a, int rows) {
 }
 
 // Number of the partial result of row tile 0 and KV head 0 of a prefix, less its workgroup's: a
-// group's row tiles start at (its first row) / (rows of a tile) + its number.
+// group's row tiles start at (its first row) / (rows of a tile) + its number, which leaves each
+// group as many as it has.
 __device__ __forceinline__ int prefix_base(const DecodeArgs &a, int g, bool many) {
   return (a.start[g] * a.nq * a.G / (many ? kDecodeRows : a.tile_rows) + g) * a.hkv;
 }
@@ -318,8 +319,8 @@ __device__ __forceinline__ Piece piece_at(const DecodeArgs &a, const Plan &p, in
   r.t0 = max(x - at, 0);
   r.t1 = max(min(part.hi - at, n), r.t0);
   r.end = at + n;
-  r.slot = cluster ? (part.wg + g * a.hkv + seg) * many_tiles(rows) + part.tile
-                   : part.wg + base + seg;
+  // (a cluster's row tiles are as many as its workgroups)
+  r.slot = cluster ? (part.wg + seg) * many_tiles(rows) + part.tile + base : part.wg + base + seg;
   r.whole = whole && r.t0 == 0 && r.t1 == n;
   return r;
 }
@@ -873,8 +874,7 @@ __global__ __launch_bounds__(kThreads) void decode_join(DecodeArgs a) {
     count[0] = cut.owner(at + n - 1) - first + 1;
     stride[0] = width * per * (D + 2);
     ml_at[0] = per * D + 2 * row - row * D;
-    const int base = width > 1 ? g * a.hkv : prefix_base(a, g, many);
-    const int slot = (first + base + seg) * width + (width > 1 ? tile : 0);
+    const int slot = (first + seg) * width + (width > 1 ? tile : 0) + prefix_base(a, g, many);
     from[0] = (many ? a.part_many : a.part_few) + (int64_t)slot * per * (D + 2) + row * D;
   }
   const int n = count[0] + count[1];

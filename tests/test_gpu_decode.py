@@ -174,6 +174,21 @@ def test_row_tiles_of_several_groups(sizes, prefix):
     Scene(groups, 8, 2, 64, 64, seed=sum(sizes)).run()
 
 
+@pytest.mark.parametrize("sizes", [(1,) * 60 + (150,), (1,) * 30 + (80, 1, 1, 90) + (2,) * 20,
+                                   (100, 90) + (1,) * 66])
+@pytest.mark.parametrize("hq,hkv,d", [(4, 1, 128), (16, 4, 64)])
+def test_large_groups_among_small_ones(sizes, hq, hkv, d):
+    """Partial results of a large group lie within the workspace whatever its number, and the
+    call writes nothing behind it."""
+    s = Scene([(100 + i, [1 + (11 * j) % 40 for j in range(n)]) for i, n in enumerate(sizes)],
+              hq, hkv, d, 32, seed=len(sizes))
+    q, c, b = s.queries(1), s.cache(), s.batch(1)
+    n = s.fpx.decode_workspace_size(c, b)
+    ws = torch.full((8 * n,), 0x5A, dtype=torch.uint8, device="cuda")
+    s.check(q, s.fpx.decode_attn(_dev(q), c, 0, b, workspace=ws[:n]), 1)
+    assert bool((ws[n:] == 0x5A).all())
+
+
 def test_a_long_prefix_of_many_rows():
     Scene([(40000, [3, 200] * 40)], 4, 1, 128, 128, seed=21).run()
 
