@@ -138,6 +138,11 @@ __device__ __forceinline__ Shares divide(int wgs, int many, int width, int lean)
 __device__ __forceinline__ Part make_plan(const DecodeArgs &a, Plan &p) {
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
   int len = 0, g = 0;
+  int rows = 0, want = 0;                 // of group t; read with the rest, before any barrier
+  if (a.any_prefix && t < a.groups) {
+    rows = group_rows(a, t);
+    want = a.prefix[t];
+  }
   if (t < a.batch) {
     g = a.group[t];
     if (a.slot[t] >= 0) len = min(max(a.len[a.slot[t]], 0), a.max_pages << a.page_shift);
@@ -156,18 +161,33 @@ __device__ __forceinline__ Part make_plan(const DecodeArgs &a, Plan &p) {
       p.rows_hi = 0;
     }
     __syncthreads();
-    if (len > 0) {
-      atomicMin(&p.prefix[g], max(len - a.nq, 0));
-      atomicMin(&p.lead[g], t);
-      atomicAdd(&p.live[g], 1);
+    const unsigned long long any = __ballot(len > 0);
+    if (any) {
+      // a wave whose sequences are all of one group takes their least length by lane moves
+      const int lead = __builtin_ctzll(any), g0 = __builtin_amdgcn_readlane(g, lead);
+      if (__ballot(len > 0 && g != g0)) {
+        if (len > 0) {
+          atomicMin(&p.prefix[g], max(len - a.nq, 0));
+          atomicMin(&p.lead[g], t);
+          atomicAdd(&p.live[g], 1);
+        }
+      } else {
+        int least = len > 0 ? max(len - a.nq, 0) : 0x7FFFFFFF;
+#pragma unroll
+        for (int d = 32; d > 0; d /= 2) least = min(least, __shfl_xor(least, d));
+        if (lane == lead) {
+          atomicMin(&p.prefix[g], least);
+          atomicMin(&p.lead[g], t);
+          atomicAdd(&p.live[g], __popcll(any));
+        }
+      }
     }
     __syncthreads();
     int tiles = 0;
     // one sequence alone has nothing to share
-    if (t < a.groups && p.live[t] >= 2) keys = min(p.prefix[t], a.prefix[t]) & ~15;
+    if (t < a.groups && p.live[t] >= 2) keys = min(p.prefix[t], want) & ~15;
     if (keys > 0) {
-      const bool many = is_many(a, t);
-      const int rows = group_rows(a, t);
+      const bool many = rows > kDecodeFew;
       tiles = many ? many_tiles(rows) : lean_tiles(a, rows);
       cost[many ? 0 : 1] = a.hkv * (tiles_of(keys) + kSegCost);
       if (many) {
