@@ -121,13 +121,17 @@ struct Part {
   int tile;             // many: row tile, when the cluster has one for each
 };
 
-// Work of the lines (`many` per row tile) in shares of a.wgs workgroups.
+// Work of the lines (`many` per row tile) in shares of a.wgs workgroups.  A place of the lean line
+// counts kLean times one of the other.  At 0.8, 1, 1.2, 1.4, 1.6: 256 samples of 128k 578, 575, 563,
+// 569, 571 us; 60 sequences of 60k with four queries at head dim 64 327, 328, 303, 304, 303; 100
+// samples of 60k (best) 154, 137, 139, 141, 142; 16 samples of 32k 45.7, 45.4, 45.8, 45.6, 45.0.
+constexpr float kLean = 1.2f;
 __device__ __forceinline__ Shares divide(int wgs, int many, int width, int lean) {
   Shares r = {0, width, 0};
   if (many > 0) {
     const float work = (float)many * width;
     const int most = (wgs - (lean > 0 ? 1 : 0)) / width;
-    r.clusters = (int)((float)wgs / width * (work / (work + lean)) + 0.5f);
+    r.clusters = (int)((float)wgs / width * (work / (work + kLean * lean)) + 0.5f);
     r.clusters = max(1, min(min(r.clusters, most), many));
   }
   r.lean = min(wgs - r.clusters * width, lean);
@@ -708,6 +712,11 @@ __device__ __forceinline__ void many_pieces(const DecodeArgs &a, const Plan &pla
 
   Piece cur = piece_at<true>(a, plan, plan.first, part.lo, part);
   if (cur.t0 == cur.t1) return;
+  // Of the two workgroups of a CU at head dim 128 the one started first is served first, and ended
+  // 10% before the other, whose work is as long.  The second (the grid's second half: the first
+  // fills every CU once) is put ahead in two of four tiles: 256 samples of 128k 588 -> 574 us, 16
+  // samples of 32k 46 -> 45.3; in every tile 594, in one of two 585, in eight of sixteen 588.
+  const bool second = D == 128 && 2 * (int)blockIdx.x >= a.wgs;
   int odd = 0;
   issue(cur, cur.t0, load.page(a, cur, cur.t0), lds0);
   int page_next = load.page(a, cur, min(cur.t0 + 1, cur.t1 - 1));
@@ -734,6 +743,8 @@ __device__ __forceinline__ void many_pieces(const DecodeArgs &a, const Plan &pla
 
     auto step = [&](uint8_t *tile, uint8_t *next, const int t) {
       const int k0 = cur.key0 + kKeys * t;
+      if (second && (t & 2)) __builtin_amdgcn_s_setprio(1);
+      else __builtin_amdgcn_s_setprio(0);
       wait_copies();                                     // this wave's part of tile t is here
       const bool edge = k0 + kKeys > cur.limit;
       if (edge)
