@@ -873,6 +873,7 @@ __global__ __launch_bounds__(kThreads) void decode_join(DecodeArgs a) {
   const int b = token / a.nq, t = token - b * a.nq, head = qh / a.G, kk = qh - head * a.G;
   const DecodeJoin &j = *a.join;
   const int4 seq = j.seq[b];              // tokens, prefix, places of own keys and of the prefix
+  const int4 grp = j.group[b];            // group, its first sequence, its rows, whether many
   const int len = seq.x, prefix = seq.y;
   uint16_t *op = a.o + id * D;
   const float c = a.scale_log2;
@@ -892,7 +893,6 @@ __global__ __launch_bounds__(kThreads) void decode_join(DecodeArgs a) {
     from[1] = a.part_own + (int64_t)(first + b * a.hkv * tiles + seg) * stride[1] + row * D;
   }
   if (prefix > 0) {
-    const int4 grp = j.group[b];          // group, its first sequence, its rows, whether many
     const int g = grp.x, many = grp.w;
     const int per = many ? kDecodeRows : a.tile_rows, width = many ? j.width : 1;
     const int r = ((b - grp.y) * a.nq + t) * a.G + kk, tile = r / per, row = r - tile * per;
@@ -918,6 +918,15 @@ __global__ __launch_bounds__(kThreads) void decode_join(DecodeArgs a) {
   f32x4 acc = f32x4{};
   for (int i0 = 0; i0 < n; i0 += 64) {
     const int k = min(64, n - i0);
+    constexpr int U = 4;                  // loads in flight
+    f32x4 x[U];
+    auto fetch = [&](int i) {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        x[u] = *reinterpret_cast<const f32x4 *>(
+            piece(i0 + min(i + u * WPR * PPW + lane / LPP, k - 1)) + 4 * (lane % LPP));
+    };
+    fetch(part * PPW);                    // beside the references, not after them
     float2 ml = make_float2(-INFINITY, 0.f);
     if (lane < k)
       ml = *reinterpret_cast<const float2 *>(piece(i0 + lane) +
@@ -935,16 +944,14 @@ __global__ __launch_bounds__(kThreads) void decode_join(DecodeArgs a) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[e] *= old;
     m = top;
-    constexpr int U = 4;                  // loads in flight
     for (int i = part * PPW; i < k; i += U * WPR * PPW) {
-      f32x4 x[U];
       float fi[U];
+      if (i != part * PPW) fetch(i);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int at = i + u * WPR * PPW + lane / LPP;
         fi[u] = __shfl(f, at & 63);       // (by all lanes)
         if (at >= k) fi[u] = 0.f;
-        x[u] = *reinterpret_cast<const f32x4 *>(piece(i0 + min(at, k - 1)) + 4 * (lane % LPP));
       }
 #pragma unroll
       for (int u = 0; u < U; ++u)
