@@ -40,6 +40,7 @@ class CacheError(RuntimeError):
 # These calls are made several times a layer and step, so the host's share of one counts: lists go
 # to the library as the bytes of int32 arrays, tensors as plain addresses.
 
+_int32 = np.dtype(np.int32)
 _bf16 = _device = _raw_stream = None
 
 
@@ -58,9 +59,9 @@ def _stream(stream):
 
 
 def _ints(x, name, n=None):
-    """x as a contiguous int32 host array of n elements."""
-    if (type(x) is np.ndarray and x.dtype == np.int32 and x.ndim == 1
-            and x.flags.c_contiguous and (n is None or x.size == n)):
+    """x as an int32 host array of n elements (tobytes and copy make it contiguous)."""
+    if (type(x) is np.ndarray and x.dtype is _int32 and x.ndim == 1
+            and (n is None or x.size == n)):
         return x
     a = np.ascontiguousarray(x if isinstance(x, np.ndarray) else list(x))
     if a.dtype != np.int32:
@@ -139,10 +140,17 @@ def cache_workspace_size(cache: Cache) -> int:
     return out.value
 
 
+def _given(workspace):
+    """The caller's workspace; its size is the library's to check, in bytes."""
+    if not (workspace.is_cuda and workspace.element_size() == 1 and workspace.is_contiguous()):
+        raise ValueError("workspace must be a contiguous uint8 CUDA tensor")
+    return workspace
+
+
 def _cache_workspace(cache, workspace, stream):
     if workspace is None:
         return _workspace(cache_workspace_size(cache), cache.meta.device, stream)
-    return workspace
+    return _given(workspace)
 
 
 def cache_init(cache: Cache, stream=None):
@@ -266,6 +274,8 @@ def decode_attn(q, cache: Cache, layer, batch: DecodeBatch, out=None, workspace=
             raise ValueError(f"out has shape {tuple(out.shape)}; the batch needs {(T, hq, d)}")
     if workspace is None:
         workspace = _workspace(decode_workspace_size(cache, batch), q.device, stream)
+    else:
+        _given(workspace)
     _call(lib().fp_decode_attn(cache.ref, batch.ref, layer, q.data_ptr(), stride,
                                out.data_ptr(), workspace.data_ptr(), workspace.numel(),
                                _stream(stream)), "fp_decode_attn")

@@ -270,9 +270,11 @@ size_t copies_layout(const fp_cache *c, char *base, fp::PageCopies *w) {
   return kAlign + 3 * list;
 }
 
-// Slot numbers of one call, distinct and in range; `seen` holds the slots so far.
+// Slot numbers of one call, distinct and in range; `seen` holds the slots so far.  Only the words
+// that the cache's slots need are cleared: these calls are made several times a layer.
 struct SlotSet {
-  uint64_t bits[65536 / 64] = {};
+  uint64_t bits[65536 / 64];
+  explicit SlotSet(const fp_cache *c) { memset(bits, 0, ((size_t)c->num_slots + 63) / 64 * 8); }
   bool add(int32_t s) {
     const uint64_t bit = (uint64_t)1 << (s & 63);
     const bool fresh = !(bits[s >> 6] & bit);
@@ -557,7 +559,7 @@ fp_status fp_cache_reserve(const fp_cache *cache, int32_t n, const int32_t *slot
   fp::CacheView c;
   fp_status st = check_cache(cache, &c);
   if (st != FP_OK) return st;
-  SlotSet seen;
+  SlotSet seen(cache);
   if ((st = check_slots(cache, n, slots, &seen)) != FP_OK) return st;
   if (!counts) return FP_ERR_INVALID_ARG;
   fp::CacheList l;
@@ -581,7 +583,7 @@ fp_status fp_cache_write(const fp_cache *cache, int32_t layer, int32_t n, const 
   fp::CacheView c;
   fp_status st = check_cache(cache, &c);
   if (st != FP_OK) return st;
-  SlotSet seen;
+  SlotSet seen(cache);
   if ((st = check_slots(cache, n, slots, &seen)) != FP_OK) return st;
   if (layer < 0 || layer >= cache->layers || !cu || cu[0] != 0) return FP_ERR_INVALID_ARG;
   const int64_t row = (int64_t)cache->num_kv_heads * cache->head_dim;
@@ -617,7 +619,7 @@ fp_status fp_cache_fork(const fp_cache *cache, int32_t n, const int32_t *src, co
   fp::CacheView c;
   fp_status st = check_cache(cache, &c);
   if (st != FP_OK) return st;
-  SlotSet seen;
+  SlotSet seen(cache);
   if ((st = check_slots(cache, n, dst, &seen)) != FP_OK) return st;
   if ((st = check_slots(cache, n, src, nullptr)) != FP_OK) return st;
   fp::ForkArgs a;
@@ -636,7 +638,7 @@ fp_status fp_cache_truncate(const fp_cache *cache, int32_t n, const int32_t *slo
   fp::CacheView c;
   fp_status st = check_cache(cache, &c);
   if (st != FP_OK) return st;
-  SlotSet seen;
+  SlotSet seen(cache);
   if ((st = check_slots(cache, n, slots, &seen)) != FP_OK) return st;
   fp::CacheList l;
   l.n = n;

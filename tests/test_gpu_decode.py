@@ -200,6 +200,26 @@ def test_several_groups(d):
     Scene(groups, 8, 2, d, 16, seed=d).run(2)
 
 
+@pytest.mark.parametrize("nq", [5, 16])
+def test_groups_of_fewer_tokens_than_queries(nq):
+    """A sequence with more queries than tokens leaves its group no prefix to share."""
+    Scene([(3, [0, 1, 30]), (40, [2, 9]), (0, [1, 2]), (2, [0, None])], 4, 2, 64, 16,
+          seed=nq).run(nq)
+
+
+@pytest.mark.parametrize("seed", range(10))
+def test_random_batches(seed):
+    rng = np.random.default_rng(1000 + seed)
+    hkv = int(rng.integers(1, 4))
+    groups = []
+    for _ in range(rng.integers(1, 9)):
+        own = [None if rng.random() < 0.1 else int(np.exp(rng.uniform(0, 6.2)))
+               for _ in range(rng.integers(1, 30))]
+        groups.append((0 if rng.random() < 0.3 else int(np.exp(rng.uniform(1, 6.8))), own))
+    Scene(groups, hkv * int(rng.integers(1, 9)), hkv, int(rng.choice([64, 128])),
+          int(rng.choice([16, 32, 64, 128, 256])), seed=seed).run(int(rng.choice([1, 1, 2, 7])))
+
+
 def test_a_sequence_shorter_than_the_prefix():
     """The group then shares what all of its queries see."""
     s = Scene([(300, [5, 9, 40])], 4, 1, 64, 32, seed=5)
@@ -419,6 +439,23 @@ def test_decoding_loop_in_a_graph():
         for a, b in zip(outs, want):
             assert torch.equal(a, b) and bool(torch.isfinite(a.float()).all()), i
     live.check()
+
+
+@pytest.mark.parametrize("make", [lambda n: torch.empty(n, dtype=torch.uint8),
+                                  lambda n: torch.empty(n, dtype=torch.int32, device="cuda"),
+                                  lambda n: torch.empty(2 * n, dtype=torch.uint8,
+                                                        device="cuda")[::2]])
+def test_refuses_workspaces_that_are_not_bytes_on_the_gpu(make):
+    s = Scene([(0, [5])], 4, 1, 64, 16, seed=18)
+    c, b = s.cache(), s.batch(1)
+    with pytest.raises(ValueError):
+        s.fpx.decode_attn(_dev(s.queries(1)), c, 0, b,
+                          workspace=make(s.fpx.decode_workspace_size(c, b)))
+    n = s.fpx.cache_workspace_size(c)
+    with pytest.raises(ValueError):
+        s.fpx.cache_reserve(c, [0], 1, workspace=make(n))
+    with pytest.raises(ValueError):
+        s.fpx.cache_compact(c, workspace=make(n))
 
 
 @pytest.mark.parametrize("bad", ["dtype", "rows", "heads", "out", "workspace", "layer"])
