@@ -685,10 +685,11 @@ __device__ __forceinline__ void lean_pieces(const DecodeArgs &a, const Plan &pla
 // scores are the consecutive keys that P^T of O^T += V^T P^T needs, one update of the reference
 // for 64 keys.  A weight is one bf16 number, as there, its error 2^-8 in O and in the sum
 // alike.  All rows see all keys of a prefix. Measured: 256 samples of a 131072-token prompt, 32
-// query and 8 KV heads of 128, 550 GFLOP in 568 us (best; 640 in the middle, with the clock
-// that the power limit leaves), 0.97 PFLOP/s where a product of 8192^3 reaches 1.28: the matrix
-// pipe is busy 55% of cycles, the vector unit 40%, at 1.7 GHz.  With 64 rows (16 samples of
-// 32k, two of the waves idle) the keys' bytes bound it: 31 us for 141 MB.
+// query and 8 KV heads of 128, 550 GFLOP in 554 us (best) to 589 (the clock that the power limit
+// leaves), 0.99 to 0.93 PFLOP/s where a product of 8192^3 reaches 1.34: the matrix pipe is busy
+// 55% of cycles, the vector unit 40%, at 1.7 GHz.  With 64 rows (16 samples of 32k, two of the
+// waves idle) the keys' bytes bound it: 35 to 41 us for 141 MB that come from memory, of which the
+// plan and the first tile are 8.7.
 template <int D>
 __device__ __forceinline__ void many_pieces(const DecodeArgs &a, const Plan &plan, uint8_t *lds0,
                                             uint8_t *lds1, const Part &part) {
