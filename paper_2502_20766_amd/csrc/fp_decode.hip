@@ -861,7 +861,10 @@ void decode_fwd(DecodeArgs a) {
 // ---- Joins the pieces of a row: WPR waves, each with every 64 / (D / 4) * WPR-th group of pieces,
 // D / 4 lanes to a piece, 16 bytes each, four loads in flight (two: 13.2 us instead of 10.2 for
 // 1024 rows of 65 pieces; eight: the same there, 12.0 instead of 10.0 for 6144 rows of 12).
-// Latency bound up to a few hundred rows (4.4 us for 32), then by the bytes of the pieces.
+// Latency bound up to a few hundred rows (4.4 us for 32), then by the bytes of the pieces, which
+// are read once: as ordinary loads the call with 16 samples of 32k takes 46.0 us, as these 44.3,
+// drafts at head dim 64 54.4 and 53.3.  (Nontemporal stores of the pieces: 45.1 and 54.6 in a row,
+// 3 us more for a call by itself.)  128 references at once instead of 64, eight waves a row: the same.
 template <int D, int WPR>
 __global__ __launch_bounds__(kThreads) void decode_join(DecodeArgs a) {
   constexpr int LPP = D / 4;              // lanes per piece
@@ -924,8 +927,8 @@ __global__ __launch_bounds__(kThreads) void decode_join(DecodeArgs a) {
     auto fetch = [&](int i) {
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        x[u] = *reinterpret_cast<const f32x4 *>(
-            piece(i0 + min(i + u * WPR * PPW + lane / LPP, k - 1)) + 4 * (lane % LPP));
+        x[u] = __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(
+            piece(i0 + min(i + u * WPR * PPW + lane / LPP, k - 1)) + 4 * (lane % LPP)));
     };
     fetch(part * PPW);                    // beside the references, not after them
     float2 ml = make_float2(-INFINITY, 0.f);
