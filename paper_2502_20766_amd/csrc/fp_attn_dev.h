@@ -71,23 +71,24 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t uniform_rsrc(const void *base,
 
 // Wave-wide 16-byte DMAs into LDS slots I .. N-1, slot i at i * 1024 past `dst` (the
 // immediate offset moves the source address by the same amount), with a per-lane offset
-// per slot (K) or one shared by all slots (V^T).
-template <int I, int N>
+// per slot (K) or one shared by all slots (V^T).  POLICY: cache policy bits of the load (2:
+// nontemporal).
+template <int I, int N, int POLICY = 0>
 __device__ __forceinline__ void dma_slots(__amdgpu_buffer_rsrc_t r,
                                           __attribute__((address_space(3))) void *dst,
                                           const uint32_t *voff) {
   if constexpr (I < N) {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, dst, 16, voff[I], 0, I * 1024, 0);
-    dma_slots<I + 1, N>(r, dst, voff);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, dst, 16, voff[I], 0, I * 1024, POLICY);
+    dma_slots<I + 1, N, POLICY>(r, dst, voff);
   }
 }
-template <int I, int N>
+template <int I, int N, int POLICY = 0>
 __device__ __forceinline__ void dma_slots(__amdgpu_buffer_rsrc_t r,
                                           __attribute__((address_space(3))) void *dst,
                                           uint32_t voff) {
   if constexpr (I < N) {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, dst, 16, voff, 0, I * 1024, 0);
-    dma_slots<I + 1, N>(r, dst, voff);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, dst, 16, voff, 0, I * 1024, POLICY);
+    dma_slots<I + 1, N, POLICY>(r, dst, voff);
   }
 }
 
