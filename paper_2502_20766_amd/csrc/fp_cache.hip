@@ -249,8 +249,10 @@ __global__ __launch_bounds__(256) void cache_copy(CacheView c, PageCopies w) { c
 // Keys are rows, copied as they are; values go through LDS and leave as 16-byte units of eight
 // tokens of one head dimension.  A unit that also holds older tokens is written element by
 // element.  Memory bound for long pieces (110k tokens, 8 KV heads of 128, 900 MB read and
-// written in two layers: 92 us a layer, 4.9 TB/s), latency bound for one token a slot (4.8 us
-// for 64 slots).
+// written in two layers: 84 us a layer, 5.4 TB/s), latency bound for one token a slot (4.8 us
+// for 64 slots).  What passes through is not read again soon, so loads and stores are nontemporal:
+// that call 195.7 -> 178.3 us, with loads or stores alone 192.5 and 183.1 (and 210 after a call
+// that left the caches full of its writes, where both take 183).
 template <int D>
 __global__ __launch_bounds__(256) void cache_write(CacheView c, WriteArgs a) {
   constexpr int CPR = D / 8;                 // 16-byte chunks per row
@@ -281,8 +283,8 @@ __global__ __launch_bounds__(256) void cache_write(CacheView c, WriteArgs a) {
     const int u = tid + 256 * i, r = u / CPR, ch = u % CPR, t = p0 + r;
     if (t < lo || t >= end) continue;
     const int64_t row = row0 + (t - start);
-    kx[i] = *(const Unit *)(a.k + row * a.k_stride + h * D + ch * 8);
-    vx[i] = *(const Unit *)(a.v + row * a.v_stride + h * D + ch * 8);
+    kx[i] = __builtin_nontemporal_load((const Unit *)(a.k + row * a.k_stride + h * D + ch * 8));
+    vx[i] = __builtin_nontemporal_load((const Unit *)(a.v + row * a.v_stride + h * D + ch * 8));
   }
   // pages of the four 16-token steps, or -1 for one that is not this slot's alone
   if (tid < 4) {
@@ -307,7 +309,7 @@ __global__ __launch_bounds__(256) void cache_write(CacheView c, WriteArgs a) {
   for (int i = 0; i < 64 * CPR / 256; ++i) {
     const int u = tid + 256 * i, r = u / CPR, ch = u % CPR, t = p0 + r, p = s_page[r >> 4];
     if (t < lo || t >= end || p < 0) continue;
-    *(Unit *)(c.k + tile_of(p, t) + (t & 15) * D + ch * 8) = kx[i];
+    __builtin_nontemporal_store(kx[i], (Unit *)(c.k + tile_of(p, t) + (t & 15) * D + ch * 8));
   }
   for (int u = tid; u < 8 * D; u += 256) {   // 8 half steps x D
     const int half = u & 1, d = (u >> 1) % D, step = (u >> 1) / D;
@@ -321,7 +323,7 @@ __global__ __launch_bounds__(256) void cache_write(CacheView c, WriteArgs a) {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         x[j] = tile[r + 2 * j][d] | (uint32_t)tile[r + 2 * j + 1][d] << 16;
-      *(Unit *)to = x;
+      __builtin_nontemporal_store(x, (Unit *)to);
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j)
