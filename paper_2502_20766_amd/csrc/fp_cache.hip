@@ -212,8 +212,10 @@ __global__ __launch_bounds__(kPlanThreads) void cache_reserve(CacheView c, Cache
 // The page copies of a list in every layer.  blockIdx.x is a part (kCopyUnits 16-byte units) of
 // a page of K or V in one layer, blockIdx.y and every gridDim.y-th after it a copy.  Plain
 // 16-byte loads and stores, four in flight per thread; memory bound: 3.15 GB read and written
-// (3000 pages of 64 tokens in four layers) in 530-630 us on different cards, 5.0-5.9 TB/s, 7 MB
-// in 4.3 us.
+// (3000 pages of 64 tokens in four layers) in 530-610 us on different cards, 5.2-5.9 TB/s, 7 MB
+// in 4.3 us.  Compaction moves each page once and past the caches (634 -> 620 us for those pages);
+// copies of a shared page read it several times (31 copies 46 -> 55 us that way).
+template <bool kOnce>
 __device__ __forceinline__ void copy_pages(const CacheView &c, const PageCopies &w) {
   const int units = c.hkv * c.page * c.d / 8;
   const int parts = (units + kCopyUnits - 1) / kCopyUnits;
@@ -229,10 +231,14 @@ __device__ __forceinline__ void copy_pages(const CacheView &c, const PageCopies 
     Unit x[kCopyUnits / 256];
 #pragma unroll
     for (int j = 0; j < kCopyUnits / 256; ++j)
-      if (u0 + 256 * j < units) x[j] = from[u0 + 256 * j];
+      if (u0 + 256 * j < units)
+        x[j] = kOnce ? __builtin_nontemporal_load(from + u0 + 256 * j) : from[u0 + 256 * j];
 #pragma unroll
     for (int j = 0; j < kCopyUnits / 256; ++j)
-      if (u0 + 256 * j < units) to[u0 + 256 * j] = x[j];
+      if (u0 + 256 * j < units) {
+        if (kOnce) __builtin_nontemporal_store(x[j], to + u0 + 256 * j);
+        else to[u0 + 256 * j] = x[j];
+      }
   }
 }
 
@@ -243,7 +249,9 @@ dim3 copy_grid(const CacheView &c, int most) {
   return dim3((unsigned)x, (unsigned)(y < most ? y : most));
 }
 
-__global__ __launch_bounds__(256) void cache_copy(CacheView c, PageCopies w) { copy_pages(c, w); }
+__global__ __launch_bounds__(256) void cache_copy(CacheView c, PageCopies w) {
+  copy_pages<false>(c, w);
+}
 
 // ---- write: a workgroup writes the new tokens among 64 positions of one slot and KV head.
 // Keys are rows, copied as they are; values go through LDS and leave as 16-byte units of eight
@@ -466,7 +474,7 @@ __global__ __launch_bounds__(256) void cache_compact_move(CacheView c, PageCopie
     const int p = c.table[i];
     if (p >= n_used && p < c.pages) c.table[i] = w.renamed[p];
   }
-  copy_pages(c, w);
+  copy_pages<true>(c, w);
 }
 
 }  // namespace
