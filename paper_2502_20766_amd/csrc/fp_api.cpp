@@ -704,6 +704,7 @@ fp_status fp_decode_attn(const fp_cache *cache, const fp_decode *batch, int32_t 
   a.any_prefix = dm.many || dm.few;
   a.any_many = dm.many;
   a.tile_rows = dm.tile_rows;
+  a.tile_shift = dm.tile_rows == 32 ? 5 : 4;
   a.pages = c.pages;
   a.hkv = c.hkv;
   a.page_shift = c.page_shift;

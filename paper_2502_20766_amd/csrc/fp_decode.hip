@@ -74,14 +74,15 @@ __device__ __forceinline__ int many_tiles(int rows) {
   return (rows + kDecodeRows - 1) / kDecodeRows;
 }
 __device__ __forceinline__ int lean_tiles(const DecodeArgs &a, int rows) {
-  return (rows + a.tile_rows - 1) / a.tile_rows;
+  return (rows + a.tile_rows - 1) >> a.tile_shift;
 }
 
 // Number of the partial result of row tile 0 and KV head 0 of a prefix, less its workgroup's: a
 // group's row tiles start at (its first row) / (rows of a tile) + its number, which leaves each
 // group as many as it has.
 __device__ __forceinline__ int prefix_base(const DecodeArgs &a, int g, bool many) {
-  return (a.start[g] * a.nq * a.G / (many ? kDecodeRows : a.tile_rows) + g) * a.hkv;
+  const int first = a.start[g] * a.nq * a.G;
+  return ((many ? first / kDecodeRows : first >> a.tile_shift) + g) * a.hkv;
 }
 
 // A line of `total` places in `wgs` equal parts, the first total % wgs of them one place
@@ -107,6 +108,18 @@ __device__ __forceinline__ int wave_scan(int x) {
   return x;
 }
 
+// Least x of the wave, in every lane.
+__device__ __forceinline__ int wave_min(int x) {
+  constexpr int none = 0x7FFFFFFF;
+  x = min(x, __builtin_amdgcn_update_dpp(none, x, 0x111, 0xf, 0xf, false));   // row_shr 1
+  x = min(x, __builtin_amdgcn_update_dpp(none, x, 0x112, 0xf, 0xf, false));
+  x = min(x, __builtin_amdgcn_update_dpp(none, x, 0x114, 0xf, 0xf, false));
+  x = min(x, __builtin_amdgcn_update_dpp(none, x, 0x118, 0xf, 0xf, false));
+  x = min(x, __builtin_amdgcn_update_dpp(none, x, 0x142, 0xa, 0xf, false));   // row_bcast 15
+  x = min(x, __builtin_amdgcn_update_dpp(none, x, 0x143, 0xc, 0xf, false));   // row_bcast 31
+  return __builtin_amdgcn_readlane(x, 63);
+}
+
 // How the workgroups are divided: `clusters` times `width` of them take the line of many rows,
 // a cluster one part of it and each of its workgroups one row tile; `lean` the other line.
 struct Shares {
@@ -121,17 +134,24 @@ struct Part {
   int tile;             // many: row tile, when the cluster has one for each
 };
 
-// Work of the lines (`many` per row tile) in shares of a.wgs workgroups.  A place of the lean line
-// counts kLean times one of the other.  At 0.8, 1, 1.2, 1.4, 1.6: 256 samples of 128k 578, 575, 563,
-// 569, 571 us; 60 sequences of 60k with four queries at head dim 64 327, 328, 303, 304, 303; 100
-// samples of 60k (best) 154, 137, 139, 141, 142; 16 samples of 32k 45.7, 45.4, 45.8, 45.6, 45.0.
-constexpr float kLean = 1.2f;
-__device__ __forceinline__ Shares divide(int wgs, int many, int width, int lean) {
+// What a place of the lean line counts against one of the other: more than one where products
+// bound the prefixes (several row tiles), less where their bytes do.
+// Several row tiles, at 0.8, 1, 1.2, 1.4, 1.6: 256 samples of 128k 578, 575, 563, 569, 571 us; 60
+// sequences of 60k with four queries at head dim 64 327, 328, 303, 304, 303; 100 samples of 60k
+// (best) 154, 137, 139, 141, 142.
+// One, at 0.6, 0.7, 0.8, 0.9, 1, 1.2: 16 samples of 32k 42.4, 41.1, 40.5, 40.2, 40.5, 41.4; drafts
+// at head dim 64 51.7, 47.9, 47.9, 47.6, 48.6, 48.4; 20 sequences of 10k and 500 to 6000 of their
+// own 45.8, 44.3, 43.6, 44.6, 45.2, 49.0.
+constexpr float kLeanProducts = 1.2f, kLeanBytes = 0.85f;
+
+// Work of the lines (`many` per row tile) in shares of a.wgs workgroups.
+__device__ __forceinline__ Shares divide(int wgs, int many, int width, int lean,
+                                         float lean_cost) {
   Shares r = {0, width, 0};
   if (many > 0) {
     const float work = (float)many * width;
     const int most = (wgs - (lean > 0 ? 1 : 0)) / width;
-    r.clusters = (int)((float)wgs / width * (work / (work + kLean * lean)) + 0.5f);
+    r.clusters = (int)((float)wgs / width * (work / (work + lean_cost * lean)) + 0.5f);
     r.clusters = max(1, min(min(r.clusters, most), many));
   }
   r.lean = min(wgs - r.clusters * width, lean);
@@ -154,6 +174,7 @@ __device__ __forceinline__ Part make_plan(const DecodeArgs &a, Plan &p) {
   }
   int cost[3] = {0, 0, 0};                // groups of many rows, of few, own keys
   int width = 1, keys = 0;
+  float lean_cost = kLeanProducts;
   if (a.any_prefix) {
     if (t < a.groups) {
       p.prefix[t] = 0x7FFFFFFF;
@@ -176,9 +197,7 @@ __device__ __forceinline__ Part make_plan(const DecodeArgs &a, Plan &p) {
           atomicAdd(&p.live[g], 1);
         }
       } else {
-        int least = len > 0 ? max(len - a.nq, 0) : 0x7FFFFFFF;
-#pragma unroll
-        for (int d = 32; d > 0; d /= 2) least = min(least, __shfl_xor(least, d));
+        const int least = wave_min(len > 0 ? max(len - a.nq, 0) : 0x7FFFFFFF);
         if (lane == lead) {
           atomicMin(&p.prefix[g], least);
           atomicMin(&p.lead[g], t);
@@ -204,6 +223,7 @@ __device__ __forceinline__ Part make_plan(const DecodeArgs &a, Plan &p) {
     // a cluster per part where all prefixes have the same number of row tiles
     if (p.rows_lo == p.rows_hi && p.rows_hi <= a.wgs / 4) width = p.rows_hi;
     else cost[0] *= tiles;
+    if (p.rows_hi <= 1) lean_cost = kLeanBytes;
     cost[1] *= tiles;
   } else if (t < a.groups) {
     p.prefix[t] = 0;
@@ -237,7 +257,7 @@ __device__ __forceinline__ Part make_plan(const DecodeArgs &a, Plan &p) {
     p.many[kMaxList] = total[0];
     p.lean[kEnd] = places;
   }
-  const Shares sh = divide(a.wgs, total[0], width, places);
+  const Shares sh = divide(a.wgs, total[0], width, places, lean_cost);
   // Workgroups of one XCD (every eighth) take neighbouring parts, which share keys, unless
   // there is not work for all.
   const int crowd = sh.clusters * sh.width, used = crowd + sh.lean;
@@ -339,7 +359,7 @@ __device__ __forceinline__ Piece piece_at(const DecodeArgs &a, const Plan &p, in
   const int seg = (x - start) / (n + kSegCost);         // (KV head, row tile) of the entry
   const int at = start + seg * (n + kSegCost) + kSegCost;   // place of its first tile
   r.once = rows <= per;
-  r.head = seg / tiles;
+  r.head = tiles == 1 ? seg : seg / tiles;
   r.row0 = (cluster ? part.tile : seg - r.head * tiles) * per;
   r.rows = min(rows - r.row0, per);
   r.t0 = max(x - at, 0);
@@ -897,9 +917,9 @@ __global__ __launch_bounds__(kThreads) void decode_join(DecodeArgs a) {
   int count[2] = {0, 0}, stride[2] = {0, 0}, ml_at[2] = {0, 0};
   const float *from[2] = {a.part_own, a.part_own};
   if (len > 0) {
-    const int per = a.tile_rows, r = t * a.G + kk, row = r % per;
+    const int per = a.tile_rows, r = t * a.G + kk, row = r & (per - 1);
     const int tiles = lean_tiles(a, a.G * a.nq), n = tiles_of(len - prefix);
-    const int seg = head * tiles + r / per;
+    const int seg = head * tiles + (r >> a.tile_shift);
     const int at = seq.z + seg * (n + kSegCost) + kSegCost;
     const Cut cut(j.places_lean, j.lean);
     const int first = cut.owner(at);
@@ -911,7 +931,8 @@ __global__ __launch_bounds__(kThreads) void decode_join(DecodeArgs a) {
   if (prefix > 0) {
     const int g = grp.x, many = grp.w;
     const int per = many ? kDecodeRows : a.tile_rows, width = many ? j.width : 1;
-    const int r = ((b - grp.y) * a.nq + t) * a.G + kk, tile = r / per, row = r - tile * per;
+    const int r = ((b - grp.y) * a.nq + t) * a.G + kk;
+    const int tile = many ? r / kDecodeRows : r >> a.tile_shift, row = r & (per - 1);
     const int tiles = width > 1 ? 1 : many ? many_tiles(grp.z) : lean_tiles(a, grp.z);
     const int n = tiles_of(prefix);
     const int seg = head * tiles + (width > 1 ? 0 : tile);

@@ -200,6 +200,7 @@ struct DecodeArgs {
   int32_t any_prefix;          // some group may share a prefix
   int32_t any_many;            // ... with more than kDecodeFew rows
   int32_t tile_rows;           // query rows of a unit of the other work: 16 or 32
+  int32_t tile_shift;          // its logarithm: 4 or 5
   int32_t pages, hkv, page_shift, max_pages;
   int32_t G, hq, nq, batch, groups;
   int32_t wgs;                 // workgroups that the key ranges are divided among
