@@ -13,11 +13,6 @@ namespace {
 constexpr int kPlanThreads = 1024;   // the single workgroup that hands out pages
 constexpr int kCopyUnits = 1024;     // 16-byte units of a page copied by one workgroup at a time
 constexpr int kCopyGrid = 2048;      // workgroups of a copy whose length the host cannot know
-// Table rows that one thread takes a place of in fork and truncate: long lists (samples of one
-// prompt, which share most pages) share atomics, short ones are spread over more threads.
-// Eight slots, fork and free: 7.1 and 6.0 us at 16 rows a thread, 5.2 and 4.9 at 4; 100 and 40
-// slots of a 128k prompt: 10.3 and 7.5 at 16, 18.0 and 9.3 at 4.
-constexpr int kFewRows = 4, kManyRows = 16, kShortList = 32;
 
 // 16 bytes as a vector: arrays of a struct of four words were kept in scratch memory, which
 // cost a short copy 13 us.
@@ -500,24 +495,37 @@ hipError_t launch_cache_write(const CacheView &c, const WriteArgs &a, hipStream_
   return hipGetLastError();
 }
 
+// Table rows that one thread takes a place of in fork and truncate.  Slots of one prompt share most
+// pages and so atomics, of which long tables have many; but a thread's rows come one after the
+// other.  Fork and free, in us, at 4, 8 and 16 rows: 60 slots with 133 places 12.2, 14.3, 17.4; 100
+// with 480 15.6, 14.8, 18.1; 100 with 1900 19.6, 16.5, 17.9; 100 with 3800 23.5, 19.0, 19.6; 100 and
+// 40 with 8200 30.7, 22.5, 21.3; 30 with 7500 14.2 throughout.
+static int table_rows(const CacheView &c, int n) {
+  const int64_t places = (int64_t)n * c.max_pages;
+  if (n <= 32 || places <= 1 << 14) return 4;
+  return places <= 1 << 19 ? 8 : 16;
+}
+
 // Workgroups of fork and truncate: 256 places of the tables, `rows` slots of the list.
 static dim3 table_grid(const CacheView &c, int n, int rows) {
   return dim3((c.max_pages + 255) / 256, (n + rows - 1) / rows);
 }
 
 hipError_t launch_cache_fork(const CacheView &c, const ForkArgs &a, hipStream_t s) {
-  if (a.n <= kShortList)
-    cache_fork<kFewRows><<<table_grid(c, a.n, kFewRows), 256, 0, s>>>(c, a);
-  else
-    cache_fork<kManyRows><<<table_grid(c, a.n, kManyRows), 256, 0, s>>>(c, a);
+  const int rows = table_rows(c, a.n);
+  const dim3 grid = table_grid(c, a.n, rows);
+  if (rows == 4) cache_fork<4><<<grid, 256, 0, s>>>(c, a);
+  else if (rows == 8) cache_fork<8><<<grid, 256, 0, s>>>(c, a);
+  else cache_fork<16><<<grid, 256, 0, s>>>(c, a);
   return hipGetLastError();
 }
 
 hipError_t launch_cache_truncate(const CacheView &c, const CacheList &l, hipStream_t s) {
-  if (l.n <= kShortList)
-    cache_truncate<kFewRows><<<table_grid(c, l.n, kFewRows), 256, 0, s>>>(c, l);
-  else
-    cache_truncate<kManyRows><<<table_grid(c, l.n, kManyRows), 256, 0, s>>>(c, l);
+  const int rows = table_rows(c, l.n);
+  const dim3 grid = table_grid(c, l.n, rows);
+  if (rows == 4) cache_truncate<4><<<grid, 256, 0, s>>>(c, l);
+  else if (rows == 8) cache_truncate<8><<<grid, 256, 0, s>>>(c, l);
+  else cache_truncate<16><<<grid, 256, 0, s>>>(c, l);
   return hipGetLastError();
 }
 

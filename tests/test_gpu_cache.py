@@ -160,6 +160,32 @@ def test_many_children_of_one():
     p.same("free")
 
 
+@pytest.mark.parametrize("max_pages", [20, 300, 6000])
+@pytest.mark.parametrize("n", [40, 101])
+def test_long_lists_and_long_tables(max_pages, n):
+    """Forks of several sequences over old ones that share their pages, and lists cut in the
+    middle of shared pages, for every length of tables; the last thread's rows not full."""
+    p = Pair(1, 2 * max_pages + 3 * n, 1, 64, n + 3, max_pages, 16)
+    tokens = 16 * max_pages - 40
+    for i in range(3):                   # three sequences, the second one a fork of the first
+        if i == 1:
+            p.fork([0], [1])
+            p.append([1], [20])
+        else:
+            p.reserve([i], [tokens - 16 * i])
+    src = [int(x) for x in p.rng.integers(0, 3, n)]
+    dst = [int(x) for x in 3 + p.rng.permutation(n)]
+    p.fork(src, dst)
+    p.same("fork")
+    again = [int(x) for x in p.rng.integers(0, 3, n)]
+    p.fork(again, dst)                   # over copies of other sequences
+    p.same("fork over forks")
+    p.truncate(dst, [int(x) for x in p.rng.integers(0, tokens, n)])
+    p.same("truncate")
+    p.free([0] + dst[:n // 2])
+    p.same("free")
+
+
 @pytest.mark.parametrize("page", [16, 64])
 @pytest.mark.parametrize("pages", [63, 64, 65, 300])
 def test_compact(page, pages):
