@@ -34,9 +34,9 @@ constexpr int kThreads = 256;
 constexpr int kMaxList = FP_MAX_CACHE_LIST;
 constexpr float kLazy = 8.f;              // rise (log2 units) that moves a row's reference
 // Places of the line, beside its tiles, that a segment takes: starting and ending a piece costs
-// a workgroup about as much as this many tiles.  At 1, 2, 3, 4, 6: 64 sequences of 3 to 32000
-// tokens 100, 95, 93, 94, 94 us; 16 samples of 32k 30.6, 31.2, 32.3, 32.6, 33.2; 256 samples of
-// 128k (best of 20) 749, 579, 583, 589, 610.
+// a workgroup about as much as this many tiles.  At 1, 2, 3, 4: 64 sequences of 3 to 32000 tokens
+// 90.2, 86.8, 87.4, 88.2 us; 16 samples of 32k 41.2, 40.0, 40.6, 41.0; 256 samples of 128k 588, 574,
+// 579, 586; 60 sequences of 60k with four queries at head dim 64 327, 306, 308, 305.
 constexpr int kSegCost = 2;
 
 static_assert(kThreads == kMaxList, "the plan has one thread per sequence");
@@ -152,7 +152,9 @@ __device__ __forceinline__ Shares divide(int wgs, int many, int width, int lean,
     const float work = (float)many * width;
     const int most = (wgs - (lean > 0 ? 1 : 0)) / width;
     r.clusters = (int)((float)wgs / width * (work / (work + lean_cost * lean)) + 0.5f);
-    r.clusters = max(1, min(min(r.clusters, most), many));
+    // two places at least to a part, so that short prefixes leave fewer pieces: 4 sequences of 20k
+    // that share 64 rows 28.7 -> 23.1 us; three places: 20.7, but others 10% more
+    r.clusters = max(1, min(min(r.clusters, most), many / 2));
   }
   r.lean = min(wgs - r.clusters * width, lean);
   return r;
@@ -487,7 +489,7 @@ __device__ __forceinline__ float quad_sum(float x) {
 //   twice: a weight is the sum of two bf16 numbers (error 2^-17), the second one in places where
 //   V^T is repeated.  That costs no product, and the keys' bytes bound the kernel anyway.
 // Measured: 64 sequences of 3 to 32000 tokens, 32 query and 8 KV heads of 128, 507 MB of keys
-// and values in 93 us, 5.4 TB/s (a copy of 1 GiB moves 5.1); pages of 16 and of 64 tokens the
+// and values in 83 us, 6.1 TB/s (a copy of 1 GiB moves 5.3); pages of 16 and of 64 tokens the
 // same.  With 32-row products instead (one wave 32 keys, weights in one piece, joined in pairs)
 // the same bytes took 189 us.  256 sequences of 100 tokens, two tiles a segment: 27 us for 105
 // MB.
@@ -717,11 +719,11 @@ __device__ __forceinline__ void lean_pieces(const DecodeArgs &a, const Plan &pla
 // scores are the consecutive keys that P^T of O^T += V^T P^T needs, one update of the reference
 // for 64 keys.  A weight is one bf16 number, as there, its error 2^-8 in O and in the sum
 // alike.  All rows see all keys of a prefix. Measured: 256 samples of a 131072-token prompt, 32
-// query and 8 KV heads of 128, 550 GFLOP in 554 us (best) to 589 (the clock that the power limit
-// leaves), 0.99 to 0.93 PFLOP/s where a product of 8192^3 reaches 1.34: the matrix pipe is busy
+// query and 8 KV heads of 128, 550 GFLOP in 535 to 570 us (by the clock that the power limit
+// leaves), 1.03 to 0.96 PFLOP/s where a product of 8192^3 reaches 1.34: the matrix pipe is busy
 // 55% of cycles, the vector unit 40%, at 1.7 GHz.  With 64 rows (16 samples of 32k, two of the
-// waves idle) the keys' bytes bound it: 35 to 41 us for 141 MB that come from memory, of which the
-// plan and the first tile are 8.7.
+// waves idle) the keys' bytes bound it: 30 to 33 us for 141 MB that come from memory, of which the
+// plan and the first tile are 8.
 template <int D>
 __device__ __forceinline__ void many_pieces(const DecodeArgs &a, const Plan &plan, uint8_t *lds0,
                                             uint8_t *lds1, const Part &part) {
@@ -747,9 +749,10 @@ __device__ __forceinline__ void many_pieces(const DecodeArgs &a, const Plan &pla
   if (cur.t0 == cur.t1) return;
   // Of the two workgroups of a CU at head dim 128 the one started first is served first, and ended
   // 10% before the other, whose work is as long.  The second (the grid's second half: the first
-  // fills every CU once) is put ahead in two of four tiles: 256 samples of 128k 588 -> 574 us, 16
-  // samples of 32k 46 -> 45.3; in every tile 594, in one of two 585, in eight of sixteen 588.
-  const bool second = D == 128 && 2 * (int)blockIdx.x >= a.wgs;
+  // fills every CU once) is put ahead in two of four tiles, except in clusters, which go at the
+  // pace of all: 16 samples of 32k 40.8 -> 40.0 us; with clusters too 256 samples of 128k take 574
+  // instead of 553, 100 of 60k 147 instead of 143.  Three workgroups at head dim 64: no difference.
+  const bool second = D == 128 && part.tile < 0 && 2 * (int)blockIdx.x >= a.wgs;
   int odd = 0;
   issue(cur, cur.t0, load.page(a, cur, cur.t0), lds0);
   int page_next = load.page(a, cur, min(cur.t0 + 1, cur.t1 - 1));

@@ -214,8 +214,8 @@ struct DecodeArgs {
 // Query rows of one unit of work on prefixes with many rows: 4 waves of 32.
 constexpr int kDecodeRows = 128;
 // Rows up to which a prefix is read like a sequence's own keys, in tiles of 16 or 32 rows.  Two such
-// tiles for 64 rows (16 samples of 32k): 48 us, one tile of 128 rows half empty 32; four for 128 rows
-// (32 samples of 64k): 165 and 66.
+// tiles for 64 rows (16 samples of 32k): 57 us, one tile of 128 rows half empty 40; five groups of 48
+// rows (12 samples of 9k) 76 and 49.6.
 constexpr int kDecodeFew = 32;
 // Workgroups that fp_decode_attn divides its keys among: every one resident, two (head dim 128)
 // or three (64) on each of 256 CUs.
