@@ -201,12 +201,16 @@ fp_status fp_sparse_attn_noalloc(const fp_shape *shape, const void *q, const voi
  *
  * What only the device knows cannot be refused by the host.  A reserve that finds too few pages
  * or too short a table row changes nothing and sets an error bit in state[1]; while a bit is set
- * reserve, fork, truncate and compact do nothing, and after a failed reserve write does nothing
- * either.  The caller reads the word when it synchronises anyway and clears it by storing 0. */
+ * reserve, fork, truncate and compact do nothing.  Write finds its place from the length that
+ * reserve, fork or truncate gave a slot, so once one of them has failed or has been left out
+ * write does nothing either, and tokens that are there already stay.  The caller reads the word
+ * when it synchronises anyway and clears it by storing 0. */
 #define FP_CACHE_FULL 1       /* fp_cache_reserve: fewer free pages than the call needs        */
 #define FP_CACHE_TOO_LONG 2   /* fp_cache_reserve: a slot would pass max_pages pages           */
 #define FP_CACHE_SHARED 4     /* fp_cache_write: tokens on a page that is not the slot's alone */
                               /* (not reserved), which were left out                           */
+#define FP_CACHE_SKIPPED 8    /* fp_cache_reserve, fp_cache_fork, fp_cache_truncate: left out  */
+                              /* because of FP_CACHE_SHARED, and the writes after them         */
 
 #define FP_MAX_CACHE_LIST 256         /* slots per call                                   */
 #define FP_MAX_CACHE_PAGES (1 << 22)  /* largest num_pages                                */

@@ -395,7 +395,7 @@ def masks_from_indices(indices: Indices):
     return out
 
 
-from .cache import (CACHE_FULL, CACHE_SHARED, CACHE_TOO_LONG, MAX_CACHE_LIST,  # noqa: E402,F401
-                    MAX_QUERIES, Cache, CacheError, DecodeBatch, cache_compact, cache_fork,
-                    cache_free, cache_init, cache_reserve, cache_truncate, cache_workspace_size,
-                    cache_write, decode_attn, decode_workspace_size)
+from .cache import (CACHE_FULL, CACHE_SHARED, CACHE_SKIPPED, CACHE_TOO_LONG,  # noqa: E402,F401
+                    MAX_CACHE_LIST, MAX_QUERIES, Cache, CacheError, DecodeBatch, cache_compact,
+                    cache_fork, cache_free, cache_init, cache_reserve, cache_truncate,
+                    cache_workspace_size, cache_write, decode_attn, decode_workspace_size)

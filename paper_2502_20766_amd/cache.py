@@ -21,7 +21,7 @@ import numpy as np
 
 from . import FP_OK, FpCache, FpDecode, _check, _check_tensor, _workspace, lib
 
-CACHE_FULL, CACHE_TOO_LONG, CACHE_SHARED = 1, 2, 4
+CACHE_FULL, CACHE_TOO_LONG, CACHE_SHARED, CACHE_SKIPPED = 1, 2, 4, 8
 MAX_CACHE_LIST = 256
 MAX_QUERIES = 16
 
@@ -33,7 +33,9 @@ class CacheError(RuntimeError):
         self.bits = bits
         names = [n for b, n in ((CACHE_FULL, "too few free pages"),
                                 (CACHE_TOO_LONG, "a sequence passes max_pages pages"),
-                                (CACHE_SHARED, "tokens written without a reserve")) if bits & b]
+                                (CACHE_SHARED, "tokens written without a reserve"),
+                                (CACHE_SKIPPED, "later calls and their writes left out"))
+                 if bits & b]
         super().__init__("; ".join(names) or f"error bits {bits}")
 
 

@@ -78,6 +78,13 @@ __device__ __forceinline__ void count_freed(const CacheView &c, int gone) {
   if ((threadIdx.x & 63) == 0 && gone) atomicSub(c.state, gone);
 }
 
+// A call that would have changed a slot's length is left out because an error bit is set.  If no
+// bit that stops writes is among them, this one is set: a write finds its place from the length,
+// and would land on tokens that are there already.
+__device__ __forceinline__ void left_out(const CacheView &c, int error) {
+  if (error == FP_CACHE_SHARED) atomicOr(c.state + 1, FP_CACHE_SKIPPED);
+}
+
 __global__ __launch_bounds__(256) void cache_init(CacheView c) {
   const int64_t n_zero = 8 + 2 * (int64_t)c.words + c.slots + c.pages;
   const int64_t n = n_zero + (int64_t)c.slots * c.max_pages;
@@ -104,7 +111,10 @@ __global__ __launch_bounds__(kPlanThreads) void cache_reserve(CacheView c, Cache
   const int tid = threadIdx.x;
   const int used_pages = c.state[0], error = c.state[1];
   if (error != 0) {
-    if (tid == 0) w.count[0] = 0;
+    if (tid == 0) {
+      w.count[0] = 0;
+      left_out(c, error);
+    }
     return;
   }
   const bool mine = tid < l.n;
@@ -268,7 +278,7 @@ __global__ __launch_bounds__(256) void cache_write(CacheView c, WriteArgs a) {
   const int error = c.state[1];
   __syncthreads();
   const int i = __builtin_amdgcn_readfirstlane(s_i);
-  if (error & (FP_CACHE_FULL | FP_CACHE_TOO_LONG)) return;
+  if (error & (FP_CACHE_FULL | FP_CACHE_TOO_LONG | FP_CACHE_SKIPPED)) return;
   const int row0 = a.list.num[i], n = a.list.num[i + 1] - row0;
   const int slot = a.list.slot[i];
   const int len = min(c.len[slot], c.max_pages << c.page_shift);
@@ -343,7 +353,11 @@ template <int kBatch>
 __global__ __launch_bounds__(256) void cache_fork(CacheView c, ForkArgs a) {
   const int first = blockIdx.y * kBatch, n = min(a.n - first, kBatch);
   const int j = blockIdx.x * 256 + threadIdx.x;
-  if (c.state[1] != 0) return;
+  const int error = c.state[1];
+  if (error != 0) {
+    if (j == 0 && blockIdx.y == 0) left_out(c, error);
+    return;
+  }
   int gone = 0;
   if (j < c.max_pages) {
     int now[kBatch], old[kBatch];
@@ -376,7 +390,11 @@ template <int kBatch>
 __global__ __launch_bounds__(256) void cache_truncate(CacheView c, CacheList l) {
   const int first = blockIdx.y * kBatch, n = min(l.n - first, kBatch);
   const int j = blockIdx.x * 256 + threadIdx.x;
-  if (c.state[1] != 0) return;
+  const int error = c.state[1];
+  if (error != 0) {
+    if (j == 0 && blockIdx.y == 0) left_out(c, error);
+    return;
+  }
   int gone = 0;
   if (j < c.max_pages) {
     int old[kBatch];
