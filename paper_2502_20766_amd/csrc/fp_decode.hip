@@ -470,6 +470,16 @@ __device__ __forceinline__ void wg_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// A weight as the sum of two bf16 numbers, both above zero if it is: both multiply the same value,
+// and an infinite one would meet a zero or the other sign in a second number that is what rounding
+// the first one left.  So the first is the largest bf16 number below the weight; the second, up to
+// 2^-7 of it, is rounded to 2^-9 of itself.
+__device__ __forceinline__ void split_weight(float w, __bf16 &top, __bf16 &low) {
+  const uint32_t below = __builtin_elementwise_sub_sat(__float_as_uint(w), 1u) & 0xFFFF0000u;
+  top = __builtin_bit_cast(__bf16, (uint16_t)(below >> 16));
+  low = (__bf16)(w - __uint_as_float(below));
+}
+
 // Largest x, and sum, over the four lanes that share lane % 16.
 __device__ __forceinline__ float quad_max(float x) {
   auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -486,8 +496,8 @@ __device__ __forceinline__ float quad_sum(float x) {
 //   S^T (16 keys x 16 rows) = K Q^T, D / 32 products; lane (row r = lane % 16, g = lane / 16) holds
 //   the scores of keys 4 g .. 4 g + 3;
 //   O^T += V^T P^T, D / 16 products.  The 32 places of a product's inner dimension are the 16 keys
-//   twice: a weight is the sum of two bf16 numbers (error 2^-17), the second one in places where
-//   V^T is repeated.  That costs no product, and the keys' bytes bound the kernel anyway.
+//   twice: a weight is the sum of two bf16 numbers (error 2^-16, see split_weight), the second one in
+//   places where V^T is repeated.  That costs no product, and the keys' bytes bound the kernel anyway.
 // Measured: 64 sequences of 3 to 32000 tokens, 32 query and 8 KV heads of 128, 507 MB of keys
 // and values in 83 us, 6.1 TB/s (a copy of 1 GiB moves 5.3); pages of 16 and of 64 tokens the
 // same.  With 32-row products instead (one wave 32 keys, weights in one piece, joined in pairs)
@@ -602,9 +612,10 @@ __device__ __forceinline__ void lean_pieces(const DecodeArgs &a, const Plan &pla
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float wt = __builtin_amdgcn_exp2f(fmaf(s[e], c, -mc[i]));
-          const __bf16 top = (__bf16)wt;
+          __bf16 top, low;
+          split_weight(wt, top, low);
           pf[i][e] = top;
-          pf[i][4 + e] = (__bf16)(wt - (float)top);
+          pf[i][4 + e] = low;
         }
         const bf16x8 pair[1] = {pf[i]};
         l_run[i] = sum_weights(pair, l_run[i]);
