@@ -205,15 +205,21 @@ def _stream_ptr(stream):
     return ctypes.c_void_p(s.cuda_stream)
 
 
+def _torch_stream(stream, device):
+    """`stream` as torch's: another object's raw handle (cuda_stream) is taken over."""
+    import torch
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    return torch.cuda.ExternalStream(stream.cuda_stream, device=device)
+
+
 def _workspace(n, device, stream):
     """n bytes for one call on `stream`, from that stream's memory: nothing pending on another
     stream still uses them, and nothing of another stream gets them while the call runs."""
     import torch
     if stream is None:
         return torch.empty(max(n, 1), dtype=torch.uint8, device=device)
-    if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(stream.cuda_stream, device=device)
-    with torch.cuda.stream(stream):
+    with torch.cuda.stream(_torch_stream(stream, device)):
         return torch.empty(max(n, 1), dtype=torch.uint8, device=device)
 
 

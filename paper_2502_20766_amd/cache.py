@@ -19,7 +19,7 @@ import ctypes
 
 import numpy as np
 
-from . import FP_OK, FpCache, FpDecode, _check, _check_tensor, _workspace, lib
+from . import (FP_OK, FpCache, FpDecode, _check, _check_tensor, _torch_stream, _workspace, lib)
 
 CACHE_FULL, CACHE_TOO_LONG, CACHE_SHARED, CACHE_SKIPPED = 1, 2, 4, 8
 MAX_CACHE_LIST = 256
@@ -125,9 +125,14 @@ class Cache:
         if not any(given):
             cache_init(self)
 
-    def check(self):
-        """Waits for the calls so far; if the device refused one since the last check, clears
-        the error, so that calls work again, and raises CacheError."""
+    def check(self, stream=None):
+        """Waits for the calls so far on `stream` or the current stream; if the device refused one
+        since the last check, clears the error there, so that calls work again, and raises
+        CacheError.  Calls on other streams are not waited for."""
+        if stream is not None:
+            import torch
+            with torch.cuda.stream(_torch_stream(stream, self.meta.device)):
+                return self.check()
         bits = int(self.state[1].item())
         if bits:
             self.state[1].zero_()

@@ -1,8 +1,8 @@
 """What the cache does between an error on the device and the check that finds it: tokens that are
 there already stay, whichever call was left out."""
-import numpy as np
 import pytest
 
+from cache_model import TOO_LONG
 from test_gpu_cache import Pair, gpu  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -74,3 +74,27 @@ def test_compaction_that_is_left_out_stops_no_write():
     with pytest.raises(p.fpx.CacheError) as e:
         p.c.check()
     assert e.value.bits == p.fpx.CACHE_SHARED
+
+
+@pytest.mark.parametrize("handle", ["stream", "raw"])
+def test_check_of_calls_on_another_stream(handle):
+    """The error of a call that is still waiting on its stream is found there, and cleared there."""
+    p, side = Pair(seed=33), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    given = side
+
+    class Raw:                           # a stream of another library: its handle alone
+        cuda_stream = side.cuda_stream
+
+    if handle == "raw":
+        given = Raw()
+    for _ in range(2):
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)
+        p.fpx.cache_reserve(p.c, [0], [10 ** 6], stream=given)
+        with pytest.raises(p.fpx.CacheError) as e:
+            p.c.check(stream=given)
+        assert e.value.bits == TOO_LONG
+        p.c.check(stream=given)
+    p.append([0], [5])
+    p.same()
