@@ -2,7 +2,8 @@
 
 Marshalling only, as in the rest of the binding: a `Cache` holds the tensors of fp_cache, a
 `DecodeBatch` the host arrays of fp_decode with their pointers, and every call enqueues the
-library's kernels on the current stream (or `stream`) without waiting for the GPU.
+library's kernels on `stream`, or on the current stream of the cache's device, without waiting for
+the GPU.  All tensors of a call lie on the cache's device; the caller need not have made it current.
 
     cache = Cache(layers, num_pages, num_kv_heads, head_dim, num_slots, max_pages)
     cache_reserve(cache, [0], [len(prompt)])          # once for all layers
@@ -55,11 +56,6 @@ def _load_torch():
     _device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 
 
-def _stream(stream):
-    """The raw handle of `stream` or of the current stream."""
-    return _raw_stream(_device()) if stream is None else stream.cuda_stream
-
-
 def _ints(x, name, n=None):
     """x as an int32 host array of n elements (tobytes and copy make it contiguous)."""
     if (type(x) is np.ndarray and x.dtype is _int32 and x.ndim == 1
@@ -76,6 +72,27 @@ def _ints(x, name, n=None):
         raise ValueError(f"{name} must be a list of {n if n is not None else 'any number of'} "
                          f"integers, got shape {a.shape}")
     return a
+
+
+def _check_stream(cache, stream):
+    if getattr(stream, "device_index", cache.index) != cache.index:
+        raise ValueError(f"the stream is on device {stream.device_index}, the cache on "
+                         f"{cache.index}")
+
+
+def _stream(cache, stream):
+    """The raw handle of `stream` or of the current stream of the cache's device."""
+    if stream is None:
+        return _raw_stream(cache.index)
+    _check_stream(cache, stream)
+    return stream.cuda_stream
+
+
+def _there(cache, call, *args):
+    """call(*args) with the cache's device current: kernels start on the one that is."""
+    import torch
+    with torch.cuda.device(cache.index):
+        return call(*args)
 
 
 def _call(status, what):
@@ -112,6 +129,9 @@ class Cache:
             _check_tensor(x, name, len(shape), dtype)
             if tuple(x.shape) != tuple(shape):
                 raise ValueError(f"{name} has shape {tuple(x.shape)}; the cache needs {shape}")
+        self.index = meta.get_device()
+        if not k.get_device() == v.get_device() == self.index:
+            raise ValueError("k, v and meta must lie on one device")
         if _bf16 is None:
             _load_torch()
         self.k, self.v, self.meta = k, v, meta
@@ -130,6 +150,7 @@ class Cache:
         since the last check, clears the error there, so that calls work again, and raises
         CacheError.  Calls on other streams are not waited for."""
         if stream is not None:
+            _check_stream(self, stream)
             import torch
             with torch.cuda.stream(_torch_stream(stream, self.meta.device)):
                 return self.check()
@@ -147,88 +168,104 @@ def cache_workspace_size(cache: Cache) -> int:
     return out.value
 
 
-def _given(workspace):
+def _given(cache, workspace):
     """The caller's workspace; its size is the library's to check, in bytes."""
-    if not (workspace.is_cuda and workspace.element_size() == 1 and workspace.is_contiguous()):
-        raise ValueError("workspace must be a contiguous uint8 CUDA tensor")
+    if not (workspace.get_device() == cache.index and workspace.element_size() == 1
+            and workspace.is_contiguous()):
+        raise ValueError("workspace must be a contiguous uint8 CUDA tensor on the cache's device")
     return workspace
 
 
 def _cache_workspace(cache, workspace, stream):
     if workspace is None:
         return _workspace(cache_workspace_size(cache), cache.meta.device, stream)
-    return _given(workspace)
+    return _given(cache, workspace)
 
 
 def cache_init(cache: Cache, stream=None):
     """Every slot empty, every page free."""
-    _call(lib().fp_cache_init(cache.ref, _stream(stream)), "fp_cache_init")
+    if _device() != cache.index:
+        return _there(cache, cache_init, cache, stream)
+    _call(lib().fp_cache_init(cache.ref, _stream(cache, stream)), "fp_cache_init")
 
 
 def cache_reserve(cache: Cache, slots, counts, workspace=None, stream=None):
     """Room for counts[i] (or the same count for all) more tokens in slots[i], once for all
     layers.  A shared last page that is not full is copied first.  If pages run out or a slot
     would grow past max_pages nothing changes, and Cache.check raises."""
+    if _device() != cache.index:
+        return _there(cache, cache_reserve, cache, slots, counts, workspace, stream)
     slots = _ints(slots, "slots")
     n = slots.size
     counts = (np.full(n, counts, np.int32) if isinstance(counts, (int, np.integer))
               else _ints(counts, "counts", n))
     ws = _cache_workspace(cache, workspace, stream)
     _call(lib().fp_cache_reserve(cache.ref, n, slots.tobytes(), counts.tobytes(), ws.data_ptr(),
-                                 ws.numel(), _stream(stream)), "fp_cache_reserve")
+                                 ws.numel(), _stream(cache, stream)), "fp_cache_reserve")
 
 
-def _check_rows(x, name, heads, d):
+def _check_rows(cache, x, name, heads):
     """Rows, and the stride between them, of a [T, heads, d] bf16 tensor with contiguous rows."""
-    shape, stride = x.shape, x.stride()
-    if len(shape) == 3 and x.is_cuda and x.dtype is _bf16:
+    shape, stride, d = x.shape, x.stride(), cache.head_dim
+    if len(shape) == 3 and x.get_device() == cache.index and x.dtype is _bf16:
         n, h, e = shape
         if h == heads and e == d and (n == 0 or (stride[2] == 1 and stride[1] == d)):
             return n, stride[0] if n > 1 else heads * d
-    raise ValueError(f"{name} must be a bf16 CUDA tensor [T, {heads}, {d}] with contiguous rows")
+    raise ValueError(f"{name} must be a bf16 tensor [T, {heads}, {d}] with contiguous rows on the "
+                     f"cache's device")
 
 
 def cache_write(cache: Cache, layer, k, v, slots, cu_seqlens, stream=None):
     """Keys and values of `layer` for the last cu_seqlens[i+1] - cu_seqlens[i] tokens of
     slots[i].  k, v: [T, Hkv, d] bf16, rows contiguous (slices of a fused projection do)."""
+    if _device() != cache.index:
+        return _there(cache, cache_write, cache, layer, k, v, slots, cu_seqlens, stream)
     slots = _ints(slots, "slots")
     cu = _ints(cu_seqlens, "cu_seqlens", slots.size + 1)
-    nk, ks = _check_rows(k, "k", cache.heads, cache.head_dim)
-    nv, vs = _check_rows(v, "v", cache.heads, cache.head_dim)
+    nk, ks = _check_rows(cache, k, "k", cache.heads)
+    nv, vs = _check_rows(cache, v, "v", cache.heads)
     if not nk == nv == cu[-1]:
         raise ValueError(f"k and v have {nk} and {nv} rows; cu_seqlens ends at {cu[-1]}")
     _call(lib().fp_cache_write(cache.ref, layer, slots.size, slots.tobytes(), cu.tobytes(),
-                               k.data_ptr(), ks, v.data_ptr(), vs, _stream(stream)),
+                               k.data_ptr(), ks, v.data_ptr(), vs, _stream(cache, stream)),
           "fp_cache_write")
 
 
 def cache_fork(cache: Cache, src, dst, stream=None):
     """dst[i] becomes a copy of src[i] that shares its pages; what it held is given back."""
+    if _device() != cache.index:
+        return _there(cache, cache_fork, cache, src, dst, stream)
     src = _ints(src, "src")
     dst = _ints(dst, "dst", src.size)
     _call(lib().fp_cache_fork(cache.ref, src.size, src.tobytes(), dst.tobytes(),
-                              _stream(stream)), "fp_cache_fork")
+                              _stream(cache, stream)), "fp_cache_fork")
 
 
 def cache_truncate(cache: Cache, slots, lens, stream=None):
     """slots[i] keeps its first lens[i] tokens (drafts that were not accepted, for one)."""
+    if _device() != cache.index:
+        return _there(cache, cache_truncate, cache, slots, lens, stream)
     slots = _ints(slots, "slots")
     lens = _ints(lens, "lens", slots.size)
     _call(lib().fp_cache_truncate(cache.ref, slots.size, slots.tobytes(), lens.tobytes(),
-                                  _stream(stream)), "fp_cache_truncate")
+                                  _stream(cache, stream)), "fp_cache_truncate")
 
 
 def cache_free(cache: Cache, slots, stream=None):
     """The slots become empty; their pages are free once no other slot holds them."""
+    if _device() != cache.index:
+        return _there(cache, cache_free, cache, slots, stream)
     slots = _ints(slots, "slots")
     _call(lib().fp_cache_truncate(cache.ref, slots.size, slots.tobytes(), None,
-                                  _stream(stream)), "fp_cache_truncate")
+                                  _stream(cache, stream)), "fp_cache_truncate")
 
 
 def cache_compact(cache: Cache, workspace=None, stream=None):
     """The pages in use become pages 0 .. state[0]-1, in every layer and table."""
+    if _device() != cache.index:
+        return _there(cache, cache_compact, cache, workspace, stream)
     ws = _cache_workspace(cache, workspace, stream)
-    _call(lib().fp_cache_compact(cache.ref, ws.data_ptr(), ws.numel(), _stream(stream)),
+    _call(lib().fp_cache_compact(cache.ref, ws.data_ptr(), ws.numel(), _stream(cache, stream)),
           "fp_cache_compact")
 
 
@@ -269,21 +306,25 @@ def decode_attn(q, cache: Cache, layer, batch: DecodeBatch, out=None, workspace=
                 stream=None):
     """Attention of the batch's query tokens over their sequences.  q: [batch * queries, Hq, d]
     bf16, rows contiguous, sequence by sequence; returns o of the same shape."""
+    if _device() != cache.index:
+        return _there(cache, decode_attn, q, cache, layer, batch, out, workspace, stream)
     T, hq, d = batch.rows, batch.heads, cache.head_dim
-    n, stride = _check_rows(q, "q", hq, d)
+    n, stride = _check_rows(cache, q, "q", hq)
     if n != T:
         raise ValueError(f"q has {n} rows; the batch has {T} query tokens")
     if out is None:
         out = _workspace(2 * T * hq * d, q.device, stream).view(_bf16).view(T, hq, d)
     else:
         _check_tensor(out, "out", 3)
+        if out.get_device() != cache.index:
+            raise ValueError("out must lie on the cache's device")
         if out.shape != (T, hq, d):
             raise ValueError(f"out has shape {tuple(out.shape)}; the batch needs {(T, hq, d)}")
     if workspace is None:
         workspace = _workspace(decode_workspace_size(cache, batch), q.device, stream)
     else:
-        _given(workspace)
+        _given(cache, workspace)
     _call(lib().fp_decode_attn(cache.ref, batch.ref, layer, q.data_ptr(), stride,
                                out.data_ptr(), workspace.data_ptr(), workspace.numel(),
-                               _stream(stream)), "fp_decode_attn")
+                               _stream(cache, stream)), "fp_decode_attn")
     return out
