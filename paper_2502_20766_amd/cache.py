@@ -209,7 +209,7 @@ def _check_rows(cache, x, name, heads):
     shape, stride, d = x.shape, x.stride(), cache.head_dim
     if len(shape) == 3 and x.get_device() == cache.index and x.dtype is _bf16:
         n, h, e = shape
-        if h == heads and e == d and (n == 0 or (stride[2] == 1 and stride[1] == d)):
+        if h == heads and e == d and (n == 0 or (stride[2] == 1 and (h == 1 or stride[1] == d))):
             return n, stride[0] if n > 1 else heads * d
     raise ValueError(f"{name} must be a bf16 tensor [T, {heads}, {d}] with contiguous rows on the "
                      f"cache's device")
