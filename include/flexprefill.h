@@ -233,7 +233,8 @@ typedef struct fp_cache {
 fp_status fp_cache_meta_size(const fp_cache *cache, size_t *elems);
 
 /* Device workspace bytes of fp_cache_reserve and fp_cache_compact: the list of page copies
- * that the call makes, and for compact the new number of every page.  Host only. */
+ * that the call makes, and for compact the new number of every page.  The workspace is 4-byte
+ * aligned.  Host only. */
 fp_status fp_cache_workspace_size(const fp_cache *cache, size_t *bytes);
 
 /* Every slot empty, every page free, no error.  The pools are left as they are. */
@@ -287,7 +288,8 @@ typedef struct fp_decode {
   float softmax_scale;         /* 0 => 1/sqrt(d)                                             */
 } fp_decode;
 
-/* Device workspace bytes of fp_decode_attn: partial results of key ranges.  Host only. */
+/* Device workspace bytes of fp_decode_attn: partial results of key ranges.  q, o and the workspace
+ * are 16-byte aligned.  Host only. */
 fp_status fp_decode_workspace_size(const fp_cache *cache, const fp_decode *batch, size_t *bytes);
 
 /* Attention of each sequence's last `queries` tokens over the whole sequence: query t (of

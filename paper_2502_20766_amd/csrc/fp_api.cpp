@@ -220,6 +220,7 @@ size_t plan_split(const fp::SeqTable &st, int hq, int hkv, int d, int block, siz
 }
 
 bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+bool aligned4(const void *p) { return ((uintptr_t)p & 3) == 0; }
 
 // Sizes of a cache; `view` (or null) gets the kernels' view of it.
 fp_status check_cache(const fp_cache *c, fp::CacheView *view) {
@@ -569,7 +570,7 @@ fp_status fp_cache_reserve(const fp_cache *cache, int32_t n, const int32_t *slot
     l.slot[i] = slots[i];
     l.num[i] = counts[i];
   }
-  if (!ws) return FP_ERR_INVALID_ARG;
+  if (!ws || !aligned4(ws)) return FP_ERR_INVALID_ARG;
   if (ws_bytes < copies_layout(cache, nullptr, nullptr)) return FP_ERR_WORKSPACE;
   fp::PageCopies w;
   copies_layout(cache, (char *)ws, &w);
@@ -655,7 +656,7 @@ fp_status fp_cache_compact(const fp_cache *cache, void *ws, size_t ws_bytes, voi
   fp::CacheView c;
   const fp_status st = check_cache(cache, &c);
   if (st != FP_OK) return st;
-  if (!ws) return FP_ERR_INVALID_ARG;
+  if (!ws || !aligned4(ws)) return FP_ERR_INVALID_ARG;
   if (ws_bytes < copies_layout(cache, nullptr, nullptr)) return FP_ERR_WORKSPACE;
   fp::PageCopies w;
   copies_layout(cache, (char *)ws, &w);
