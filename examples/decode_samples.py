@@ -62,7 +62,8 @@ def run(tokens=8192, samples=8, steps=16, layers=2, heads=32, kv_heads=8, head_d
         history.append([[k], [v]])
 
     # ---- one slot per sample; they share the prompt's pages until they write
-    fpx.cache_fork(cache, [0] * (samples - 1), np.arange(1, samples, dtype=np.int32))
+    if samples > 1:
+        fpx.cache_fork(cache, [0] * (samples - 1), np.arange(1, samples, dtype=np.int32))
 
     def decoder(alive):
         """A graph of one step of the samples in slots `alive`, its input and its outputs."""
@@ -103,7 +104,8 @@ def run(tokens=8192, samples=8, steps=16, layers=2, heads=32, kv_heads=8, head_d
 
     # ---- the first half ends; what they held is given back, the rest moves together
     ended, alive = everyone[:samples // 2], everyone[samples // 2:]
-    fpx.cache_free(cache, ended)
+    if len(ended):                                   # of one sample none does
+        fpx.cache_free(cache, ended)
     fpx.cache_compact(cache)
     say(f"{len(ended)} samples ended: {int(cache.state[0])} pages in use")
     x, out, seconds = decode(alive, len(alive) - 1)
