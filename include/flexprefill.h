@@ -300,7 +300,12 @@ fp_status fp_decode_workspace_size(const fp_cache *cache, const fp_decode *batch
  * matters: what lies in a page past its tokens, or in tokens after a query, does not reach it.
  * The keys and values of a group's prefix are read once for all of its sequences, from the pages
  * of the first one that is not empty; if a sequence of the group is shorter, as much of the
- * prefix as every query of the group sees. */
+ * prefix as every query of the group sees.
+ * Scores, maxima, sums and O are float32.  The weights that multiply the values are rounded to
+ * 2^-16 of themselves, over a prefix with more than 32 rows ((Hq / Hkv) * queries * sequences of
+ * the group) to bf16, 2^-8, as in fp_sparse_attn; the sum is that of the rounded weights.  The same
+ * call on the same state gives the same bits.  Where the keys are cut into ranges follows from the
+ * lengths and groups of the whole batch, so the last bits of a row depend on the rest of it. */
 fp_status fp_decode_attn(const fp_cache *cache, const fp_decode *batch, int32_t layer,
                          const void *q, int64_t q_stride, void *o, void *ws, size_t ws_bytes,
                          void *stream);

@@ -148,7 +148,8 @@ class Cache:
     def check(self, stream=None):
         """Waits for the calls so far on `stream` or the current stream; if the device refused one
         since the last check, clears the error there, so that calls work again, and raises
-        CacheError.  Calls on other streams are not waited for."""
+        CacheError.  Until then later reserves, forks, truncations and compactions are left out,
+        and so are the writes that would follow them.  Calls on other streams are not waited for."""
         if stream is not None:
             _check_stream(self, stream)
             import torch
@@ -305,7 +306,9 @@ def decode_workspace_size(cache: Cache, batch: DecodeBatch) -> int:
 def decode_attn(q, cache: Cache, layer, batch: DecodeBatch, out=None, workspace=None,
                 stream=None):
     """Attention of the batch's query tokens over their sequences.  q: [batch * queries, Hq, d]
-    bf16, rows contiguous, sequence by sequence; returns o of the same shape."""
+    bf16, rows contiguous, sequence by sequence; returns o of the same shape.  The last bits of a
+    row depend on the rest of the batch; weights over a prefix with more than 32 query rows of a KV
+    head are bf16 numbers, others are held to 2^-16 of themselves."""
     if _device() != cache.index:
         return _there(cache, decode_attn, q, cache, layer, batch, out, workspace, stream)
     T, hq, d = batch.rows, batch.heads, cache.head_dim

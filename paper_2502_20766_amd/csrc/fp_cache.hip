@@ -98,8 +98,8 @@ __global__ __launch_bounds__(256) void cache_init(CacheView c) {
 // its last page is not full and another slot will still hold it: with r holders, the first r -
 // 1 such slots of the list take copies.  The free pages, in ascending order, go to the slots in
 // list order; rank r among the free pages belongs to the slot whose range of the prefix sums
-// holds r, found by bisection. Latency bound (one workgroup, a chain of about six loads): 4.5
-// us for 64 slots and one token each, 7 for 1200 new pages.
+// holds r, found by bisection. Latency bound (one workgroup, a chain of about six loads): 4.8
+// us for 64 slots and one token each, 6.0 for 860 new pages, 7.2 with 31 copies.
 __global__ __launch_bounds__(kPlanThreads) void cache_reserve(CacheView c, CacheList l,
                                                               PageCopies w) {
   __shared__ int part[kPlanThreads / 64];
@@ -215,11 +215,12 @@ __global__ __launch_bounds__(kPlanThreads) void cache_reserve(CacheView c, Cache
 }
 
 // The page copies of a list in every layer.  blockIdx.x is a part (kCopyUnits 16-byte units) of
-// a page of K or V in one layer, blockIdx.y and every gridDim.y-th after it a copy.  Plain
-// 16-byte loads and stores, four in flight per thread; memory bound: 3.15 GB read and written
-// (3000 pages of 64 tokens in four layers) in 530-610 us on different cards, 5.2-5.9 TB/s, 7 MB
-// in 4.3 us.  Compaction moves each page once and past the caches (634 -> 620 us for those pages);
-// copies of a shared page read it several times (31 copies 46 -> 55 us that way).
+// a page of K or V in one layer, blockIdx.y and every gridDim.y-th after it a copy.  16-byte loads
+// and stores, four in flight per thread; memory bound: compaction reads and writes 3.15 GB (1500
+// pages of 64 tokens in four layers) in 619 us, 5.1 TB/s; a few pages take 4.3 us.  Compaction moves
+// each page once and past the caches (with its plan 634 -> 620 us for those pages); copies of a
+// shared page read it several times (reserve with 31 copies, and the writes: 46 -> 55 us that way).
+// Of such a page the whole is copied, 65 MB for 31 of 128 tokens in four layers: 13.6 us.
 template <bool kOnce>
 __device__ __forceinline__ void copy_pages(const CacheView &c, const PageCopies &w) {
   const int units = c.hkv * c.page * c.d / 8;
@@ -262,7 +263,7 @@ __global__ __launch_bounds__(256) void cache_copy(CacheView c, PageCopies w) {
 // Keys are rows, copied as they are; values go through LDS and leave as 16-byte units of eight
 // tokens of one head dimension.  A unit that also holds older tokens is written element by
 // element.  Memory bound for long pieces (110k tokens, 8 KV heads of 128, 900 MB read and
-// written in two layers: 84 us a layer, 5.4 TB/s), latency bound for one token a slot (4.8 us
+// written in two layers: 84 us a layer, 5.4 TB/s), latency bound for one token a slot (5.4 us
 // for 64 slots).  What passes through is not read again soon, so loads and stores are nontemporal:
 // that call 195.7 -> 178.3 us, with loads or stores alone 192.5 and 183.1 (and 210 after a call
 // that left the caches full of its writes, where both take 183).

@@ -591,8 +591,8 @@ __device__ __forceinline__ void lean_pieces(const DecodeArgs &a, const Plan &pla
 #pragma unroll
         for (int k = 0; k < KS; ++k)
           s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[k], qf[i][k], s, 0, 0, 0);
-        // (Not only on an edge: with a branch around these few instructions the compiler leaves
-        // out the wait between the product and what reads it on the other path.)
+        // (On every step: with a branch for the steps off the edges the times are the same, 4 short
+        // sequences 0.5 us more.)
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[e] = k0 + 4 * g4 + e < lim[i] ? s[e] : -INFINITY;
         const float mt = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
@@ -728,13 +728,16 @@ __device__ __forceinline__ void lean_pieces(const DecodeArgs &a, const Plan &pla
 // buffered, each wave bringing 16) and are read by all four waves; the products are those of
 // the prefill, on v_mfma_f32_32x32x16_bf16: S^T = K Q^T with K rows permuted so that a lane's
 // scores are the consecutive keys that P^T of O^T += V^T P^T needs, one update of the reference
-// for 64 keys.  A weight is one bf16 number, as there, its error 2^-8 in O and in the sum
-// alike.  All rows see all keys of a prefix. Measured: 256 samples of a 131072-token prompt, 32
+// for 64 keys.  A weight is one bf16 number, as there, its error 2^-8 in O and in the sum alike;
+// the error of the result, 1.6e-3 in norm against 64 bits, is that of its rounding all the same.  Two
+// numbers would be half as many products again: 40.3 -> 40.8 us for 64 rows (16 samples of 32k), where
+// the keys' bytes bound most of it, 48.2 -> 53.4 for 96 rows (drafts at head dim 64).
+// All rows see all keys of a prefix. Measured: 256 samples of a 131072-token prompt, 32
 // query and 8 KV heads of 128, 550 GFLOP in 535 to 570 us (by the clock that the power limit
 // leaves), 1.03 to 0.96 PFLOP/s where a product of 8192^3 reaches 1.34: the matrix pipe is busy
 // 55% of cycles, the vector unit 40%, at 1.7 GHz.  With 64 rows (16 samples of 32k, two of the
-// waves idle) the keys' bytes bound it: 30 to 33 us for 141 MB that come from memory, of which the
-// plan and the first tile are 8.
+// waves idle) 30 to 35 us for 141 MB that come from memory, of which the plan and the first tile
+// are 8.
 template <int D>
 __device__ __forceinline__ void many_pieces(const DecodeArgs &a, const Plan &plan, uint8_t *lds0,
                                             uint8_t *lds1, const Part &part) {
