@@ -271,7 +271,8 @@ fp_status fp_cache_truncate(const fp_cache *cache, int32_t n, const int32_t *slo
 
 /* The pages in use become pages 0 .. state[0]-1: the k-th free page below that number takes the
  * content (in every layer), holders and place in every table of the k-th page in use at or above
- * it.  The pools can then be cut to state[0] pages, or another cache laid behind them. */
+ * it.  The pools can then be cut to state[0] pages, or another cache laid behind them.  Where
+ * state[0] and the bitmap disagree (a caller's own bookkeeping) nothing moves. */
 fp_status fp_cache_compact(const fp_cache *cache, void *ws, size_t ws_bytes, void *stream);
 
 /* One batch of fp_decode_attn. */

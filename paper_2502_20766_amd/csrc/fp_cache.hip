@@ -442,6 +442,8 @@ __global__ __launch_bounds__(kPlanThreads) void cache_compact_plan(CacheView c, 
         const int below = min(max(n_used - word * 64, 0), 64);
         const unsigned long long mask = below == 64 ? ~0ull : (1ull << below) - 1;
         bits = pass == 0 ? ~bits & mask : bits & ~mask;
+        const int left = c.pages - word * 64;
+        if (left < 64) bits &= (1ull << left) - 1;
       }
       int found;
       s_base[tid] = block_scan(__popcll(bits), part, found) + seen;
@@ -465,6 +467,8 @@ __global__ __launch_bounds__(kPlanThreads) void cache_compact_plan(CacheView c, 
     if (pass == 0) {
       holes = seen;
       if (holes == 0) break;
+    } else if (seen != holes) {
+      holes = 0;                             // the bitmap and state[0] disagree: nothing moves
     }
   }
   if (tid == 0) w.count[0] = holes;
