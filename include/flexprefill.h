@@ -311,6 +311,103 @@ fp_status fp_decode_attn(const fp_cache *cache, const fp_decode *batch, int32_t 
                          const void *q, int64_t q_stride, void *o, void *ws, size_t ws_bytes,
                          void *stream);
 
+/* ---------------------------------------------------------------------------------------
+ * Between a layer's projection and its attention: norms of query and key heads and their rotation
+ * by position, by themselves (before fp_select and fp_sparse_attn) and on the way into the cache. */
+
+#define FP_ROPE_HALF 0         /* pairs (i, i + rotary_dim / 2) of a head                       */
+#define FP_ROPE_INTERLEAVED 1  /* pairs (2 i, 2 i + 1)                                          */
+
+#define FP_ROPE_UNSCALED 0
+#define FP_ROPE_LINEAR 1       /* every frequency divided by `factor`                           */
+#define FP_ROPE_BASE 2         /* base * factor^(R / (R - 2)): the first frequency stays, the   */
+                               /* last one is divided by `factor`                               */
+#define FP_ROPE_PARTS 3        /* by the turns t = original_len f / 2 pi that a pair makes in   */
+                               /* the original context: f g + (f / factor) (1 - g) with         */
+                               /* g = clamp((t - low_turns) / (high_turns - low_turns), 0, 1)   */
+
+typedef struct fp_rope_params {
+  int32_t rotary_dim;    /* R: the first R elements of a head are rotated; a multiple of 16,    */
+                         /* 16..128                                                             */
+  int32_t layout;        /* FP_ROPE_HALF or FP_ROPE_INTERLEAVED                                 */
+  int32_t scaling;       /* FP_ROPE_UNSCALED ..                                                 */
+  double base;           /* f_i = base^(-2 i / R) radians per position, i < R / 2; > 0          */
+  double factor;         /* >= 1 (scaling)                                                      */
+  double original_len, low_turns, high_turns;   /* FP_ROPE_PARTS: > 0, >= 0, > low_turns        */
+  double amplitude;      /* cosine and sine are multiplied by it; 0 => 1                        */
+  const double *inv_freq;  /* HOST [R / 2], or NULL: the frequencies themselves (|f| <= 2^20),  */
+                         /* unscaled; base is not looked at                                     */
+} fp_rope_params;
+
+/* Written by fp_rope_init; plain data, which may be copied. */
+typedef struct fp_rope {
+  int32_t rotary_dim, layout;
+  float amplitude;
+  int32_t reserved;
+  uint64_t step[64];     /* per pair: turns per position as a fraction of 2^64                  */
+} fp_rope;
+
+/* Host only. */
+fp_status fp_rope_init(const fp_rope_params *params, fp_rope *rope);
+
+/* RMS norm over a head: x / sqrt(mean(x^2) + eps) * weight. */
+typedef struct fp_head_norm {
+  const void *q_weight, *k_weight;  /* device [d], 16-byte aligned, or NULL: 1                  */
+  int32_t weight_f32;               /* the weights are float32, else bf16                       */
+  float eps;                        /* >= 2^-126                                                */
+} fp_head_norm;
+
+/* Heads of `tokens` tokens normed (norm == NULL: not) and rotated by positions[token] (rope ==
+ * NULL: not; positions is then not looked at).  q, q_out: [tokens][Hq][d] and k, k_out:
+ * [tokens][Hkv][d] bf16, a token's heads contiguous, strides in elements from one token to the next
+ * (>= heads * d, a multiple of 8; pointers 16-byte aligned); d in {64, 128}, rotary_dim <= d.  Hq or
+ * Hkv may be 0, and its pointers NULL.  An output may be its own input (same pointer and stride),
+ * and must not overlap an input otherwise.  positions: int32 on the device, of any sign and size.
+ * Computed in float32 and rounded once; cosines and sines are off by at most 2^-22 (times the
+ * amplitude), whatever the position.  A NaN or an infinity stays within its head (norm) or its pair. */
+fp_status fp_rotate(int32_t tokens, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                    const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                    const int32_t *positions, const fp_rope *rope, const fp_head_norm *norm,
+                    void *q_out, int64_t q_out_stride, void *k_out, int64_t k_out_stride,
+                    void *stream);
+
+/* fp_cache_write of keys that are normed and rotated on the way, and of values as they are; the
+ * queries of the same tokens are normed and rotated into q_out.  A token's position is its place in
+ * the slot, so row cu[i] + j of a slot of n tokens has position n - (cu[i+1] - cu[i]) + j.  As in
+ * fp_cache_write rows beyond a slot's length are left out (of q_out too), and nothing is done once
+ * a reserve, fork or truncate has failed or been left out.  q, q_out: rows [Hq][d] bf16, strides,
+ * alignment and overlap as in fp_rotate; q == NULL with Hq 0: keys and values alone.  rope and norm
+ * may be NULL.  Takes up to 2^24 / (Hkv + 8) pieces of 64 tokens. */
+fp_status fp_cache_append(const fp_cache *cache, int32_t layer, int32_t n, const int32_t *slots,
+                          const int32_t *cu, int32_t num_q_heads, const void *q, int64_t q_stride,
+                          const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                          const fp_rope *rope, const fp_head_norm *norm, void *q_out,
+                          int64_t q_out_stride, void *stream);
+
+/* One batch of fp_chunk_attn. */
+typedef struct fp_chunk {
+  int32_t batch;               /* sequences, 1..FP_MAX_CACHE_LIST                            */
+  const int32_t *slots;        /* HOST [batch]: the cache slot of a sequence, or -1: none    */
+  const int32_t *cu;           /* HOST [batch+1], cu[0] = 0, non-decreasing: rows of q and o */
+                               /* of a sequence, for its last cu[i+1] - cu[i] tokens, whose  */
+                               /* keys and values are in the cache                           */
+  int32_t num_q_heads;         /* Hq, a multiple of Hkv                                      */
+  float softmax_scale;         /* 0 => 1/sqrt(d)                                             */
+} fp_chunk;
+
+/* Device workspace bytes of fp_chunk_attn: partial results of key ranges.  Host only. */
+fp_status fp_chunk_workspace_size(const fp_cache *cache, const fp_chunk *batch, size_t *bytes);
+
+/* Causal attention of chunks of new tokens over their sequences: query t of m = cu[i+1] - cu[i] of a
+ * sequence of n tokens attends to its keys 0 .. n - m + t.  Rows, strides and alignment of q and o, rows
+ * without a key and what of the cache reaches a row are as in fp_decode_attn.  Slots may repeat.
+ * Scores, maxima, sums and O are float32; the weights that multiply the values are rounded to bf16, 2^-8,
+ * and the sum is that of the rounded weights.  The same call on the same state gives the same bits;
+ * where keys are cut into ranges follows from the lengths of the whole batch, so the last bits of a row
+ * depend on the rest of it. */
+fp_status fp_chunk_attn(const fp_cache *cache, const fp_chunk *batch, int32_t layer, const void *q,
+                        int64_t q_stride, void *o, void *ws, size_t ws_bytes, void *stream);
+
 /* Static description of a status code. */
 const char *fp_status_string(fp_status status);
 

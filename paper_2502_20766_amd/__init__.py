@@ -64,6 +64,30 @@ class FpDecode(ctypes.Structure):
                 ("prefix_lens", ctypes.c_void_p), ("softmax_scale", ctypes.c_float)]
 
 
+class FpRopeParams(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32),
+                ("scaling", ctypes.c_int32), ("base", ctypes.c_double),
+                ("factor", ctypes.c_double), ("original_len", ctypes.c_double),
+                ("low_turns", ctypes.c_double), ("high_turns", ctypes.c_double),
+                ("amplitude", ctypes.c_double), ("inv_freq", ctypes.c_void_p)]
+
+
+class FpRope(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32),
+                ("amplitude", ctypes.c_float), ("reserved", ctypes.c_int32),
+                ("step", ctypes.c_uint64 * 64)]
+
+
+class FpHeadNorm(ctypes.Structure):
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p),
+                ("weight_f32", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class FpChunk(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("slots", ctypes.c_void_p), ("cu", ctypes.c_void_p),
+                ("num_q_heads", ctypes.c_int32), ("softmax_scale", ctypes.c_float)]
+
+
 _lib_handle = None
 
 
@@ -98,6 +122,14 @@ def lib() -> ctypes.CDLL:
         h.fp_cache_compact.argtypes = [C, vp, ctypes.c_size_t, vp]
         h.fp_decode_workspace_size.argtypes = [C, D, sz]
         h.fp_decode_attn.argtypes = [C, D, i32, vp, i64, vp, vp, ctypes.c_size_t, vp]
+        h.fp_rope_init.argtypes = [ctypes.POINTER(FpRopeParams), ctypes.POINTER(FpRope)]
+        h.fp_rotate.argtypes = [i32, i32, i32, i32, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, i64,
+                                vp]
+        h.fp_cache_append.argtypes = [C, i32, i32, vp, vp, i32, vp, i64, vp, i64, vp, i64, vp, vp,
+                                      vp, i64, vp]
+        h.fp_chunk_workspace_size.argtypes = [C, ctypes.POINTER(FpChunk), sz]
+        h.fp_chunk_attn.argtypes = [C, ctypes.POINTER(FpChunk), i32, vp, i64, vp, vp,
+                                    ctypes.c_size_t, vp]
         h.fp_status_string.argtypes = [ctypes.c_int]
         h.fp_status_string.restype = ctypes.c_char_p
         h.fp_last_error.argtypes = []
@@ -107,7 +139,8 @@ def lib() -> ctypes.CDLL:
                      "fp_sparse_attn_noalloc", "fp_cache_meta_size", "fp_cache_workspace_size",
                      "fp_cache_init", "fp_cache_reserve", "fp_cache_write", "fp_cache_fork",
                      "fp_cache_truncate", "fp_cache_compact", "fp_decode_workspace_size",
-                     "fp_decode_attn"):
+                     "fp_decode_attn", "fp_rope_init", "fp_rotate", "fp_cache_append",
+                     "fp_chunk_workspace_size", "fp_chunk_attn"):
             getattr(h, name).restype = ctypes.c_int
         _lib_handle = h
     return _lib_handle
@@ -405,3 +438,5 @@ from .cache import (CACHE_FULL, CACHE_SHARED, CACHE_SKIPPED, CACHE_TOO_LONG,  # 
                     MAX_CACHE_LIST, MAX_QUERIES, Cache, CacheError, DecodeBatch, cache_compact,
                     cache_fork, cache_free, cache_init, cache_reserve, cache_truncate,
                     cache_workspace_size, cache_write, decode_attn, decode_workspace_size)
+from .chunk import ChunkBatch, cache_append, chunk_attn, chunk_workspace_size  # noqa: E402,F401
+from .rope import HeadNorm, Rope, rotate  # noqa: E402,F401

@@ -357,6 +357,111 @@ fp_status check_decode(const fp_cache *c, const fp_decode *b, DecodeDims *dm) {
   return FP_OK;
 }
 
+// The kernels' view of a rotation and of norms; either may be null.
+fp_status rope_args(const fp_rope *rope, const fp_head_norm *norm, int32_t d, fp::RopeArgs *r) {
+  memset(r, 0, sizeof(*r));
+  r->half = 1;
+  r->amplitude = 1.f;
+  if (rope) {
+    if (rope->rotary_dim < 16 || rope->rotary_dim > d || rope->rotary_dim % 16 ||
+        (rope->layout != FP_ROPE_HALF && rope->layout != FP_ROPE_INTERLEAVED) ||
+        !isfinite(rope->amplitude))
+      return FP_ERR_INVALID_ARG;
+    r->rotary = rope->rotary_dim;
+    r->half = rope->layout == FP_ROPE_HALF;
+    r->amplitude = rope->amplitude;
+    memcpy(r->step, rope->step, sizeof(r->step[0]) * (size_t)(rope->rotary_dim / 2));
+  }
+  if (norm) {
+    if (!(norm->eps >= 1.17549435e-38f) || !isfinite(norm->eps) ||
+        (norm->weight_f32 != 0 && norm->weight_f32 != 1) || !aligned16(norm->q_weight) ||
+        !aligned16(norm->k_weight))
+      return FP_ERR_INVALID_ARG;
+    r->normed = 1;
+    r->w_f32 = norm->weight_f32;
+    r->eps = norm->eps;
+    r->wq = norm->q_weight;
+    r->wk = norm->k_weight;
+  }
+  return FP_OK;
+}
+
+// Rows of `heads` heads that are read from x and written to y; no heads: not looked at.
+bool rows_ok(int32_t heads, int32_t d, const void *x, int64_t x_stride, const void *y,
+             int64_t y_stride) {
+  const int64_t row = (int64_t)heads * d;
+  return heads == 0 ||
+         (x && y && aligned16(x) && aligned16(y) && x_stride >= row && y_stride >= row &&
+          x_stride % 8 == 0 && y_stride % 8 == 0 && (x != y || x_stride == y_stride));
+}
+
+// The rows of a write: slots, first rows and 64-token blocks.
+fp_status write_args(const fp_cache *cache, int32_t layer, int32_t n, const int32_t *slots,
+                     const int32_t *cu, int64_t *blocks, fp::WriteArgs *a) {
+  SlotSet seen(cache);
+  const fp_status st = check_slots(cache, n, slots, &seen);
+  if (st != FP_OK) return st;
+  if (layer < 0 || layer >= cache->layers || !cu || cu[0] != 0) return FP_ERR_INVALID_ARG;
+  a->list.n = n;
+  *blocks = 0;
+  for (int i = 0; i < n; ++i) {
+    const int64_t m = (int64_t)cu[i + 1] - cu[i];
+    if (m < 0) return FP_ERR_INVALID_ARG;
+    a->list.slot[i] = slots[i];
+    a->list.num[i] = cu[i];
+    a->blk[i] = (int32_t)*blocks;
+    if (m > 0) *blocks += (m + 62) / 64 + 1;   // 64-token blocks that m tokens can touch
+  }
+  a->list.num[n] = cu[n];
+  a->blk[n] = (int32_t)*blocks;
+  a->layer = layer;
+  return FP_OK;
+}
+
+// Keys and values of a write of at least one row.
+fp_status write_rows(const fp_cache *cache, const void *k, int64_t k_stride, const void *v,
+                     int64_t v_stride, fp::WriteArgs *a) {
+  const int64_t row = (int64_t)cache->num_kv_heads * cache->head_dim;
+  if (!k || !v || !aligned16(k) || !aligned16(v) || k_stride < row || v_stride < row ||
+      k_stride % 8 || v_stride % 8)
+    return FP_ERR_INVALID_ARG;
+  a->k = (const uint16_t *)k;
+  a->v = (const uint16_t *)v;
+  a->k_stride = k_stride;
+  a->v_stride = v_stride;
+  return FP_OK;
+}
+
+// A batch of chunks: query heads per KV head, and the row tiles of the sequences.
+struct ChunkDims {
+  int G;
+  int32_t tile[FP_MAX_CACHE_LIST + 1];
+  size_t bytes;
+};
+
+fp_status check_chunk(const fp_cache *c, const fp_chunk *b, ChunkDims *dm) {
+  const fp_status st = check_cache(c, nullptr);
+  if (st != FP_OK) return st;
+  if (!b || !b->slots || !b->cu || b->batch < 1 || b->num_q_heads < 1) return FP_ERR_INVALID_ARG;
+  if (b->num_q_heads % c->num_kv_heads) return FP_ERR_INVALID_ARG;
+  if (b->batch > FP_MAX_CACHE_LIST || b->num_q_heads > 8192) return FP_ERR_UNSUPPORTED;
+  if (!scale_ok(b->softmax_scale) || b->cu[0] != 0) return FP_ERR_INVALID_ARG;
+  dm->G = b->num_q_heads / c->num_kv_heads;
+  int64_t tiles = 0;
+  for (int i = 0; i < b->batch; ++i) {
+    if (b->slots[i] < -1 || b->slots[i] >= c->num_slots || b->cu[i + 1] < b->cu[i])
+      return FP_ERR_INVALID_ARG;
+    const int64_t rows = ((int64_t)b->cu[i + 1] - b->cu[i]) * dm->G;
+    if (rows > 0x7FFFFF00) return FP_ERR_UNSUPPORTED;
+    dm->tile[i] = (int32_t)tiles;
+    tiles += (rows + fp::kChunkRows - 1) / fp::kChunkRows;
+    if (tiles * c->num_kv_heads >= (1 << 24)) return FP_ERR_UNSUPPORTED;   // grid size
+  }
+  dm->tile[b->batch] = (int32_t)tiles;
+  dm->bytes = kAlign;
+  return FP_OK;
+}
+
 fp_status hip_fail(hipError_t e, const char *what) {
   snprintf(g_last_error, sizeof(g_last_error), "%s: %s", what, hipGetErrorString(e));
   return FP_ERR_HIP;
@@ -584,33 +689,12 @@ fp_status fp_cache_write(const fp_cache *cache, int32_t layer, int32_t n, const 
   fp::CacheView c;
   fp_status st = check_cache(cache, &c);
   if (st != FP_OK) return st;
-  SlotSet seen(cache);
-  if ((st = check_slots(cache, n, slots, &seen)) != FP_OK) return st;
-  if (layer < 0 || layer >= cache->layers || !cu || cu[0] != 0) return FP_ERR_INVALID_ARG;
-  const int64_t row = (int64_t)cache->num_kv_heads * cache->head_dim;
   fp::WriteArgs a;
-  a.list.n = n;
-  int64_t blocks = 0;
-  for (int i = 0; i < n; ++i) {
-    const int64_t m = (int64_t)cu[i + 1] - cu[i];
-    if (m < 0) return FP_ERR_INVALID_ARG;
-    a.list.slot[i] = slots[i];
-    a.list.num[i] = cu[i];
-    a.blk[i] = (int32_t)blocks;
-    if (m > 0) blocks += (m + 62) / 64 + 1;   // 64-token blocks that m tokens can touch
-  }
+  int64_t blocks;
+  if ((st = write_args(cache, layer, n, slots, cu, &blocks, &a)) != FP_OK) return st;
   if (cu[n] == 0) return FP_OK;
-  if (!k || !v || !aligned16(k) || !aligned16(v) || k_stride < row || v_stride < row ||
-      k_stride % 8 || v_stride % 8)
-    return FP_ERR_INVALID_ARG;
+  if ((st = write_rows(cache, k, k_stride, v, v_stride, &a)) != FP_OK) return st;
   if (blocks * cache->num_kv_heads >= (1 << 24)) return FP_ERR_UNSUPPORTED;   // grid size
-  a.list.num[n] = cu[n];
-  a.blk[n] = (int32_t)blocks;
-  a.k = (const uint16_t *)k;
-  a.v = (const uint16_t *)v;
-  a.k_stride = k_stride;
-  a.v_stride = v_stride;
-  a.layer = layer;
   const hipError_t e = fp::launch_cache_write(c, a, (hipStream_t)stream);
   return e == hipSuccess ? FP_OK : hip_fail(e, "fp_cache_write");
 }
@@ -731,6 +815,157 @@ fp_status fp_decode_attn(const fp_cache *cache, const fp_decode *batch, int32_t 
   a.start[a.groups] = (int16_t)batch->batch;
   const hipError_t e = fp::launch_decode_attn(a, c.d, (hipStream_t)stream);
   return e == hipSuccess ? FP_OK : hip_fail(e, "fp_decode_attn");
+}
+
+fp_status fp_rope_init(const fp_rope_params *p, fp_rope *rope) {
+  if (!p || !rope) return FP_ERR_INVALID_ARG;
+  if (p->layout != FP_ROPE_HALF && p->layout != FP_ROPE_INTERLEAVED) return FP_ERR_INVALID_ARG;
+  const int32_t R = p->rotary_dim;
+  if (R < 2 || R % 2) return FP_ERR_INVALID_ARG;
+  if (R > 128 || R % 16) return FP_ERR_UNSUPPORTED;
+  if (!isfinite(p->amplitude) || p->amplitude < 0 || p->amplitude > 3.0e38) return FP_ERR_INVALID_ARG;
+  if (!p->inv_freq) {
+    if (!(p->base > 0) || !isfinite(p->base)) return FP_ERR_INVALID_ARG;
+    if (p->scaling < FP_ROPE_UNSCALED || p->scaling > FP_ROPE_PARTS) return FP_ERR_INVALID_ARG;
+    if (p->scaling != FP_ROPE_UNSCALED && (!(p->factor >= 1) || !isfinite(p->factor)))
+      return FP_ERR_INVALID_ARG;
+    if (p->scaling == FP_ROPE_PARTS &&
+        (!(p->original_len > 0) || !isfinite(p->original_len) || !(p->low_turns >= 0) ||
+         !(p->high_turns > p->low_turns) || !isfinite(p->high_turns)))
+      return FP_ERR_INVALID_ARG;
+  }
+  constexpr long double kTurn = 6.283185307179586476925286766559005768L;
+  const double base =
+      p->scaling == FP_ROPE_BASE ? p->base * pow(p->factor, (double)R / (R - 2)) : p->base;
+  fp_rope r;
+  memset(&r, 0, sizeof(r));
+  r.rotary_dim = R;
+  r.layout = p->layout;
+  r.amplitude = p->amplitude == 0 ? 1.f : (float)p->amplitude;
+  for (int i = 0; i < R / 2; ++i) {
+    double f = p->inv_freq ? p->inv_freq[i] : pow(base, -2.0 * i / R);
+    if (!p->inv_freq && p->scaling == FP_ROPE_LINEAR) f /= p->factor;
+    if (!p->inv_freq && p->scaling == FP_ROPE_PARTS) {
+      const double turns = p->original_len * f / (double)kTurn;
+      const double g =
+          std::min(std::max((turns - p->low_turns) / (p->high_turns - p->low_turns), 0.0), 1.0);
+      f = f * g + f / p->factor * (1 - g);
+    }
+    if (!(fabs(f) <= 1048576.0)) return FP_ERR_INVALID_ARG;
+    // the fraction of a turn, in 2^-64
+    long double turn = f / kTurn;
+    turn -= floorl(turn);
+    const long double scaled = rintl(turn * 18446744073709551616.0L);
+    r.step[i] = scaled >= 18446744073709551616.0L ? 0 : (uint64_t)scaled;
+  }
+  *rope = r;
+  return FP_OK;
+}
+
+fp_status fp_rotate(int32_t tokens, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                    const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                    const int32_t *positions, const fp_rope *rope, const fp_head_norm *norm,
+                    void *q_out, int64_t q_out_stride, void *k_out, int64_t k_out_stride,
+                    void *stream) {
+  if (tokens < 0 || num_q_heads < 0 || num_kv_heads < 0 || num_q_heads + (int64_t)num_kv_heads < 1)
+    return FP_ERR_INVALID_ARG;
+  if (head_dim != 64 && head_dim != 128) return FP_ERR_UNSUPPORTED;
+  if (num_q_heads > 8192 || num_kv_heads > 8192 || tokens > (1 << 25)) return FP_ERR_UNSUPPORTED;
+  fp::RotateArgs a;
+  const fp_status st = rope_args(rope, norm, head_dim, &a.rope);
+  if (st != FP_OK) return st;
+  if (tokens == 0) return FP_OK;
+  if (!rows_ok(num_q_heads, head_dim, q, q_stride, q_out, q_out_stride) ||
+      !rows_ok(num_kv_heads, head_dim, k, k_stride, k_out, k_out_stride))
+    return FP_ERR_INVALID_ARG;
+  if (rope && (!positions || !aligned4(positions))) return FP_ERR_INVALID_ARG;
+  a.q = (const uint16_t *)q;
+  a.k = (const uint16_t *)k;
+  a.qo = (uint16_t *)q_out;
+  a.ko = (uint16_t *)k_out;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.qo_stride = q_out_stride;
+  a.ko_stride = k_out_stride;
+  a.positions = rope ? positions : nullptr;
+  a.tokens = tokens;
+  a.hq = num_q_heads;
+  a.hkv = num_kv_heads;
+  const hipError_t e = fp::launch_rotate(a, head_dim, (hipStream_t)stream);
+  return e == hipSuccess ? FP_OK : hip_fail(e, "fp_rotate");
+}
+
+fp_status fp_cache_append(const fp_cache *cache, int32_t layer, int32_t n, const int32_t *slots,
+                          const int32_t *cu, int32_t num_q_heads, const void *q, int64_t q_stride,
+                          const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                          const fp_rope *rope, const fp_head_norm *norm, void *q_out,
+                          int64_t q_out_stride, void *stream) {
+  fp::CacheView c;
+  fp_status st = check_cache(cache, &c);
+  if (st != FP_OK) return st;
+  if (num_q_heads < 0) return FP_ERR_INVALID_ARG;
+  if (num_q_heads > 8192) return FP_ERR_UNSUPPORTED;
+  fp::AppendArgs a;
+  int64_t blocks;
+  if ((st = write_args(cache, layer, n, slots, cu, &blocks, &a.w)) != FP_OK) return st;
+  if ((st = rope_args(rope, norm, c.d, &a.rope)) != FP_OK) return st;
+  if (cu[n] == 0) return FP_OK;
+  if ((st = write_rows(cache, k, k_stride, v, v_stride, &a.w)) != FP_OK) return st;
+  if (!rows_ok(num_q_heads, c.d, q, q_stride, q_out, q_out_stride)) return FP_ERR_INVALID_ARG;
+  if (blocks * fp::append_parts(c, num_q_heads > 0) >= (1 << 24)) return FP_ERR_UNSUPPORTED;
+  a.hq = num_q_heads;
+  a.q = num_q_heads > 0 ? (const uint16_t *)q : nullptr;
+  a.qo = (uint16_t *)q_out;
+  a.q_stride = q_stride;
+  a.qo_stride = q_out_stride;
+  const hipError_t e = fp::launch_cache_append(c, a, (hipStream_t)stream);
+  return e == hipSuccess ? FP_OK : hip_fail(e, "fp_cache_append");
+}
+
+fp_status fp_chunk_workspace_size(const fp_cache *cache, const fp_chunk *batch, size_t *bytes) {
+  ChunkDims dm;
+  const fp_status st = check_chunk(cache, batch, &dm);
+  if (st != FP_OK) return st;
+  if (!bytes) return FP_ERR_INVALID_ARG;
+  *bytes = dm.bytes;
+  return FP_OK;
+}
+
+fp_status fp_chunk_attn(const fp_cache *cache, const fp_chunk *batch, int32_t layer, const void *q,
+                        int64_t q_stride, void *o, void *ws, size_t ws_bytes, void *stream) {
+  ChunkDims dm;
+  fp_status st = check_chunk(cache, batch, &dm);
+  if (st != FP_OK) return st;
+  fp::CacheView c;
+  if ((st = check_cache(cache, &c)) != FP_OK) return st;
+  if (layer < 0 || layer >= cache->layers) return FP_ERR_INVALID_ARG;
+  if (dm.tile[batch->batch] == 0) return FP_OK;      // no query
+  if (!q || !o || !ws || !aligned16(q) || !aligned16(o) || !aligned16(ws))
+    return FP_ERR_INVALID_ARG;
+  if (q_stride < (int64_t)batch->num_q_heads * c.d || q_stride % 8) return FP_ERR_INVALID_ARG;
+  if (ws_bytes < dm.bytes) return FP_ERR_WORKSPACE;
+  fp::ChunkArgs a;
+  const int64_t pool = (int64_t)layer * c.pages * c.hkv * c.page * c.d;
+  a.k = c.k + pool;
+  a.v = c.v + pool;
+  a.len = c.len;
+  a.table = c.table;
+  a.q = (const uint16_t *)q;
+  a.o = (uint16_t *)o;
+  a.q_stride = q_stride;
+  a.pages = c.pages;
+  a.hkv = c.hkv;
+  a.page_shift = c.page_shift;
+  a.max_pages = c.max_pages;
+  a.G = dm.G;
+  a.hq = batch->num_q_heads;
+  a.batch = batch->batch;
+  a.scale_log2 = resolved_scale(batch->softmax_scale, c.d) * 1.4426950408889634f;
+  memcpy(a.slot, batch->slots, sizeof(int32_t) * (size_t)batch->batch);
+  memcpy(a.cu, batch->cu, sizeof(int32_t) * (size_t)(batch->batch + 1));
+  memcpy(a.tile, dm.tile, sizeof(int32_t) * (size_t)(batch->batch + 1));
+  const hipError_t e = fp::launch_chunk_attn(a, c.d, (hipStream_t)stream);
+  return e == hipSuccess ? FP_OK : hip_fail(e, "fp_chunk_attn");
 }
 
 const char *fp_status_string(fp_status status) {

@@ -5,7 +5,7 @@
 // and can be captured into a graph.  Free pages are a bitmap beside the reference counts: pages
 // are taken lowest number first by counting bits, and given back by clearing them, in any order
 // with the same result, so no list has to be kept in order.
-#include "fp_internal.h"
+#include "fp_cache_dev.h"
 
 namespace fp {
 namespace {
@@ -13,10 +13,6 @@ namespace {
 constexpr int kPlanThreads = 1024;   // the single workgroup that hands out pages
 constexpr int kCopyUnits = 1024;     // 16-byte units of a page copied by one workgroup at a time
 constexpr int kCopyGrid = 2048;      // workgroups of a copy whose length the host cannot know
-
-// 16 bytes as a vector: arrays of a struct of four words were kept in scratch memory, which
-// cost a short copy 13 us.
-typedef uint32_t Unit __attribute__((ext_vector_type(4)));
 
 // Exclusive prefix sum over the workgroup (kPlanThreads threads) and the total; `part` is an
 // int of LDS per wave.
@@ -300,19 +296,7 @@ __global__ __launch_bounds__(256) void cache_write(CacheView c, WriteArgs a) {
     kx[i] = __builtin_nontemporal_load((const Unit *)(a.k + row * a.k_stride + h * D + ch * 8));
     vx[i] = __builtin_nontemporal_load((const Unit *)(a.v + row * a.v_stride + h * D + ch * 8));
   }
-  // pages of the four 16-token steps, or -1 for one that is not this slot's alone
-  if (tid < 4) {
-    const int t = p0 + 16 * tid;
-    int p = -1;
-    if (t < end && t + 16 > lo) {
-      p = c.table[(int64_t)slot * c.max_pages + (t >> c.page_shift)];
-      if ((unsigned)p >= (unsigned)c.pages || c.ref[p] != 1) {
-        p = -1;
-        atomicOr(c.state + 1, FP_CACHE_SHARED);
-      }
-    }
-    s_page[tid] = p;
-  }
+  if (tid < 4) s_page[tid] = step_page(c, slot, p0 + 16 * tid, lo, end);
 #pragma unroll
   for (int i = 0; i < 64 * CPR / 256; ++i) {
     const int u = tid + 256 * i, r = u / CPR, ch = u % CPR, t = p0 + r;
@@ -325,25 +309,7 @@ __global__ __launch_bounds__(256) void cache_write(CacheView c, WriteArgs a) {
     if (t < lo || t >= end || p < 0) continue;
     __builtin_nontemporal_store(kx[i], (Unit *)(c.k + tile_of(p, t) + (t & 15) * D + ch * 8));
   }
-  for (int u = tid; u < 8 * D; u += 256) {   // 8 half steps x D
-    const int half = u & 1, d = (u >> 1) % D, step = (u >> 1) / D;
-    const int r = 16 * step + 8 * half, t = p0 + r;
-    if (t + 8 <= lo || t >= end) continue;
-    const int p = s_page[step];
-    if (p < 0) continue;
-    uint16_t *to = c.v + tile_of(p, t) + d * 16 + 8 * half;
-    if (t >= lo && t + 8 <= end) {
-      Unit x;
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        x[j] = tile[r + 2 * j][d] | (uint32_t)tile[r + 2 * j + 1][d] << 16;
-      __builtin_nontemporal_store(x, (Unit *)to);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (t + j >= lo && t + j < end) to[j] = tile[r + j][d];
-    }
-  }
+  write_values<D>(c, tile, s_page, p0, lo, end, tile_of);
 }
 
 // ---- fork: a thread takes one place of the tables of kBatch sources to their copies.  A source

@@ -23,16 +23,13 @@
 
 #include "fp_attn_dev.h"
 #include "fp_internal.h"
+#include "fp_paged_dev.h"
 
 namespace fp {
 namespace {
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-
-constexpr int kKeys = 64;                 // keys per tile
 constexpr int kThreads = 256;
 constexpr int kMaxList = FP_MAX_CACHE_LIST;
-constexpr float kLazy = 8.f;              // rise (log2 units) that moves a row's reference
 // Places of the line, beside its tiles, that a segment takes: starting and ending a piece costs
 // a workgroup about as much as this many tiles.  At 1, 2, 3, 4: 64 sequences of 3 to 32000 tokens
 // 90.2, 86.8, 87.4, 88.2 us; 16 samples of 32k 41.2, 40.0, 40.6, 41.0; 256 samples of 128k 588, 574,
@@ -373,103 +370,6 @@ __device__ __forceinline__ Piece piece_at(const DecodeArgs &a, const Plan &p, in
   return r;
 }
 
-template <int D>
-struct DecGeo {
-  static constexpr int OCC = D == 64 ? 3 : 2;      // workgroups per CU = waves per SIMD
-  static constexpr int RB = 2 * D;                 // bytes per key row
-  static constexpr int STEP = 16 * RB;             // bytes of 16 keys, of K or of V
-  static constexpr int DMA = STEP / 1024;          // 1 KB copies of them
-  static constexpr int CPR = RB / 16;              // 16-byte chunks per key row
-  static constexpr int RPI = 1024 / RB;            // key rows per copy
-};
-
-// A wave's 16 keys of a tile, which always lie in one page, brought into LDS by DMA: K
-// row-major with 16-byte chunks swizzled as in the prefill, V^T in the fragment order of
-// vt_unit.
-template <int D>
-struct Loader {
-  using S = DecGeo<D>;
-  uint32_t koff[S::DMA], voff;
-  int w;
-  __device__ __forceinline__ Loader(int w, int lane) : w(w) {
-#pragma unroll
-    for (int i = 0; i < S::DMA; ++i) {
-      const int r = i * S::RPI + lane / S::CPR;
-      koff[i] = r * S::RB + swz_k<D>(lane % S::CPR, r) * 16 - i * 1024;
-    }
-    const int d = 8 * (lane >> 4) + (lane & 7), half = ((lane >> 3) ^ (lane >> 4)) & 1;
-    voff = (2 * d + half) * 16;
-  }
-  // Table entry of the keys of tile t; loaded a tile ahead and first looked at in `issue`, so
-  // that nothing waits for it.
-  __device__ __forceinline__ int page(const DecodeArgs &a, const Piece &r, int t) const {
-    const int key = min(r.key0 + kKeys * t + 16 * w, r.limit - 1);
-    return a.table[(int64_t)r.row * a.max_pages + (key >> a.page_shift)];
-  }
-  __device__ __forceinline__ void issue(const DecodeArgs &a, const Piece &r, int t, int pg,
-                                        uint8_t *k, uint8_t *v) const {
-    const int key = r.key0 + kKeys * t + 16 * w;
-    if (key >= r.limit) return;           // past the segment: those keys are masked
-    pg = min(max(__builtin_amdgcn_readfirstlane(pg), 0), a.pages - 1);
-    const int64_t off = ((((int64_t)pg * a.hkv + r.head) << a.page_shift) +
-                         (key & ((1 << a.page_shift) - 1))) * D;
-    const auto ks = uniform_rsrc(a.k + off, S::STEP), vs = uniform_rsrc(a.v + off, S::STEP);
-    const auto kd = (__attribute__((address_space(3))) void *)k;
-    const auto vd = (__attribute__((address_space(3))) void *)v;
-    // Keys that are read once pass the caches by: 64 sequences of 3 to 32000 tokens 98.5 -> 87.3
-    // us, 16 samples of 32k 43.8 -> 40.9, drafts at head dim 64 53.8 -> 48.8, and 130 -> 88, 58 ->
-    // 44, 68 -> 52 after a call that left the caches full of its own writes.  For prefixes of
-    // several row tiles 560 -> 582 (256 samples of 128k).
-    if (r.once) {
-      dma_slots<0, S::DMA, 2>(ks, kd, koff);
-      dma_slots<0, S::DMA, 2>(vs, vd, voff);
-    } else {
-      dma_slots<0, S::DMA>(ks, kd, koff);
-      dma_slots<0, S::DMA>(vs, vd, voff);
-    }
-  }
-};
-
-// 16 keys of V^T in LDS, of which some row does not see all.  Values past the segment may hold
-// anything, NaN among it, which a weight of zero would not cancel: they become zero.  So do
-// infinities and NaN of tokens that only later queries see; returns whether there were any, and
-// the rows that see them then take them separately.
-template <int D>
-__device__ __forceinline__ bool settle(uint8_t *v, int key0, int limit, int vis, int lane) {
-  bool odd = false;
-  for (int i = 0; i < 2 * D / 64; ++i) {
-    const int u = 64 * i + lane;          // unit (d, half), see Loader::voff
-    const int key = key0 + 8 * (((u >> 3) ^ (u >> 4)) & 1);
-    s16x8 x = *reinterpret_cast<const s16x8 *>(v + 16 * u);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const bool out = key + e >= limit;
-      const bool late = key + e >= vis && (x[e] & 0x7F80) == 0x7F80;
-      odd |= late && !out;
-      if (out || late) x[e] = 0;
-    }
-    *reinterpret_cast<s16x8 *>(v + 16 * u) = x;
-  }
-  return __ballot(odd) != 0;
-}
-
-// Waits for this wave's copies into LDS (and its other loads and stores).  The builtin, unlike
-// the same instruction in an asm statement, also tells the compiler, which would else wait for
-// them where their LDS is first read, after the next copies have been issued, and so for those
-// too.
-__device__ __forceinline__ void wait_copies() {
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0x0F70);     // vmcnt(0)
-  asm volatile("" ::: "memory");
-}
-
-// Workgroup barrier that orders LDS accesses only: it waits for no copy and no store in flight.
-__device__ __forceinline__ void wg_barrier() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-  __builtin_amdgcn_s_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-}
-
 // A weight as the sum of two bf16 numbers, both above zero if it is: both multiply the same value,
 // and an infinite one would meet a zero or the other sign in a second number that is what rounding
 // the first one left.  So the first is the largest bf16 number below the weight; the second, up to
@@ -507,7 +407,7 @@ template <int D, int RT>
 __device__ __forceinline__ void lean_pieces(const DecodeArgs &a, const Plan &plan, uint8_t *lds0,
                                             uint8_t *lds1, float2 (*s_ml)[16],
                                             const Part &part) {
-  using S = DecGeo<D>;
+  using S = PagedGeo<D>;
   constexpr int KS = D / 32, DB = D / 16;
   // K and V of wave w's even (0) or odd steps; at the end of a piece the last one holds the
   // wave's O (16 x D floats)
@@ -741,7 +641,7 @@ __device__ __forceinline__ void lean_pieces(const DecodeArgs &a, const Plan &pla
 template <int D>
 __device__ __forceinline__ void many_pieces(const DecodeArgs &a, const Plan &plan, uint8_t *lds0,
                                             uint8_t *lds1, const Part &part) {
-  using S = DecGeo<D>;
+  using S = PagedGeo<D>;
   constexpr int KS = D / 16, DB = D / 32, TILE = 4 * S::STEP;
   // K and V of even tiles in lds0, of odd ones in lds1
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
@@ -893,12 +793,12 @@ __device__ __forceinline__ void many_pieces(const DecodeArgs &a, const Plan &pla
 // RT: row tiles of 16 of a piece with few rows.  MANY: the batch may have prefixes with many.
 template <int D, int RT, bool MANY>
 __global__ __launch_bounds__(kThreads)
-__attribute__((amdgpu_waves_per_eu(DecGeo<D>::OCC, DecGeo<D>::OCC)))
+__attribute__((amdgpu_waves_per_eu(PagedGeo<D>::OCC, PagedGeo<D>::OCC)))
 void decode_fwd(DecodeArgs a) {
   // two arrays, so that the compiler sees that reads of one do not wait for copies into the
   // other
-  __shared__ __attribute__((aligned(1024))) uint8_t lds0[8 * DecGeo<D>::STEP];
-  __shared__ __attribute__((aligned(1024))) uint8_t lds1[8 * DecGeo<D>::STEP];
+  __shared__ __attribute__((aligned(1024))) uint8_t lds0[8 * PagedGeo<D>::STEP];
+  __shared__ __attribute__((aligned(1024))) uint8_t lds1[8 * PagedGeo<D>::STEP];
   __shared__ Plan plan;
   __shared__ float2 s_ml[4][16];
   const Part part = make_plan(a, plan);

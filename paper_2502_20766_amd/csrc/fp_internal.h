@@ -179,6 +179,35 @@ struct ForkArgs {
   int32_t src[FP_MAX_CACHE_LIST], dst[FP_MAX_CACHE_LIST];
 };
 
+// fp_rope and fp_head_norm as the kernels see them.
+struct RopeArgs {
+  int32_t rotary;              // elements that are rotated; 0: none
+  int32_t half;                // pairs (i, i + rotary / 2), else (2 i, 2 i + 1)
+  int32_t normed, w_f32;       // heads are normed; the weights' type
+  float amplitude, eps;
+  const void *wq, *wk;         // weights [d], or null: 1
+  uint64_t step[64];           // per pair: turns per position, times 2^64
+};
+
+struct RotateArgs {
+  const uint16_t *q, *k;
+  uint16_t *qo, *ko;
+  int64_t q_stride, k_stride, qo_stride, ko_stride;
+  const int32_t *positions;
+  int32_t tokens, hq, hkv;
+  int32_t groups;              // set by the launcher: waves that share the heads of a token
+  RopeArgs rope;
+};
+
+struct AppendArgs {
+  WriteArgs w;
+  const uint16_t *q;           // or null
+  uint16_t *qo;
+  int64_t q_stride, qo_stride;
+  int32_t hq;
+  RopeArgs rope;
+};
+
 // What the joining launch of decode_attn knows of the call's plan (workspace).
 struct DecodeJoin {
   int4 seq[FP_MAX_CACHE_LIST];     // per sequence: tokens, keys of the prefix, places of its own
@@ -211,6 +240,23 @@ struct DecodeArgs {
   uint8_t group[FP_MAX_CACHE_LIST];        // per sequence
 };
 
+struct ChunkArgs {
+  const uint16_t *k, *v;       // pools of the layer
+  const int32_t *len, *table;
+  const uint16_t *q;
+  uint16_t *o;
+  int64_t q_stride;
+  int32_t pages, hkv, page_shift, max_pages;
+  int32_t G, hq, batch;
+  float scale_log2;            // softmax scale * log2(e)
+  int32_t slot[FP_MAX_CACHE_LIST];
+  int32_t cu[FP_MAX_CACHE_LIST + 1];
+  int32_t tile[FP_MAX_CACHE_LIST + 1];     // prefix sums of the row tiles of a sequence and KV head
+};
+
+// Query rows of a row tile of chunk_attn: 4 waves of 32.
+constexpr int kChunkRows = 128;
+
 // Query rows of one unit of work on prefixes with many rows: 4 waves of 32.
 constexpr int kDecodeRows = 128;
 // Rows up to which a prefix is read like a sequence's own keys, in tiles of 16 or 32 rows.  Two such
@@ -237,5 +283,10 @@ hipError_t launch_cache_fork(const CacheView &c, const ForkArgs &a, hipStream_t 
 hipError_t launch_cache_truncate(const CacheView &c, const CacheList &l, hipStream_t s);
 hipError_t launch_cache_compact(const CacheView &c, const PageCopies &w, hipStream_t s);
 hipError_t launch_decode_attn(const DecodeArgs &a, int d, hipStream_t s);
+hipError_t launch_chunk_attn(const ChunkArgs &a, int d, hipStream_t s);
+hipError_t launch_rotate(const RotateArgs &a, int d, hipStream_t s);
+hipError_t launch_cache_append(const CacheView &c, const AppendArgs &a, hipStream_t s);
+// Workgroups of launch_cache_append per 64 positions of a slot.
+int append_parts(const CacheView &c, bool queries);
 
 }  // namespace fp
