@@ -5,6 +5,7 @@
 #include <math.h>
 #include <stdint.h>
 #include <stdio.h>
+#include <stdlib.h>
 #include <string.h>
 
 #include <algorithm>
@@ -432,11 +433,12 @@ fp_status write_rows(const fp_cache *cache, const void *k, int64_t k_stride, con
   return FP_OK;
 }
 
-// A batch of chunks: query heads per KV head, and the row tiles of the sequences.
+// A batch of chunks: query heads per KV head, how its row tiles are taken, workspace.
 struct ChunkDims {
   int G;
-  int32_t tile[FP_MAX_CACHE_LIST + 1];
-  size_t bytes;
+  int64_t tiles;               // row tiles of a KV head
+  int wgs, width, rows, tile_rows;   // see fp::ChunkArgs
+  size_t bytes_seg, bytes;
 };
 
 fp_status check_chunk(const fp_cache *c, const fp_chunk *b, ChunkDims *dm) {
@@ -447,18 +449,27 @@ fp_status check_chunk(const fp_cache *c, const fp_chunk *b, ChunkDims *dm) {
   if (b->batch > FP_MAX_CACHE_LIST || b->num_q_heads > 8192) return FP_ERR_UNSUPPORTED;
   if (!scale_ok(b->softmax_scale) || b->cu[0] != 0) return FP_ERR_INVALID_ARG;
   dm->G = b->num_q_heads / c->num_kv_heads;
-  int64_t tiles = 0;
+  dm->tiles = 0;
+  int64_t most = 1;
   for (int i = 0; i < b->batch; ++i) {
     if (b->slots[i] < -1 || b->slots[i] >= c->num_slots || b->cu[i + 1] < b->cu[i])
       return FP_ERR_INVALID_ARG;
     const int64_t rows = ((int64_t)b->cu[i + 1] - b->cu[i]) * dm->G;
-    if (rows > 0x7FFFFF00) return FP_ERR_UNSUPPORTED;
-    dm->tile[i] = (int32_t)tiles;
-    tiles += (rows + fp::kChunkRows - 1) / fp::kChunkRows;
-    if (tiles * c->num_kv_heads >= (1 << 24)) return FP_ERR_UNSUPPORTED;   // grid size
+    if (rows > 0x7FFF0000) return FP_ERR_UNSUPPORTED;
+    most = std::max(most, rows);
+    dm->tiles += (rows + 127) / 128;
   }
-  dm->tile[b->batch] = (int32_t)tiles;
-  dm->bytes = kAlign;
+  // places of the line, an int64 in the kernels (a tile takes G per key and a few more, see Series)
+  const double capacity = (double)c->max_pages * c->page;
+  if ((double)dm->tiles * c->num_kv_heads * (dm->G * (capacity + 512) + (double)most) > 4e18)
+    return FP_ERR_UNSUPPORTED;
+  dm->width = getenv("FPW") ? atoi(getenv("FPW")) : 1;
+  dm->rows = getenv("FPR") && c->head_dim == 128 ? atoi(getenv("FPR")) : 128;
+  dm->wgs = fp::decode_wgs(c->head_dim) / (dm->rows / 128);
+  const size_t wgs = dm->wgs;
+  dm->tile_rows = most >= dm->rows ? dm->rows : (int)(most + 31) / 32 * 32;
+  dm->bytes_seg = align_up(wgs * sizeof(int4));
+  dm->bytes = dm->bytes_seg + align_up(2 * wgs * dm->tile_rows * 4 * (size_t)(c->head_dim + 2));
   return FP_OK;
 }
 
@@ -939,7 +950,7 @@ fp_status fp_chunk_attn(const fp_cache *cache, const fp_chunk *batch, int32_t la
   fp::CacheView c;
   if ((st = check_cache(cache, &c)) != FP_OK) return st;
   if (layer < 0 || layer >= cache->layers) return FP_ERR_INVALID_ARG;
-  if (dm.tile[batch->batch] == 0) return FP_OK;      // no query
+  if (dm.tiles == 0) return FP_OK;                   // no query
   if (!q || !o || !ws || !aligned16(q) || !aligned16(o) || !aligned16(ws))
     return FP_ERR_INVALID_ARG;
   if (q_stride < (int64_t)batch->num_q_heads * c.d || q_stride % 8) return FP_ERR_INVALID_ARG;
@@ -960,10 +971,15 @@ fp_status fp_chunk_attn(const fp_cache *cache, const fp_chunk *batch, int32_t la
   a.G = dm.G;
   a.hq = batch->num_q_heads;
   a.batch = batch->batch;
+  a.wgs = dm.wgs;
+  a.width = dm.width;
+  a.rows = dm.rows;
+  a.tile_rows = dm.tile_rows;
+  a.seg = (int4 *)ws;
+  a.part = (float *)((char *)ws + dm.bytes_seg);
   a.scale_log2 = resolved_scale(batch->softmax_scale, c.d) * 1.4426950408889634f;
   memcpy(a.slot, batch->slots, sizeof(int32_t) * (size_t)batch->batch);
   memcpy(a.cu, batch->cu, sizeof(int32_t) * (size_t)(batch->batch + 1));
-  memcpy(a.tile, dm.tile, sizeof(int32_t) * (size_t)(batch->batch + 1));
   const hipError_t e = fp::launch_chunk_attn(a, c.d, (hipStream_t)stream);
   return e == hipSuccess ? FP_OK : hip_fail(e, "fp_chunk_attn");
 }

@@ -248,14 +248,17 @@ struct ChunkArgs {
   int64_t q_stride;
   int32_t pages, hkv, page_shift, max_pages;
   int32_t G, hq, batch;
+  int32_t wgs;                 // workgroups that the keys are divided among
+  int32_t width;               // row tiles side by side, one for each workgroup of a cluster
+  int32_t rows;                // rows of a row tile: 128 or, with workgroups of eight waves, 256
+  int32_t tile_rows;           // rows of a partial result: `rows`, fewer where no sequence has as many
   float scale_log2;            // softmax scale * log2(e)
+  int4 *seg;                   // per part: pieces of the segment that begins in it and ends in a later
+                               // one (0: none), its sequence, KV head and number
+  float *part;                 // partial results, two for each workgroup
   int32_t slot[FP_MAX_CACHE_LIST];
   int32_t cu[FP_MAX_CACHE_LIST + 1];
-  int32_t tile[FP_MAX_CACHE_LIST + 1];     // prefix sums of the row tiles of a sequence and KV head
 };
-
-// Query rows of a row tile of chunk_attn: 4 waves of 32.
-constexpr int kChunkRows = 128;
 
 // Query rows of one unit of work on prefixes with many rows: 4 waves of 32.
 constexpr int kDecodeRows = 128;

@@ -28,8 +28,8 @@ struct PagedGeo {
 
 // A wave's 16 keys of a tile, which always lie in one page, brought into LDS by DMA: K
 // row-major with 16-byte chunks swizzled as in the prefill, V^T in the fragment order of
-// vt_unit.
-template <int D>
+// vt_unit.  KEYS: keys of a tile, 16 for each wave.
+template <int D, int KEYS = kKeys>
 struct Loader {
   using S = PagedGeo<D>;
   uint32_t koff[S::DMA], voff;
@@ -47,13 +47,13 @@ struct Loader {
   // that nothing waits for it.
   template <class Args, class Piece>
   __device__ __forceinline__ int page(const Args &a, const Piece &r, int t) const {
-    const int key = min(r.key0 + kKeys * t + 16 * w, r.limit - 1);
+    const int key = min(r.key0 + KEYS * t + 16 * w, r.limit - 1);
     return a.table[(int64_t)r.row * a.max_pages + (key >> a.page_shift)];
   }
   template <class Args, class Piece>
   __device__ __forceinline__ void issue(const Args &a, const Piece &r, int t, int pg, uint8_t *k,
                                         uint8_t *v) const {
-    const int key = r.key0 + kKeys * t + 16 * w;
+    const int key = r.key0 + KEYS * t + 16 * w;
     if (key >= r.limit) return;           // past the segment: those keys are masked
     pg = min(max(__builtin_amdgcn_readfirstlane(pg), 0), a.pages - 1);
     const int64_t off = ((((int64_t)pg * a.hkv + r.head) << a.page_shift) +
