@@ -5,7 +5,6 @@
 #include <math.h>
 #include <stdint.h>
 #include <stdio.h>
-#include <stdlib.h>
 #include <string.h>
 
 #include <algorithm>
@@ -463,8 +462,18 @@ fp_status check_chunk(const fp_cache *c, const fp_chunk *b, ChunkDims *dm) {
   const double capacity = (double)c->max_pages * c->page;
   if ((double)dm->tiles * c->num_kv_heads * (dm->G * (capacity + 512) + (double)most) > 4e18)
     return FP_ERR_UNSUPPORTED;
-  dm->width = getenv("FPW") ? atoi(getenv("FPW")) : 1;
-  dm->rows = getenv("FPR") && c->head_dim == 128 ? atoi(getenv("FPR")) : 128;
+  // Eight waves where that leaves few rows of a tile empty, and clusters of as many row tiles as do.
+  const int64_t tiles_128 = dm->tiles;
+  auto tiles_of = [&](int64_t span) {        // row tiles of 128 that tiles of `span` rows take up
+    int64_t n = 0;
+    for (int i = 0; i < b->batch; ++i)
+      n += (((int64_t)b->cu[i + 1] - b->cu[i]) * dm->G + span - 1) / span;
+    return n * (span / 128);
+  };
+  dm->rows = c->head_dim == 128 && 16 * tiles_of(256) <= 17 * tiles_128 ? 256 : 128;
+  dm->width = 8;
+  while (dm->width > 1 && 16 * tiles_of((int64_t)dm->rows * dm->width) > 17 * tiles_of(dm->rows))
+    --dm->width;
   dm->wgs = fp::decode_wgs(c->head_dim) / (dm->rows / 128);
   const size_t wgs = dm->wgs;
   dm->tile_rows = most >= dm->rows ? dm->rows : (int)(most + 31) / 32 * 32;

@@ -258,9 +258,9 @@ void chunk_fwd(ChunkArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds0[2 * TILE];
   __shared__ __attribute__((aligned(1024))) uint8_t lds1[2 * TILE];
   __shared__ Plan plan;
-  // the piece at hand and the next one, each wave's own: in registers they would take as many scalar
-  // ones as there are
-  __shared__ Piece s_piece[WAVES][2];
+  // the piece at hand, each wave's own copy: what is looked at after its tiles would else take scalar
+  // registers meanwhile
+  __shared__ Piece s_piece[WAVES];
   __shared__ int s_odd[2];                // piece with late values that are not finite, by its parity
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int lr = lane & 31, lh = lane >> 5;
@@ -275,31 +275,39 @@ void chunk_fwd(ChunkArgs a) {
     return;
   }
   const Loader<D, G::KEYS> load(w, lane);
-  auto issue = [&](const Source &r, int t, int pg, uint8_t *into) {
-    uint8_t *k = into + w * S::STEP;
-    load.issue(a, r, t, pg, k, k + TILE);
-  };
   const int kr = (lr & ~12) | ((lr >> 1) & 4) | ((lr << 1) & 8);
   uint32_t kaddr[KS];
 #pragma unroll
   for (int k = 0; k < KS; ++k) kaddr[k] = kr * S::RB + swz_k<D>(2 * k + lh, kr) * 16;
   const uint32_t vaddr = TILE + 16 * vt_unit(lr, lh);
-  auto uniform_source = [&](const Source &r) {
-    return Source{uniform(r.row), uniform(r.head), 0, uniform(r.limit), uniform(r.once)};
-  };
-
-  s_piece[w][0] = piece_at<G>(a, plan, plan.first, part.lo, part);
-  int which = 0, odd = 0, page_next = 0, worked = 1;
-  bool loading = false;                   // the piece's first tile is on its way
+  int e = plan.first, worked = 1;
+  int64_t x = part.lo;
   while (true) {
+    s_piece[w] = piece_at<G>(a, plan, e, x, part);
     asm volatile("" ::: "memory");
-    const Piece &me = s_piece[w][which], &nxt = s_piece[w][which ^ 1];
-    const Source src = uniform_source(me.src);
+    const Piece &me = s_piece[w];
+    const Source src = {uniform(me.src.row), uniform(me.src.head), 0, uniform(me.src.limit),
+                        uniform(me.src.once)};
     const int t0 = uniform(me.t0), t1 = uniform(me.t1);
-    if (!loading && t0 < t1) {
-      wg_barrier();                       // (other waves may still read the tile before)
-      issue(src, t0, load.page(a, src, t0), odd ? lds1 : lds0);
-      page_next = load.page(a, src, min(t0 + 1, t1 - 1));
+    const int32_t *table = a.table + (int64_t)src.row * a.max_pages;
+    const int64_t in_page = ((int64_t)src.head << a.page_shift) * D;
+    const int64_t page_size = ((int64_t)a.hkv << a.page_shift) * D;
+    // this wave's 16 keys of tile t: the table's entry, a tile ahead, and their copies
+    auto page = [&](int t) {
+      return table[min(G::KEYS * t + 16 * w, src.limit - 1) >> a.page_shift];
+    };
+    auto issue = [&](int t, int pg, uint8_t *into) {
+      const int key = G::KEYS * t + 16 * w;
+      if (key >= src.limit) return;       // past the sequence: those keys are masked
+      pg = min(max(uniform(pg), 0), a.pages - 1);
+      load.copy(a.k, a.v, pg * page_size + in_page + (key & ((1 << a.page_shift) - 1)) * D, src.once,
+                into + w * S::STEP, into + w * S::STEP + TILE);
+    };
+    int page_next = 0;
+    if (t0 < t1) {
+      wg_barrier();                       // (other waves may still read the last piece's tiles)
+      issue(t0, page(t0), lds0);
+      page_next = page(min(t0 + 1, t1 - 1));
     }
     const int row0 = uniform(me.row0), seq = uniform(me.seq), vis = uniform(me.vis);
     const bool active = 32 * w < uniform(me.rows);
@@ -322,15 +330,6 @@ void chunk_fwd(ChunkArgs a) {
 #pragma unroll
     for (int i = 0; i < DB; ++i) oacc[i] = f32x16{};
     float m_ref = -INFINITY, mc = 0.f, m_trig = -INFINITY, l_run = 0.f;
-    loading = false;
-    const int64_t end = uniform(me.end);
-    const bool more = end < part.hi;
-    if (more) {
-      const Piece p = piece_at<G>(a, plan, seq, end, part);
-      loading = p.t0 < p.t1 && t0 < t1;
-      s_piece[w][which ^ 1] = p;
-      asm volatile("" ::: "memory");
-    }
 
     auto step = [&](uint8_t *tile, uint8_t *next, const int t) {
       const int k0 = G::KEYS * t;
@@ -341,38 +340,40 @@ void chunk_fwd(ChunkArgs a) {
         s_odd[worked & 1] = worked;
       wg_barrier();                                    // ... and every wave's
       if (t + 1 < t1) {
-        issue(src, t + 1, page_next, next);
-        page_next = load.page(a, src, min(t + 2, t1 - 1));
-      } else if (loading) {
-        const Source to = uniform_source(nxt.src);
-        const int n0 = uniform(nxt.t0), n1 = uniform(nxt.t1);
-        issue(to, n0, load.page(a, to, n0), next);
-        page_next = load.page(a, to, min(n0 + 1, n1 - 1));
+        issue(t + 1, page_next, next);
+        page_next = page(min(t + 2, t1 - 1));
       }
       if (!active) return;
 #pragma unroll
       for (int sub = 0; sub < G::KEYS / kKeys; ++sub) {
         const int ks = k0 + kKeys * sub;
         if (ks >= lim_all) return;
-        f32x16 sacc[2];
+        f32x16 sacc[2] = {f32x16{}, f32x16{}};
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          bf16x8 kf[KS];
+        for (int k = 0; k < KS; ++k) {
+          bf16x8 kf[2];
 #pragma unroll
-          for (int k = 0; k < KS; ++k)
-            kf[k] = *reinterpret_cast<const bf16x8 *>(tile + kaddr[k] + (2 * sub + i) * 32 * S::RB);
-          sacc[i] = f32x16{};
+          for (int i = 0; i < 2; ++i)
+            kf[i] = *reinterpret_cast<const bf16x8 *>(tile + kaddr[k] + (2 * sub + i) * 32 * S::RB);
 #pragma unroll
-          for (int k = 0; k < KS; ++k)
-            sacc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k], qf[k], sacc[i], 0, 0, 0);
+          for (int i = 0; i < 2; ++i)
+            sacc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], qf[k], sacc[i], 0, 0, 0);
         }
+        __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+        for (int i = 0; i < 2 * KS - 6; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x8, 6, 0);
         if (ks + kKeys > lim_w) {
-          const int room = lim - ks - 8 * lh;
+          // (the least of a score and + or - infinity: comparisons would take scalar registers)
+          const float room = (float)(lim - ks - 8 * lh) - 0.5f;
 #pragma unroll
           for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int v = 0; v < 16; ++v)
-              if (32 * i + 16 * (v >> 3) + (v & 7) >= room) sacc[i][v] = -INFINITY;
+              sacc[i][v] = fminf(sacc[i][v], (room - (32 * i + 16 * (v >> 3) + (v & 7))) * INFINITY);
         }
         float mt = -INFINITY;
 #pragma unroll
@@ -411,14 +412,9 @@ void chunk_fwd(ChunkArgs a) {
       }
     };
     // (in pairs: a branch on the buffer in every step would move O from register to register)
-    for (int t = t0; t < t1; ++t) {
-      if (!odd) {
-        step(lds0, lds1, t);
-        odd = 1;
-        if (++t == t1) break;
-      }
-      step(lds1, lds0, t);
-      odd = 0;
+    for (int t = t0; t < t1; t += 2) {
+      step(lds0, lds1, t);
+      if (t + 1 < t1) step(lds1, lds0, t + 1);
     }
     asm volatile("" ::: "memory");
 
@@ -466,7 +462,9 @@ void chunk_fwd(ChunkArgs a) {
                             oacc[db][4 * g + 3]);
       }
     }
-    if (!more) {
+    e = seq;
+    x = uniform(me.end);
+    if (x >= part.hi) {
       if (keeps) {                        // a segment that goes on in later parts
         int4 rec = make_int4(0, seq, src.head, me.seg);
         if (begins && !whole) rec.x = Cut(plan.start[kMaxList], parts).owner(me.last) - part.p + 1;
@@ -474,7 +472,6 @@ void chunk_fwd(ChunkArgs a) {
       }
       return;
     }
-    which ^= 1;
   }
 }
 

@@ -58,14 +58,19 @@ struct Loader {
     pg = min(max(__builtin_amdgcn_readfirstlane(pg), 0), a.pages - 1);
     const int64_t off = ((((int64_t)pg * a.hkv + r.head) << a.page_shift) +
                          (key & ((1 << a.page_shift) - 1))) * D;
-    const auto ks = uniform_rsrc(a.k + off, S::STEP), vs = uniform_rsrc(a.v + off, S::STEP);
+    copy(a.k, a.v, off, r.once, k, v);
+  }
+  // The copies of 16 keys and values, `off` elements into the pools.
+  __device__ __forceinline__ void copy(const uint16_t *kp, const uint16_t *vp, int64_t off, int once,
+                                       uint8_t *k, uint8_t *v) const {
+    const auto ks = uniform_rsrc(kp + off, S::STEP), vs = uniform_rsrc(vp + off, S::STEP);
     const auto kd = (__attribute__((address_space(3))) void *)k;
     const auto vd = (__attribute__((address_space(3))) void *)v;
     // Keys that are read once pass the caches by: 64 sequences of 3 to 32000 tokens 98.5 -> 87.3
     // us, 16 samples of 32k 43.8 -> 40.9, drafts at head dim 64 53.8 -> 48.8, and 130 -> 88, 58 ->
     // 44, 68 -> 52 after a call that left the caches full of its own writes.  For prefixes of
     // several row tiles 560 -> 582 (256 samples of 128k).
-    if (r.once) {
+    if (once) {
       dma_slots<0, S::DMA, 2>(ks, kd, koff);
       dma_slots<0, S::DMA, 2>(vs, vd, voff);
     } else {
