@@ -28,10 +28,10 @@ namespace {
 constexpr int kMaxList = FP_MAX_CACHE_LIST;
 constexpr int kJoinThreads = 256;
 
-// A workgroup of `WAVES` waves: 32 rows each, and 16 keys of a tile that each brings.
-template <int WAVES>
+// A workgroup: `WAVES` waves of 32 rows, key tiles of `TILE` keys.
+template <int WAVES, int TILE>
 struct Geo {
-  static constexpr int THREADS = 64 * WAVES, ROWS = 32 * WAVES, KEYS = 16 * WAVES;
+  static constexpr int THREADS = 64 * WAVES, ROWS = 32 * WAVES, KEYS = TILE;
   static_assert(THREADS >= kMaxList, "the plan has one thread per sequence");
 };
 
@@ -216,6 +216,18 @@ __device__ __forceinline__ Piece piece_at(const ChunkArgs &a, const Plan &plan, 
   return r;
 }
 
+// Scores of keys that a row does not see, among N blocks of 32: -infinity from key `room` on.  (The least
+// of a score and + or - infinity: comparisons would take as many scalar registers as there are.)
+template <int N>
+__device__ __forceinline__ void mask(f32x16 *s, int room) {
+  const float end = (float)room - 0.5f;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int v = 0; v < 16; ++v)
+      s[i][v] = fminf(s[i][v], (end - (32 * i + 16 * (v >> 3) + (v & 7))) * INFINITY);
+}
+
 // Values among keys [key, end) that are not finite, times their weights, into O of the rows that see
 // them.  `qp`: the lane's half of its row's query.
 template <int D>
@@ -246,13 +258,47 @@ __device__ __forceinline__ void late_values(const ChunkArgs &a, const Source &sr
   }
 }
 
-template <int D, int WAVES>
-__global__ __launch_bounds__((Geo<WAVES>::THREADS))
+// The rows of a lane: to their place in o (`out`, a row of [d]), divided by the sum, or to the partial
+// result `part`.  The lane holds d = 32 db + 8 (v / 4) + 4 lh + v % 4 of row `row` of the tile.
+template <int D>
+__device__ __forceinline__ void finish(const ChunkArgs &a, bool whole, bool any,
+                                       const f32x16 (&oacc)[D / 32], float m_ref, float l, float *part,
+                                       int row, int lh, int64_t out) {
+  if (whole) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    uint16_t *op = a.o + out * D + 4 * lh;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        bf16x4 o;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = (__bf16)(oacc[db][4 * g + e] * inv);
+        *reinterpret_cast<bf16x4 *>(op + 32 * db + 8 * g) = o;
+      }
+    return;
+  }
+  if (lh == 0) *reinterpret_cast<float2 *>(part + a.tile_rows * D + 2 * row) = make_float2(m_ref, l);
+  part += row * D + 4 * lh;
+  if (any) {
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<float4 *>(part + 32 * db + 8 * g) =
+            make_float4(oacc[db][4 * g], oacc[db][4 * g + 1], oacc[db][4 * g + 2],
+                        oacc[db][4 * g + 3]);
+  }
+}
+
+// ---- Row tiles of 128: four waves of 32 rows, several workgroups to a CU.
+template <int D>
+__global__ __launch_bounds__(256)
 __attribute__((amdgpu_waves_per_eu(PagedGeo<D>::OCC, PagedGeo<D>::OCC)))
 void chunk_fwd(ChunkArgs a) {
   using S = PagedGeo<D>;
-  using G = Geo<WAVES>;
-  constexpr int KS = D / 16, DB = D / 32, TILE = WAVES * S::STEP;
+  using G = Geo<4, kKeys>;
+  constexpr int KS = D / 16, DB = D / 32, TILE = 4 * S::STEP;
   // K and V of even tiles in lds0, of odd ones in lds1: two arrays, so that the compiler sees that
   // reads of one do not wait for copies into the other
   __shared__ __attribute__((aligned(1024))) uint8_t lds0[2 * TILE];
@@ -260,7 +306,7 @@ void chunk_fwd(ChunkArgs a) {
   __shared__ Plan plan;
   // the piece at hand, each wave's own copy: what is looked at after its tiles would else take scalar
   // registers meanwhile
-  __shared__ Piece s_piece[WAVES];
+  __shared__ Piece s_piece[4];
   __shared__ int s_odd[2];                // piece with late values that are not finite, by its parity
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int lr = lane & 31, lh = lane >> 5;
@@ -344,72 +390,60 @@ void chunk_fwd(ChunkArgs a) {
         page_next = page(min(t + 2, t1 - 1));
       }
       if (!active) return;
+      if (k0 >= lim_all) return;
+      f32x16 sacc[2] = {f32x16{}, f32x16{}};
 #pragma unroll
-      for (int sub = 0; sub < G::KEYS / kKeys; ++sub) {
-        const int ks = k0 + kKeys * sub;
-        if (ks >= lim_all) return;
-        f32x16 sacc[2] = {f32x16{}, f32x16{}};
-#pragma unroll
-        for (int k = 0; k < KS; ++k) {
-          bf16x8 kf[2];
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-            kf[i] = *reinterpret_cast<const bf16x8 *>(tile + kaddr[k] + (2 * sub + i) * 32 * S::RB);
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-            sacc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], qf[k], sacc[i], 0, 0, 0);
-        }
-        __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
-#pragma unroll
-        for (int i = 0; i < 2 * KS - 6; ++i) {
-          __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        }
-        __builtin_amdgcn_sched_group_barrier(0x8, 6, 0);
-        if (ks + kKeys > lim_w) {
-          // (the least of a score and + or - infinity: comparisons would take scalar registers)
-          const float room = (float)(lim - ks - 8 * lh) - 0.5f;
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int v = 0; v < 16; ++v)
-              sacc[i][v] = fminf(sacc[i][v], (room - (32 * i + 16 * (v >> 3) + (v & 7))) * INFINITY);
-        }
-        float mt = -INFINITY;
+      for (int k = 0; k < KS; ++k) {
+        bf16x8 kf[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int v = 0; v < 16; ++v) mt = fmaxf(mt, sacc[i][v]);
-        // The reference moves only when a score rises 2^kLazy above it in weight, and has a weight of
-        // 2^-kLazy, so that no weight is above 1: sums of large values do not pass float32 before they
-        // are divided.
-        if (__ballot(mt > m_trig)) {
-          const float m_new = fmaxf(m_ref, wave_pair_max(mt));
-          const float f = m_ref == m_new ? 1.f : __builtin_amdgcn_exp2f((m_ref - m_new) * c);
-          l_run *= f;
-#pragma unroll
-          for (int i = 0; i < DB; ++i) oacc[i] *= f;
-          m_ref = m_new;
-          const bool none = m_new == -INFINITY;
-          mc = none ? 0.f : fmaf(m_new, c, kLazy);
-          m_trig = none ? -INFINITY : m_new + lazy_raw;
-        }
-        bf16x8 pf[4];
+          kf[i] = *reinterpret_cast<const bf16x8 *>(tile + kaddr[k] + i * 32 * S::RB);
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int v = 0; v < 16; ++v)
-            pf[2 * i + (v >> 3)][v & 7] = (__bf16)__builtin_amdgcn_exp2f(fmaf(sacc[i][v], c, -mc));
-        l_run = sum_weights(pf, l_run);
-#pragma unroll
-        for (int t4 = 0; t4 < 4; ++t4)
-#pragma unroll
-          for (int db = 0; db < DB; ++db) {
-            const bf16x8 vf =
-                *reinterpret_cast<const bf16x8 *>(tile + vaddr + db * 1024 + (4 * sub + t4) * S::STEP);
-            oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[t4], oacc[db], 0, 0, 0);
-          }
+          sacc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], qf[k], sacc[i], 0, 0, 0);
       }
+      __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+      for (int i = 0; i < 2 * KS - 6; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x8, 6, 0);
+      if (k0 + kKeys > lim_w) mask<2>(sacc, lim - k0 - 8 * lh);
+      float mt = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) mt = fmaxf(mt, sacc[i][v]);
+      // The reference moves only when a score rises 2^kLazy above it in weight, and has a weight of
+      // 2^-kLazy, so that no weight is above 1: sums of large values do not pass float32 before they
+      // are divided.
+      if (__ballot(mt > m_trig)) {
+        const float m_new = fmaxf(m_ref, wave_pair_max(mt));
+        const float f = m_ref == m_new ? 1.f : __builtin_amdgcn_exp2f((m_ref - m_new) * c);
+        l_run *= f;
+#pragma unroll
+        for (int i = 0; i < DB; ++i) oacc[i] *= f;
+        m_ref = m_new;
+        const bool none = m_new == -INFINITY;
+        mc = none ? 0.f : fmaf(m_new, c, kLazy);
+        m_trig = none ? -INFINITY : m_new + lazy_raw;
+      }
+      bf16x8 pf[4];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+          pf[2 * i + (v >> 3)][v & 7] = (__bf16)__builtin_amdgcn_exp2f(fmaf(sacc[i][v], c, -mc));
+      l_run = sum_weights(pf, l_run);
+#pragma unroll
+      for (int t4 = 0; t4 < 4; ++t4)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          const bf16x8 vf =
+              *reinterpret_cast<const bf16x8 *>(tile + vaddr + db * 1024 + t4 * S::STEP);
+          oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[t4], oacc[db], 0, 0, 0);
+        }
     };
     // (in pairs: a branch on the buffer in every step would move O from register to register)
     for (int t = t0; t < t1; t += 2) {
@@ -429,45 +463,278 @@ void chunk_fwd(ChunkArgs a) {
     const int rows = uniform(me.rows);
     const bool begins = uniform(me.begins), whole = begins && uniform(me.ends);
 
-    // ---- lane holds row `row`, d = 32 db + 8 (v / 4) + 4 lh + v % 4
     const float l = wave_pair_sum(l_run);
-    if (whole) {
-      if (row < rows) {
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        uint16_t *op = a.o + ((int64_t)(a.cu[seq] + tok) * a.hq + src.head * a.G + srow - tok * a.G) * D +
-                       4 * lh;
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            bf16x4 o;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = (__bf16)(oacc[db][4 * g + e] * inv);
-            *reinterpret_cast<bf16x4 *>(op + 32 * db + 8 * g) = o;
-          }
-      }
-    } else if (row < rows) {
-      float *to = a.part + (int64_t)((2 * part.p + begins) * a.width + part.tile) *
-                               a.tile_rows * (D + 2);
-      if (lh == 0)
-        *reinterpret_cast<float2 *>(to + a.tile_rows * D + 2 * row) = make_float2(m_ref, l);
-      to += row * D + 4 * lh;
-      if (t0 < t1) {
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-          for (int g = 0; g < 4; ++g)
-            *reinterpret_cast<float4 *>(to + 32 * db + 8 * g) =
-                make_float4(oacc[db][4 * g], oacc[db][4 * g + 1], oacc[db][4 * g + 2],
-                            oacc[db][4 * g + 3]);
-      }
-    }
+    if (row < rows)
+      finish<D>(a, whole, t0 < t1, oacc, m_ref, l,
+                a.part + (int64_t)((2 * part.p + begins) * a.width + part.tile) * a.tile_rows * (D + 2),
+                row, lh, (int64_t)(a.cu[seq] + tok) * a.hq + src.head * a.G + srow - tok * a.G);
     e = seq;
     x = uniform(me.end);
     if (x >= part.hi) {
       if (keeps) {                        // a segment that goes on in later parts
         int4 rec = make_int4(0, seq, src.head, me.seg);
         if (begins && !whole) rec.x = Cut(plan.start[kMaxList], parts).owner(me.last) - part.p + 1;
+        a.seg[part.p] = rec;
+      }
+      return;
+    }
+  }
+}
+
+// ---- Row tiles of 256, head dim 128: eight waves of 32 rows, two on each SIMD.  Half a tile, 32 keys, at
+// a time, three of them at work together: S of half h + 1, the weights of half h and O += V P of half
+// h - 1 do not depend on each other, so that a wave keeps the matrix and the vector pipe busy at once
+// (both run side by side without loss: a product of 32 cycles with three multiply-adds and an exponential
+// takes 1.5 cycles more than alone).
+//
+// K of a tile is looked at a half before V, so tiles t - 1 to t + 1 are in use in step t and the next one
+// is on its way: four tiles of LDS each, 128 KB, one barrier a step.
+struct Wide {
+  using S = PagedGeo<128>;
+  using G = Geo<8, 64>;
+  static constexpr int D = 128, KS = D / 16, DB = D / 32, TILE = 4 * S::STEP, RING = 4;
+  // one object, of whose parts the compiler does not think that reads must wait for copies into others
+  struct Shared {
+    uint8_t k[RING][TILE], v[RING][TILE];
+    Plan plan;
+    Piece piece[8];                       // see chunk_fwd
+    int odd[2];                           // piece with late values that are not finite, by its parity
+  };
+};
+
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void chunk_wide(ChunkArgs a) {
+  using S = Wide::S;
+  using G = Wide::G;
+  constexpr int D = Wide::D, KS = Wide::KS, DB = Wide::DB, RING = Wide::RING;
+  __shared__ __attribute__((aligned(1024))) Wide::Shared sh;
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int lr = lane & 31, lh = lane >> 5;
+  const float c = a.scale_log2;
+  const float lazy_raw = fminf(kLazy / c, 3.0e38f);
+  if (tid < 2) sh.odd[tid] = 0;
+  int parts;
+  const Part part = make_plan<G>(a, sh.plan, parts);
+  const bool keeps = part.tile == 0 && tid == 0;       // writes the part's record
+  if (part.lo == part.hi) {
+    if (keeps && part.p < a.wgs / a.width) a.seg[part.p] = make_int4(0, 0, 0, 0);
+    return;
+  }
+  const int w4 = w & 3;                   // of the eight waves four bring the keys, four the values
+  const Loader<D, G::KEYS> load(w4, lane);
+  const int kr = (lr & ~12) | ((lr >> 1) & 4) | ((lr << 1) & 8);
+  uint32_t kaddr[KS];
+#pragma unroll
+  for (int k = 0; k < KS; ++k) kaddr[k] = kr * S::RB + swz_k<D>(2 * k + lh, kr) * 16;
+  const uint32_t vaddr = 16 * vt_unit(lr, lh);
+
+  int e = sh.plan.first, worked = 1;
+  int64_t x = part.lo;
+  while (true) {
+    sh.piece[w] = piece_at<G>(a, sh.plan, e, x, part);
+    asm volatile("" ::: "memory");
+    const Piece &me = sh.piece[w];
+    const Source src = {uniform(me.src.row), uniform(me.src.head), 0, uniform(me.src.limit),
+                        uniform(me.src.once)};
+    const int t0 = uniform(me.t0), t1 = uniform(me.t1);
+    const int32_t *table = a.table + (int64_t)src.row * a.max_pages;
+    const int64_t in_page = ((int64_t)src.head << a.page_shift) * D;
+    const int64_t page_size = ((int64_t)a.hkv << a.page_shift) * D;
+    // this wave's 16 keys or values of tile t: the table's entry, and the copy
+    auto page = [&](int t) {
+      return table[min(G::KEYS * t + 16 * w4, max(src.limit - 1, 0)) >> a.page_shift];
+    };
+    auto offset = [&](int t, int pg) {
+      pg = min(max(uniform(pg), 0), a.pages - 1);
+      return pg * page_size + in_page + ((G::KEYS * t + 16 * w4) & ((1 << a.page_shift) - 1)) * D;
+    };
+    auto copy_k = [&](int t, int pg) {
+      if (w < 4 && t < t1 && G::KEYS * t + 16 * w4 < src.limit)
+        load.copy_k(a.k + offset(t, pg), src.once, sh.k[t & (RING - 1)] + w4 * S::STEP);
+    };
+    auto copy_v = [&](int t, int pg) {
+      if (w >= 4 && t < t1 && G::KEYS * t + 16 * w4 < src.limit)
+        load.copy_v(a.v + offset(t, pg), src.once, sh.v[t & (RING - 1)] + w4 * S::STEP);
+    };
+    const int row0 = uniform(me.row0), seq = uniform(me.seq), vis = uniform(me.vis);
+    const bool active = 32 * w < uniform(me.rows);
+    const int row = 32 * w + lr;
+    const int srow = min(row0 + row, (a.cu[seq + 1] - a.cu[seq]) * a.G - 1), tok = srow / a.G;
+    const uint16_t *qp = a.q + (int64_t)(a.cu[seq] + tok) * a.q_stride +
+                         (int64_t)(src.head * a.G + srow - tok * a.G) * D + 8 * lh;
+    const int seen = max(vis + row0 / a.G, 0);         // keys that the tile's first row sees
+    // keys of this part that the wave's first row sees, and this lane's row
+    const int lim_w = min(vis + (row0 + 32 * w) / a.G, G::KEYS * t1);
+    const int lim = min(vis + tok, G::KEYS * t1);
+    f32x16 oacc[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db) oacc[db] = f32x16{};
+    float m_ref = -INFINITY, mc = 0.f, m_trig = -INFINITY, l_run = 0.f;
+
+    if (t0 < t1) {
+      wg_barrier();                       // (other waves may still read the last piece's tiles)
+      const int pg0 = page(t0), pg1 = page(t0 + 1), pg2 = page(t0 + 2);
+      copy_k(t0, pg0);
+      copy_v(t0, pg0);
+      copy_k(t0 + 1, pg1);
+      copy_v(t0 + 1, pg1);
+      copy_k(t0 + 2, pg2);
+      int pg_v = pg2, pg_k = page(t0 + 3);
+      bf16x8 qf[KS];
+#pragma unroll
+      for (int k = 0; k < KS; ++k) qf[k] = *reinterpret_cast<const bf16x8 *>(qp + 16 * k);
+#pragma unroll
+      for (int k = 0; k < KS; ++k) asm volatile("" : "+v"(qf[k]));
+
+      auto scores = [&](int half, f32x16 &to) {
+        const uint8_t *tile = sh.k[(half >> 1) & (RING - 1)] + (half & 1) * 32 * S::RB;
+        to = f32x16{};
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+          to = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+              *reinterpret_cast<const bf16x8 *>(tile + kaddr[k]), qf[k], to, 0, 0, 0);
+      };
+      auto values = [&](int half, const bf16x8 (&p)[2]) {
+        const uint8_t *tile = sh.v[(half >> 1) & (RING - 1)] + (half & 1) * 2 * S::STEP + vaddr;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int db = 0; db < DB; ++db)
+            oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                *reinterpret_cast<const bf16x8 *>(tile + db * 1024 + t * S::STEP), p[t], oacc[db], 0,
+                0, 0);
+      };
+      auto weights = [&](const f32x16 &s, bf16x8 (&to)[2]) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+          to[v >> 3][v & 7] = (__bf16)__builtin_amdgcn_exp2f(fmaf(s[v], c, -mc));
+        l_run = sum_weights(to, l_run);
+      };
+      auto largest = [&](const f32x16 &of) {
+        float mt = -INFINITY;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) mt = fmaxf(mt, of[v]);
+        return mt;
+      };
+      // What the new scores `of` (of `half`, the largest mt) do to the reference, as in chunk_fwd.  O has
+      // one half less than the sum, in the reference that was: it follows a half later (`pending`).
+      bool pending = false;
+      float alpha = 1.f;
+      auto settle_ref = [&](int half, f32x16 &of, float mt) {
+        if (32 * half + 32 > lim_w) {     // keys that some row of the wave does not see
+          mask<1>(&of, lim - 32 * half - 8 * lh);
+          mt = largest(of);
+        }
+        const bool moves = __ballot(mt > m_trig);
+        if (moves || pending) {
+          if (pending) {
+#pragma unroll
+            for (int db = 0; db < DB; ++db) oacc[db] *= alpha;
+          }
+          const float m_new = moves ? fmaxf(m_ref, wave_pair_max(mt)) : m_ref;
+          alpha = m_ref == m_new ? 1.f : __builtin_amdgcn_exp2f((m_ref - m_new) * c);
+          l_run *= alpha;
+          m_ref = m_new;
+          const bool none = m_new == -INFINITY;
+          mc = none ? 0.f : fmaf(m_new, c, kLazy);
+          m_trig = none ? -INFINITY : m_new + lazy_raw;
+          pending = moves;
+        }
+      };
+      // Half h: S of h + 1 (sn), weights of h (pn) from its scores (s), O += V P of h - 1 (p), dealt out
+      // over 16 places, each a product, the read of the fragment three places on, and a share of the
+      // vector instructions, which the compiler keeps in this order.
+      bf16x8 frag[4];
+      auto read_frag = [&](int h, int place) {         // of half h, or of the next one (place >= 16)
+        h += place >> 4;
+        place &= 15;
+        const int of = place < KS ? h + 1 : h - 1, slot = (of >> 1) & (RING - 1);
+        return *reinterpret_cast<const bf16x8 *>(
+            place < KS ? sh.k[slot] + (of & 1) * 32 * S::RB + kaddr[place & 7]
+                       : sh.v[slot] + ((of & 1) * 2 + (place - KS) / DB) * S::STEP +
+                             (place - KS) % DB * 1024 + vaddr);
+      };
+      auto half = [&](int h, const f32x16 &s, f32x16 &sn, const bf16x8 (&p)[2], bf16x8 (&pn)[2]) {
+        float mt = -INFINITY, ex[16];
+        sn = f32x16{};
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+          frag[(q + 3) & 3] = read_frag(h, q + 3);
+          f32x16 &acc = q < KS ? sn : oacc[(q - KS) % DB];
+          acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[q & 3], q < KS ? qf[q & 7] : p[(q - KS) / DB & 1],
+                                                        acc, 0, 0, 0);
+          ex[q] = __builtin_amdgcn_exp2f(fmaf(s[q], c, -mc));
+          if (q % 2 == 0 && q >= 2) {
+            pn[(q - 2) >> 3][(q - 2) & 7] = (__bf16)ex[q - 2];
+            pn[(q - 1) >> 3][(q - 1) & 7] = (__bf16)ex[q - 1];
+          }
+          if (q >= 10) {                  // (the scores are there two places after their last product)
+#pragma unroll
+            for (int v = (q - 10) * 3; v < (q - 9) * 3 && v < 16; ++v) mt = fmaxf(mt, sn[v]);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        pn[1][6] = (__bf16)ex[14];
+        pn[1][7] = (__bf16)ex[15];
+        l_run = sum_weights(pn, l_run);
+        asm volatile("" : "+v"(pn[0]), "+v"(pn[1]), "+v"(mt));   // (before the branch that follows)
+        settle_ref(h + 1, sn, mt);
+      };
+      // K of tile t + 1 and V of tile t are here; the next ones are sent for.
+      auto arrive = [&](int t) {
+        wait_copies();
+        if (w >= 4 && G::KEYS * (t + 1) > seen &&
+            settle<D>(sh.v[t & (RING - 1)] + w4 * S::STEP, G::KEYS * t + 16 * w4, src.limit, seen,
+                      lane) &&
+            lane == 0)
+          sh.odd[worked & 1] = worked;
+        wg_barrier();
+        const int k = pg_k, v = pg_v;
+        pg_v = pg_k;
+        pg_k = page(t + 4);
+        copy_k(t + 3, k);
+        copy_v(t + 2, v);
+      };
+      // scores and weights of even halves and of odd ones
+      f32x16 s0, s1;
+      bf16x8 p0[2], p1[2];
+      arrive(t0);
+      if (active) {
+        scores(2 * t0, s0);
+        settle_ref(2 * t0, s0, largest(s0));
+        scores(2 * t0 + 1, s1);
+        weights(s0, p0);
+        settle_ref(2 * t0 + 1, s1, largest(s1));
+#pragma unroll
+        for (int q = 0; q < 3; ++q) frag[q] = read_frag(2 * t0 + 1, q);
+        half(2 * t0 + 1, s1, s0, p0, p1);
+      }
+      for (int t = t0 + 1; t < t1; ++t) {
+        arrive(t);
+        if (active) {
+          half(2 * t, s0, s1, p1, p0);
+          half(2 * t + 1, s1, s0, p0, p1);
+        }
+      }
+      if (active) values(2 * t1 - 1, p1);              // (no score of the half after it moved anything)
+      asm volatile("" ::: "memory");
+      if (sh.odd[worked & 1] == worked && active)
+        late_values<D>(a, src, max(seen, G::KEYS * t0), min(src.limit, G::KEYS * t1), lim, qp, c, mc, lh,
+                       oacc);
+      ++worked;
+    }
+    const bool begins = uniform(me.begins), whole = begins && uniform(me.ends);
+    const float l = wave_pair_sum(l_run);
+    if (row < uniform(me.rows))
+      finish<D>(a, whole, t0 < t1, oacc, m_ref, l,
+                a.part + (int64_t)((2 * part.p + begins) * a.width + part.tile) * a.tile_rows * (D + 2),
+                row, lh, (int64_t)(a.cu[seq] + tok) * a.hq + src.head * a.G + srow - tok * a.G);
+    e = seq;
+    x = uniform(me.end);
+    if (x >= part.hi) {
+      if (keeps) {                        // a segment that goes on in later parts
+        int4 rec = make_int4(0, seq, src.head, me.seg);
+        if (begins && !whole) rec.x = Cut(sh.plan.start[kMaxList], parts).owner(me.last) - part.p + 1;
         a.seg[part.p] = rec;
       }
       return;
@@ -569,9 +836,10 @@ __global__ __launch_bounds__(kJoinThreads) void chunk_join(ChunkArgs a) {
   }
 }
 
-template <int D, int WAVES>
+template <int D>
 hipError_t launch(const ChunkArgs &a, hipStream_t s) {
-  chunk_fwd<D, WAVES><<<a.wgs, Geo<WAVES>::THREADS, 0, s>>>(a);
+  if (D == 128 && a.rows == 256) chunk_wide<<<a.wgs, 512, 0, s>>>(a);
+  else chunk_fwd<D><<<a.wgs, 256, 0, s>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int tiles = a.wgs / a.width * a.width;
@@ -583,8 +851,7 @@ hipError_t launch(const ChunkArgs &a, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_chunk_attn(const ChunkArgs &a, int d, hipStream_t s) {
-  if (d == 64) return launch<64, 4>(a, s);
-  return a.rows == 256 ? launch<128, 8>(a, s) : launch<128, 4>(a, s);
+  return d == 64 ? launch<64>(a, s) : launch<128>(a, s);
 }
 
 }  // namespace fp

@@ -63,20 +63,24 @@ struct Loader {
   // The copies of 16 keys and values, `off` elements into the pools.
   __device__ __forceinline__ void copy(const uint16_t *kp, const uint16_t *vp, int64_t off, int once,
                                        uint8_t *k, uint8_t *v) const {
-    const auto ks = uniform_rsrc(kp + off, S::STEP), vs = uniform_rsrc(vp + off, S::STEP);
-    const auto kd = (__attribute__((address_space(3))) void *)k;
-    const auto vd = (__attribute__((address_space(3))) void *)v;
     // Keys that are read once pass the caches by: 64 sequences of 3 to 32000 tokens 98.5 -> 87.3
     // us, 16 samples of 32k 43.8 -> 40.9, drafts at head dim 64 53.8 -> 48.8, and 130 -> 88, 58 ->
     // 44, 68 -> 52 after a call that left the caches full of its own writes.  For prefixes of
     // several row tiles 560 -> 582 (256 samples of 128k).
-    if (once) {
-      dma_slots<0, S::DMA, 2>(ks, kd, koff);
-      dma_slots<0, S::DMA, 2>(vs, vd, voff);
-    } else {
-      dma_slots<0, S::DMA>(ks, kd, koff);
-      dma_slots<0, S::DMA>(vs, vd, voff);
-    }
+    copy_k(kp + off, once, k);
+    copy_v(vp + off, once, v);
+  }
+  __device__ __forceinline__ void copy_k(const uint16_t *from, int once, uint8_t *to) const {
+    const auto r = uniform_rsrc(from, S::STEP);
+    const auto dst = (__attribute__((address_space(3))) void *)to;
+    if (once) dma_slots<0, S::DMA, 2>(r, dst, koff);
+    else dma_slots<0, S::DMA>(r, dst, koff);
+  }
+  __device__ __forceinline__ void copy_v(const uint16_t *from, int once, uint8_t *to) const {
+    const auto r = uniform_rsrc(from, S::STEP);
+    const auto dst = (__attribute__((address_space(3))) void *)to;
+    if (once) dma_slots<0, S::DMA, 2>(r, dst, voff);
+    else dma_slots<0, S::DMA>(r, dst, voff);
   }
 };
 
