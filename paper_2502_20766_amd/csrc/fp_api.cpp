@@ -984,6 +984,14 @@ fp_status fp_chunk_attn(const fp_cache *cache, const fp_chunk *batch, int32_t la
   a.width = dm.width;
   a.rows = dm.rows;
   a.tile_rows = dm.tile_rows;
+  int64_t records = 0;
+  for (int i = 0; i < batch->batch; ++i) {
+    const int64_t rows = ((int64_t)batch->cu[i + 1] - batch->cu[i]) * dm.G, span = dm.rows * dm.width;
+    a.base[i] = (int32_t)std::min<int64_t>(records, dm.wgs);
+    records += (rows + span - 1) / span * c.hkv;
+  }
+  a.by_segment = records <= dm.wgs / dm.width;
+  a.records = a.by_segment ? (int32_t)records : dm.wgs / dm.width;
   a.seg = (int4 *)ws;
   a.part = (float *)((char *)ws + dm.bytes_seg);
   a.scale_log2 = resolved_scale(batch->softmax_scale, c.d) * 1.4426950408889634f;

@@ -37,8 +37,16 @@ struct Geo {
 
 // Key tiles that a segment takes of the line beside its own: the cost of starting and ending a piece.
 constexpr int kSegCost = 2;
-// Fewest key tiles of a part.
-constexpr int kPartTiles = 4;
+// Fewest key tiles of a part: less than a segment's, so that every short one gets a part of its own.
+constexpr int kPartTiles = 3;
+// Key tiles from a segment's start or end within which a cut moves there.
+constexpr int kSnapTiles = 4;
+
+// A segment: sequence, KV head, its number there, its places in the line.
+struct Segment {
+  int seq, head, seg;
+  int64_t start, end;
+};
 
 // The line: places where the segments of a sequence begin, in (key, query head) pairs: a key tile is 64 G
 // places, so that the places of a sequence's segments are an arithmetic series.
@@ -46,62 +54,106 @@ struct Plan {
   int64_t start[kMaxList + 1];
   int64_t scan[kMaxList / 64];
   int len[kMaxList];                      // tokens of a sequence (0: no slot)
-  int first;                              // sequence that this workgroup's part begins in
+  int64_t lo, hi;                         // this workgroup's part
+  Segment first;                          // the segment that its uncut start lies in
 };
+
+// a / b for 0 <= a < 2^62 and b > 0 where the result is below 2^45: an estimate, off by one at most, by a
+// reciprocal in float64.  (The division itself is a call's worth of instructions, and the plan has six.)
+__device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
+  const double y = (double)b;
+  double r = __builtin_amdgcn_rcp(y);
+  r = fma(fma(-y, r, 1.0), r, r);
+  r = fma(fma(-y, r, 1.0), r, r);
+  int64_t q = (int64_t)((double)a * r);
+  const int64_t rest = a - q * b;
+  if (rest < 0) --q;
+  else if (rest >= b) ++q;
+  return q;
+}
+
+// Inclusive prefix sum over the wave: within rows of 16 lanes, then the rows' sums handed on.
+__device__ __forceinline__ int64_t wave_scan(int64_t x) {
+  auto add = [&](auto ctrl, auto rows, auto zero) {
+    constexpr int c = decltype(ctrl)::value, m = decltype(rows)::value;
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)x, c, m, 0xf, decltype(zero)::value);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(x >> 32), c, m, 0xf, decltype(zero)::value);
+    x += (int64_t)(((uint64_t)hi << 32) | lo);
+  };
+  using std::integral_constant;
+  typedef integral_constant<int, 0xf> All;
+  add(integral_constant<int, 0x111>{}, All{}, std::true_type{});          // row_shr 1
+  add(integral_constant<int, 0x112>{}, All{}, std::true_type{});
+  add(integral_constant<int, 0x114>{}, All{}, std::true_type{});
+  add(integral_constant<int, 0x118>{}, All{}, std::true_type{});
+  add(integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{}, std::false_type{});  // row_bcast 15
+  add(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{}, std::false_type{});  // row_bcast 31
+  return x;
+}
 
 // A line of `total` places in `parts` equal parts, the first total % parts of them one place longer.
 struct Cut {
   int64_t per, rem;
-  __device__ __forceinline__ Cut(int64_t total, int parts) : per(total / parts) {
+  __device__ __forceinline__ Cut(int64_t total, int parts) : per(divide(total, parts)) {
     rem = total - per * parts;
   }
   __device__ __forceinline__ int64_t begin(int p) const { return per * p + min((int64_t)p, rem); }
   __device__ __forceinline__ int owner(int64_t x) const {
     const int64_t longer = rem * (per + 1);
-    return (int)(x < longer ? x / (per + 1) : rem + (x - longer) / per);
+    return (int)(x < longer ? divide(x, per + 1) : rem + divide(x - longer, per));
   }
 };
 
-// A sequence's segments of one KV head: segment i takes fixed + (i + 1) * step places.
+// A sequence's segments of one KV head: segment i takes fixed + (i + 1) * step places, the last one fixed +
+// its rows.
 template <class G>
 struct Series {
-  int64_t fixed, step;
-  int n;
+  int64_t fixed;
+  int step, n, rows;
   __device__ __forceinline__ Series(const ChunkArgs &a, int m, int len) {
-    const int64_t base = len > m ? len - m : 0;
     const int span = a.width * G::ROWS;
-    n = (int)(((int64_t)m * a.G + span - 1) / span);
-    fixed = a.G * (int64_t)(G::KEYS * kSegCost + (len > 0 ? G::KEYS + base : 0));
+    rows = m * a.G;
+    n = (int)((uint32_t)(rows + span - 1) / (uint32_t)span);
+    fixed = a.G * (int64_t)(G::KEYS * kSegCost + (len > 0 ? G::KEYS + max(len - m, 0) : 0));
     step = len > 0 ? span : 0;
+    if (len == 0) rows = 0;
   }
-  __device__ __forceinline__ int64_t begin(int64_t i) const {
-    return i * fixed + step * (i * (i + 1) / 2);
+  __device__ __forceinline__ int64_t begin(int i) const {
+    return i * fixed + (int64_t)step * ((int64_t)i * (i + 1) / 2);
   }
+  __device__ __forceinline__ int64_t end(int i) const {
+    return i + 1 < n ? begin(i + 1) : begin(i) + fixed + rows;
+  }
+  __device__ __forceinline__ int64_t whole() const { return n > 0 ? end(n - 1) : 0; }
 };
 
 struct Part {
   int p, tile;          // number of the part, row tile of its segments
-  int64_t lo, hi;       // places; lo == hi: none
+  int64_t lo, hi;       // places; lo >= hi: none
 };
+
+// A cut of the line in segment [start, end) of it: at `x`, or where that is near an end there, which
+// leaves short segments whole and long ones no short pieces.
+template <class G>
+__device__ __forceinline__ int64_t snap(const ChunkArgs &a, int64_t x, int64_t start, int64_t end) {
+  const int64_t near = (int64_t)kSnapTiles * G::KEYS * a.G;
+  return x - start <= near ? start : end - x <= near ? end : x;
+}
 
 // Fills the plan and finds this workgroup's part.
 template <class G>
 __device__ __forceinline__ Part make_plan(const ChunkArgs &a, Plan &plan, int &parts) {
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
-  int64_t cost = 0;
+  int len = 0, m = 0;
   if (t < a.batch) {
-    const int slot = a.slot[t], m = a.cu[t + 1] - a.cu[t];
-    const int len = slot < 0 ? 0 : min(max(a.len[slot], 0), a.max_pages << a.page_shift);
-    plan.len[t] = len;
-    const Series<G> series(a, m, len);
-    cost = series.begin(series.n) * a.hkv;
+    const int slot = a.slot[t];
+    m = a.cu[t + 1] - a.cu[t];
+    if (slot >= 0) len = min(max(a.len[slot], 0), a.max_pages << a.page_shift);
   }
-  int64_t sum = cost;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int64_t y = __shfl_up(sum, d);
-    if (lane >= d) sum += y;
-  }
+  if (t < kMaxList) plan.len[t] = len;
+  const Series<G> series(a, m, len);
+  const int64_t whole = series.whole(), cost = whole * a.hkv;
+  const int64_t sum = wave_scan(cost);
   if (lane == 63 && w < kMaxList / 64) plan.scan[w] = sum;
   __syncthreads();
   int64_t start = sum - cost, total = 0;
@@ -113,7 +165,7 @@ __device__ __forceinline__ Part make_plan(const ChunkArgs &a, Plan &plan, int &p
   if (t < kMaxList) plan.start[t] = start;
   if (t == 0) plan.start[kMaxList] = total;
   const int most = a.wgs / a.width;
-  const int64_t want = total / (kPartTiles * G::KEYS * (int64_t)a.G);
+  const int64_t want = divide(total, kPartTiles * G::KEYS * (int64_t)a.G);
   parts = (int)min(max(want, (int64_t)1), (int64_t)most);
   // Workgroups of one XCD (every eighth) take neighbouring parts; where there is not work for all, the
   // clusters are dealt out over the XCDs.
@@ -131,11 +183,52 @@ __device__ __forceinline__ Part make_plan(const ChunkArgs &a, Plan &plan, int &p
   r.lo = r.hi = 0;
   if (r.p < parts) {
     const Cut cut(total, parts);
-    r.lo = cut.begin(r.p);
-    r.hi = cut.begin(r.p + 1);
-    if (start <= r.lo && r.lo < start + cost) plan.first = t;
+    // its two ends, each by the thread of the sequence that it lies in
+    for (int i = 0; i < 2; ++i) {
+      const int64_t at = cut.begin(r.p + i);
+      if (at >= total) {
+        if (t == 0) plan.hi = total;
+      } else if (start <= at && at < start + cost) {
+        const int64_t in = at - start, head = divide(in, whole), z = in - head * whole;
+        int lo = 0, hi = series.n;                     // begin(lo) <= z < begin(hi)
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) / 2;
+          if (series.begin(mid) <= z) lo = mid;
+          else hi = mid;
+        }
+        const int64_t from = at - z + series.begin(lo), to = at - z + series.end(lo);
+        (i ? plan.hi : plan.lo) = snap<G>(a, at, from, to);
+        if (i == 0) plan.first = {t, (int)head, lo, from, to};
+      }
+    }
   }
   __syncthreads();
+  if (r.p < parts) {
+    r.lo = plan.lo;
+    r.hi = plan.hi;
+  }
+  return r;
+}
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  return (int64_t)(((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32) | (uint32_t)uniform((int)x));
+}
+
+// The segment after `s`, which is not the line's last.
+template <class G>
+__device__ __forceinline__ Segment after(const ChunkArgs &a, const Plan &plan, const Segment &s) {
+  Segment r = {s.seq, s.head, s.seg + 1, s.end, 0};
+  Series<G> series(a, a.cu[s.seq + 1] - a.cu[s.seq], uniform(plan.len[s.seq]));
+  if (r.seg == series.n) {
+    r.seg = 0;
+    if (++r.head == a.hkv) {
+      r.head = 0;
+      while (uniform(plan.start[r.seq + 1]) <= r.start) ++r.seq;
+      series = Series<G>(a, a.cu[r.seq + 1] - a.cu[r.seq], uniform(plan.len[r.seq]));
+    }
+  }
+  r.end = r.start + series.end(r.seg) - series.begin(r.seg);
   return r;
 }
 
@@ -152,43 +245,23 @@ struct Piece {
   Source src;
   int t0, t1;           // tiles [t0, t1) of its keys that this row tile sees
   int row0, rows;       // rows of the sequence and KV head: first, and how many (0: none)
-  int seq, seg;         // sequence, and segment of it and the KV head
   int vis;              // keys that the sequence's first query sees (may be negative)
+  int here;             // the part has any of the segment's tiles, or its start if it has none
   int begins, ends;     // the part has the segment's first tile, its last
-  int64_t end;          // place of the line where the segment ends
-  int64_t last;         // place of the segment's last tile
+  int64_t last;         // last place of the segment's last tile
+  Segment s;
 };
 
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ int64_t uniform(int64_t x) {
-  return (int64_t)(((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32) | (uint32_t)uniform((int)x));
-}
-
-// The piece at place x of the workgroup's part, which lies in sequence `e` or a later one.
+// The piece of a segment in the workgroup's part.
 template <class G>
-__device__ __forceinline__ Piece piece_at(const ChunkArgs &a, const Plan &plan, int e, int64_t x,
+__device__ __forceinline__ Piece piece_of(const ChunkArgs &a, const Plan &plan, const Segment &s,
                                           const Part &part) {
-  while (plan.start[e + 1] <= x) ++e;
   Piece r;
-  r.seq = uniform(e);
-  const int len = uniform(plan.len[r.seq]), m = a.cu[r.seq + 1] - a.cu[r.seq];
-  const Series<G> series(a, m, len);
-  const int64_t whole = series.begin(series.n);        // places of one KV head
-  const int64_t y = uniform(x - plan.start[r.seq]);
-  const int head = uniform((int)(y / whole));
-  const int64_t z = y - head * whole;
-  int lo = 0, hi = series.n;                           // begin(lo) <= z < begin(hi)
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (series.begin(mid) <= z) lo = mid;
-    else hi = mid;
-  }
-  r.seg = uniform(lo);
-  const int64_t start = x - z + series.begin(lo);
-  r.end = x - z + series.begin(lo + 1);
+  r.s = s;
+  const int len = uniform(plan.len[s.seq]), m = a.cu[s.seq + 1] - a.cu[s.seq];
   const int rows = m * a.G, span = a.width * G::ROWS;
-  r.src.row = a.slot[r.seq];
-  r.src.head = head;
+  r.src.row = a.slot[s.seq];
+  r.src.head = s.head;
   r.src.key0 = 0;
   r.src.limit = len;
   r.src.once = rows <= G::ROWS;
@@ -199,21 +272,45 @@ __device__ __forceinline__ Piece piece_at(const ChunkArgs &a, const Plan &plan, 
     const int keys = len > 0 ? max(r.vis + (end - 1) / a.G, 0) : 0;
     return (keys + G::KEYS - 1) / G::KEYS;
   };
-  const int all = tiles_of(min((lo + 1) * span, rows));
-  const int64_t first = start + kSegCost * (int64_t)tile;
+  const int all = tiles_of(min((s.seg + 1) * span, rows));
+  const int64_t first = s.start + kSegCost * (int64_t)tile;
   r.last = first + (int64_t)tile * all - 1;
-  const int t0 = part.lo <= first ? 0 : (int)min((part.lo - first) / tile, (int64_t)all);
-  const int t1 = part.hi >= r.end ? all
-                 : part.hi <= first ? 0 : (int)min((part.hi - first) / tile, (int64_t)all);
+  const int t0 = part.lo <= first ? 0 : (int)min(divide(part.lo - first, tile), (int64_t)all);
+  const int t1 = part.hi >= s.end ? all
+                 : part.hi <= first ? 0 : (int)min(divide(part.hi - first, tile), (int64_t)all);
   // (rows without a key belong to the part where they begin)
-  const bool here = all > 0 ? t0 < t1 : part.lo <= start;
-  r.row0 = lo * span + part.tile * G::ROWS;
+  const bool here = all > 0 ? t0 < t1 : part.lo <= s.start;
+  r.row0 = s.seg * span + part.tile * G::ROWS;
   r.rows = here ? max(min(rows - r.row0, G::ROWS), 0) : 0;
   r.t0 = t0;
   r.t1 = r.rows > 0 ? max(min(t1, tiles_of(r.row0 + r.rows)), t0) : t0;
+  r.here = here;
   r.begins = t0 == 0;
-  r.ends = t1 == all || !here;
+  r.ends = t1 == all;
   return r;
+}
+
+// What the join needs: of a segment that goes on in later parts, how many pieces it has and its first part.
+// With `by_segment` there is a record for every segment, from the part that it begins in, else one for
+// every part, of the segment that begins in it and goes on.
+template <class G>
+__device__ __forceinline__ void record(const ChunkArgs &a, const Plan &plan, const Part &part, int parts,
+                                       const Piece &p, bool last) {
+  const bool goes_on = p.here && p.begins && !p.ends;
+  int pieces = 0;
+  if (goes_on) {
+    // (a cut near the segment's end has moved there)
+    const int64_t near = (int64_t)kSnapTiles * G::KEYS * a.G;
+    const Cut cut(plan.start[kMaxList], parts);
+    pieces = cut.owner(min(p.last, p.s.end - near - 1)) - part.p + 1;
+  }
+  const int4 rec = make_int4(pieces | part.p << 16, p.s.seq, p.s.head, p.s.seg);
+  if (a.by_segment) {
+    const int n = Series<G>(a, a.cu[p.s.seq + 1] - a.cu[p.s.seq], 0).n;
+    if (p.here && p.begins) a.seg[a.base[p.s.seq] + p.s.head * n + p.s.seg] = rec;
+  } else if (last) {
+    a.seg[part.p] = rec;
+  }
 }
 
 // Scores of keys that a row does not see, among N blocks of 32: -infinity from key `room` on.  (The least
@@ -316,8 +413,8 @@ void chunk_fwd(ChunkArgs a) {
   int parts;
   const Part part = make_plan<G>(a, plan, parts);
   const bool keeps = part.tile == 0 && tid == 0;       // writes the part's record
-  if (part.lo == part.hi) {
-    if (keeps && part.p < a.wgs / a.width) a.seg[part.p] = make_int4(0, 0, 0, 0);
+  if (part.lo >= part.hi) {
+    if (keeps && !a.by_segment && part.p < a.wgs / a.width) a.seg[part.p] = make_int4(0, 0, 0, 0);
     return;
   }
   const Loader<D, G::KEYS> load(w, lane);
@@ -326,10 +423,13 @@ void chunk_fwd(ChunkArgs a) {
 #pragma unroll
   for (int k = 0; k < KS; ++k) kaddr[k] = kr * S::RB + swz_k<D>(2 * k + lh, kr) * 16;
   const uint32_t vaddr = TILE + 16 * vt_unit(lr, lh);
-  int e = plan.first, worked = 1;
-  int64_t x = part.lo;
+  Segment next = plan.first;
+  next = {uniform(next.seq), uniform(next.head), uniform(next.seg), uniform(next.start),
+          uniform(next.end)};
+  if (next.end <= part.lo) next = after<G>(a, plan, next);
+  int worked = 1;
   while (true) {
-    s_piece[w] = piece_at<G>(a, plan, e, x, part);
+    s_piece[w] = piece_of<G>(a, plan, next, part);
     asm volatile("" ::: "memory");
     const Piece &me = s_piece[w];
     const Source src = {uniform(me.src.row), uniform(me.src.head), 0, uniform(me.src.limit),
@@ -355,7 +455,7 @@ void chunk_fwd(ChunkArgs a) {
       issue(t0, page(t0), lds0);
       page_next = page(min(t0 + 1, t1 - 1));
     }
-    const int row0 = uniform(me.row0), seq = uniform(me.seq), vis = uniform(me.vis);
+    const int row0 = uniform(me.row0), seq = uniform(me.s.seq), vis = uniform(me.vis);
     const bool active = 32 * w < uniform(me.rows);
     const int row = 32 * w + lr;
     const int srow = min(row0 + row, (a.cu[seq + 1] - a.cu[seq]) * a.G - 1);
@@ -468,16 +568,11 @@ void chunk_fwd(ChunkArgs a) {
       finish<D>(a, whole, t0 < t1, oacc, m_ref, l,
                 a.part + (int64_t)((2 * part.p + begins) * a.width + part.tile) * a.tile_rows * (D + 2),
                 row, lh, (int64_t)(a.cu[seq] + tok) * a.hq + src.head * a.G + srow - tok * a.G);
-    e = seq;
-    x = uniform(me.end);
-    if (x >= part.hi) {
-      if (keeps) {                        // a segment that goes on in later parts
-        int4 rec = make_int4(0, seq, src.head, me.seg);
-        if (begins && !whole) rec.x = Cut(plan.start[kMaxList], parts).owner(me.last) - part.p + 1;
-        a.seg[part.p] = rec;
-      }
-      return;
-    }
+    next = {seq, src.head, uniform(me.s.seg), uniform(me.s.start), uniform(me.s.end)};
+    const bool last = next.end >= part.hi;
+    if (keeps) record<G>(a, plan, part, parts, me, last);
+    if (last) return;
+    next = after<G>(a, plan, next);
   }
 }
 
@@ -516,8 +611,8 @@ void chunk_wide(ChunkArgs a) {
   int parts;
   const Part part = make_plan<G>(a, sh.plan, parts);
   const bool keeps = part.tile == 0 && tid == 0;       // writes the part's record
-  if (part.lo == part.hi) {
-    if (keeps && part.p < a.wgs / a.width) a.seg[part.p] = make_int4(0, 0, 0, 0);
+  if (part.lo >= part.hi) {
+    if (keeps && !a.by_segment && part.p < a.wgs / a.width) a.seg[part.p] = make_int4(0, 0, 0, 0);
     return;
   }
   const int w4 = w & 3;                   // of the eight waves four bring the keys, four the values
@@ -528,10 +623,13 @@ void chunk_wide(ChunkArgs a) {
   for (int k = 0; k < KS; ++k) kaddr[k] = kr * S::RB + swz_k<D>(2 * k + lh, kr) * 16;
   const uint32_t vaddr = 16 * vt_unit(lr, lh);
 
-  int e = sh.plan.first, worked = 1;
-  int64_t x = part.lo;
+  Segment next = sh.plan.first;
+  next = {uniform(next.seq), uniform(next.head), uniform(next.seg), uniform(next.start),
+          uniform(next.end)};
+  if (next.end <= part.lo) next = after<G>(a, sh.plan, next);
+  int worked = 1;
   while (true) {
-    sh.piece[w] = piece_at<G>(a, sh.plan, e, x, part);
+    sh.piece[w] = piece_of<G>(a, sh.plan, next, part);
     asm volatile("" ::: "memory");
     const Piece &me = sh.piece[w];
     const Source src = {uniform(me.src.row), uniform(me.src.head), 0, uniform(me.src.limit),
@@ -556,7 +654,7 @@ void chunk_wide(ChunkArgs a) {
       if (w >= 4 && t < t1 && G::KEYS * t + 16 * w4 < src.limit)
         load.copy_v(a.v + offset(t, pg), src.once, sh.v[t & (RING - 1)] + w4 * S::STEP);
     };
-    const int row0 = uniform(me.row0), seq = uniform(me.seq), vis = uniform(me.vis);
+    const int row0 = uniform(me.row0), seq = uniform(me.s.seq), vis = uniform(me.vis);
     const bool active = 32 * w < uniform(me.rows);
     const int row = 32 * w + lr;
     const int srow = min(row0 + row, (a.cu[seq + 1] - a.cu[seq]) * a.G - 1), tok = srow / a.G;
@@ -729,110 +827,159 @@ void chunk_wide(ChunkArgs a) {
       finish<D>(a, whole, t0 < t1, oacc, m_ref, l,
                 a.part + (int64_t)((2 * part.p + begins) * a.width + part.tile) * a.tile_rows * (D + 2),
                 row, lh, (int64_t)(a.cu[seq] + tok) * a.hq + src.head * a.G + srow - tok * a.G);
-    e = seq;
-    x = uniform(me.end);
-    if (x >= part.hi) {
-      if (keeps) {                        // a segment that goes on in later parts
-        int4 rec = make_int4(0, seq, src.head, me.seg);
-        if (begins && !whole) rec.x = Cut(sh.plan.start[kMaxList], parts).owner(me.last) - part.p + 1;
-        a.seg[part.p] = rec;
-      }
-      return;
-    }
+    next = {seq, src.head, uniform(me.s.seg), uniform(me.s.start), uniform(me.s.end)};
+    const bool last = next.end >= part.hi;
+    if (keeps) record<G>(a, sh.plan, part, parts, me, last);
+    if (last) return;
+    next = after<G>(a, sh.plan, next);
   }
 }
 
-// ---- Joins the pieces of a row of a segment that begins in part p and ends in a later one: WPR waves,
-// each with every 64 / (D / 4) * WPR-th group of pieces, D / 4 lanes to a piece, 16 bytes each, four loads
-// in flight.
+// ---- Joins the pieces of a segment that begins in part p and ends in a later one; blockIdx.y is a
+// record and a row tile of its segment, of which the workgroups blockIdx.x share the rows.  D / 4 lanes to a row, 16 bytes
+// each.  Up to kFewPieces pieces: 32 rows at a time, all their loads in flight together.  More: WPR waves
+// to a row, each with every 64 / (D / 4) * WPR-th group of pieces, four loads in flight.
+constexpr int kFewPieces = 4;
+
 template <int D, int WPR>
 __global__ __launch_bounds__(kJoinThreads) void chunk_join(ChunkArgs a) {
   constexpr int LPP = D / 4;              // lanes per piece
   constexpr int PPW = 64 / LPP;           // pieces at once in a wave
   constexpr int U = 4;                    // loads in flight
   __shared__ f32x4 s_sum[4][LPP];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, part = w % WPR;
-  const int tile_at = blockIdx.y, p = tile_at / a.width, j = tile_at - p * a.width;
-  const int4 rec = a.seg[p];
-  const int n = rec.x;
+  const int at = blockIdx.y / a.width, j = blockIdx.y - at * a.width;
+  const int4 rec = a.seg[at];
+  const int n = rec.x & 0xFFFF, p = rec.x >> 16;
   if (n == 0) return;
-  const int r = blockIdx.x * (4 / WPR) + w / WPR;      // row of the tile
-  const int b = rec.y, m = a.cu[b + 1] - a.cu[b];
-  const int srow = (rec.w * a.width + j) * a.rows + r;
-  const bool live = r < a.tile_rows && srow < m * a.G;
-  if (WPR == 1 && !live) return;
+  const int b = rec.y, first = (rec.w * a.width + j) * a.rows;    // the tile's first row
+  const int rows = min((a.cu[b + 1] - a.cu[b]) * a.G - first, a.rows);
   const int64_t size = (int64_t)a.tile_rows * (D + 2);
   auto piece = [&](int i) {
     const int q = min(i, n - 1);
     return a.part + ((int64_t)(q == 0 ? 2 * p + 1 : 2 * (p + q)) * a.width + j) * size;
   };
-  const int row = live ? r : 0, ml_at = a.tile_rows * D + 2 * row;
-  const float c = a.scale_log2;
-  float top_all = -INFINITY, l = 0.f;
-  f32x4 acc = f32x4{};
-  for (int i0 = 0; i0 < n; i0 += 64) {
-    const int k = min(64, n - i0);
-    f32x4 x[U];
-    auto fetch = [&](int i) {
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        x[u] = __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(
-            piece(i0 + min(i + u * WPR * PPW + lane / LPP, k - 1)) + row * D + 4 * (lane % LPP)));
-    };
-    fetch(part * PPW);                    // beside the references, not after them
-    float2 ml = make_float2(-INFINITY, 0.f);
-    if (lane < k) ml = *reinterpret_cast<const float2 *>(piece(i0 + lane) + ml_at);
-    float top = fmaxf(top_all, ml.x);
-#pragma unroll
-    for (int d = 32; d > 0; d /= 2) top = fmaxf(top, __shfl_xor(top, d));
-    const float old = top_all == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((top_all - top) * c);
-    // (a sum of 0: no key seen; a NaN has to come through, whatever its reference)
-    const float f = ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f((ml.x - top) * c);
-    float sum = f * ml.y;
-#pragma unroll
-    for (int d = 32; d > 0; d /= 2) sum += __shfl_xor(sum, d);
-    l = l * old + sum;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e] *= old;
-    top_all = top;
-    for (int i = part * PPW; i < k; i += U * WPR * PPW) {
-      float fi[U];
-      if (i != part * PPW) fetch(i);
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int at = i + u * WPR * PPW + lane / LPP;
-        fi[u] = __shfl(f, at & 63);       // (by all lanes)
-        if (at >= k) fi[u] = 0.f;
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (fi[u] != 0.f) acc[e] = fmaf(fi[u], x[u][e], acc[e]);
-    }
-  }
-#pragma unroll
-  for (int d = LPP; d < 64; d *= 2)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], d);
-  if constexpr (WPR > 1) {
-    if (lane < LPP) s_sum[w][lane] = acc;
-    __syncthreads();
-    if (part != 0) return;
-    if (lane < LPP) {
-      acc = f32x4{};
-#pragma unroll
-      for (int i = 0; i < WPR; ++i) acc += s_sum[w + i][lane];
-    }
-  }
-  if (lane < LPP && live) {
+  auto store = [&](int r, const f32x4 &acc, float l, int lane) {
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    const int tok = srow / a.G;
+    const int srow = first + r, tok = srow / a.G;
     bf16x4 o;
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] = (__bf16)(acc[e] * inv);
-    *reinterpret_cast<bf16x4 *>(a.o + ((int64_t)(a.cu[b] + tok) * a.hq + rec.z * a.G + srow -
-                                       tok * a.G) * D + 4 * lane) = o;
+    *reinterpret_cast<bf16x4 *>(
+        a.o + ((int64_t)(a.cu[b] + tok) * a.hq + rec.z * a.G + srow - tok * a.G) * D + 4 * lane) = o;
+  };
+  const float c = a.scale_log2;
+  if (n <= kFewPieces) {
+    constexpr int AT_ONCE = kJoinThreads / LPP, PER = 32 / AT_ONCE;
+    const int lane = threadIdx.x % LPP, group = threadIdx.x / LPP;
+    for (int r0 = 32 * blockIdx.x; r0 < rows; r0 += 32 * gridDim.x) {
+      int row[PER];
+      float2 ml[PER][kFewPieces];
+      f32x4 x[PER][kFewPieces], acc[PER];
+      float l[PER];
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        row[i] = min(r0 + AT_ONCE * i + group, rows - 1);
+#pragma unroll
+        for (int q = 0; q < kFewPieces; ++q)
+          ml[i][q] = q < n ? *reinterpret_cast<const float2 *>(piece(q) + a.tile_rows * D + 2 * row[i])
+                           : make_float2(-INFINITY, 0.f);
+      }
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+#pragma unroll
+        for (int q = 0; q < kFewPieces; ++q)
+          if (q < n)
+            x[i][q] = __builtin_nontemporal_load(
+                reinterpret_cast<const f32x4 *>(piece(q) + row[i] * D + 4 * lane));
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int q = 0; q < kFewPieces; ++q) top = fmaxf(top, ml[i][q].x);
+        l[i] = 0.f;
+        acc[i] = f32x4{};
+#pragma unroll
+        for (int q = 0; q < kFewPieces; ++q) {
+          // (a sum of 0: no key seen; a NaN has to come through, whatever its reference)
+          ml[i][q].x = ml[i][q].y == 0.f ? 0.f : __builtin_amdgcn_exp2f((ml[i][q].x - top) * c);
+          l[i] = fmaf(ml[i][q].x, ml[i][q].y, l[i]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+#pragma unroll
+        for (int q = 0; q < kFewPieces; ++q)
+          if (q < n && ml[i][q].x != 0.f)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i][e] = fmaf(ml[i][q].x, x[i][q][e], acc[i][e]);
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (r0 + AT_ONCE * i + group < rows) store(row[i], acc[i], l[i], lane);
+    }
+    return;
+  }
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, part = w % WPR;
+  for (int r0 = blockIdx.x * (4 / WPR); r0 < rows; r0 += gridDim.x * (4 / WPR)) {
+    const int r = r0 + w / WPR;           // (with WPR == 4 all waves have the same)
+    if (WPR == 1 && r >= rows) break;
+    const int ml_at = a.tile_rows * D + 2 * r;
+    float top_all = -INFINITY, l = 0.f;
+    f32x4 acc = f32x4{};
+    for (int i0 = 0; i0 < n; i0 += 64) {
+      const int k = min(64, n - i0);
+      f32x4 x[U];
+      auto fetch = [&](int i) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          x[u] = __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(
+              piece(i0 + min(i + u * WPR * PPW + lane / LPP, k - 1)) + r * D + 4 * (lane % LPP)));
+      };
+      fetch(part * PPW);                  // beside the references, not after them
+      float2 ml = make_float2(-INFINITY, 0.f);
+      if (lane < k) ml = *reinterpret_cast<const float2 *>(piece(i0 + lane) + ml_at);
+      float top = fmaxf(top_all, ml.x);
+#pragma unroll
+      for (int d = 32; d > 0; d /= 2) top = fmaxf(top, __shfl_xor(top, d));
+      const float old = top_all == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((top_all - top) * c);
+      const float f = ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f((ml.x - top) * c);
+      float sum = f * ml.y;
+#pragma unroll
+      for (int d = 32; d > 0; d /= 2) sum += __shfl_xor(sum, d);
+      l = l * old + sum;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] *= old;
+      top_all = top;
+      for (int i = part * PPW; i < k; i += U * WPR * PPW) {
+        float fi[U];
+        if (i != part * PPW) fetch(i);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int at = i + u * WPR * PPW + lane / LPP;
+          fi[u] = __shfl(f, at & 63);     // (by all lanes)
+          if (at >= k) fi[u] = 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (fi[u] != 0.f) acc[e] = fmaf(fi[u], x[u][e], acc[e]);
+      }
+    }
+#pragma unroll
+    for (int d = LPP; d < 64; d *= 2)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], d);
+    if constexpr (WPR > 1) {
+      __syncthreads();                    // the sums of the row before are read
+      if (lane < LPP) s_sum[w][lane] = acc;
+      __syncthreads();
+      if (part == 0 && lane < LPP) {
+        acc = f32x4{};
+#pragma unroll
+        for (int i = 0; i < WPR; ++i) acc += s_sum[w + i][lane];
+      }
+    }
+    if (part == 0 && lane < LPP) store(r, acc, l, lane);
   }
 }
 
@@ -842,9 +989,12 @@ hipError_t launch(const ChunkArgs &a, hipStream_t s) {
   else chunk_fwd<D><<<a.wgs, 256, 0, s>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int tiles = a.wgs / a.width * a.width;
-  if (a.tile_rows <= 32) chunk_join<D, 4><<<dim3(a.tile_rows, tiles), kJoinThreads, 0, s>>>(a);
-  else chunk_join<D, 1><<<dim3(a.tile_rows / 4, tiles), kJoinThreads, 0, s>>>(a);
+  // 32 rows to a workgroup where there are many tiles, few of them cut into many pieces; else four, or one
+  const int tiles = a.records * a.width, few = a.tile_rows <= 32 ? 1 : 4;
+  const int per = (int64_t)tiles * a.tile_rows > 8192 * few ? 32 : few;
+  const dim3 grid((a.tile_rows + per - 1) / per, tiles);
+  if (a.tile_rows <= 32) chunk_join<D, 4><<<grid, kJoinThreads, 0, s>>>(a);
+  else chunk_join<D, 1><<<grid, kJoinThreads, 0, s>>>(a);
   return hipGetLastError();
 }
 

@@ -251,13 +251,16 @@ struct ChunkArgs {
   int32_t wgs;                 // workgroups that the keys are divided among
   int32_t width;               // row tiles side by side, one for each workgroup of a cluster
   int32_t rows;                // rows of a row tile: 128 or, with workgroups of eight waves, 256
+  int32_t records;             // what the join looks at: one for every segment or for every part
+  int32_t by_segment;
   int32_t tile_rows;           // rows of a partial result: `rows`, fewer where no sequence has as many
   float scale_log2;            // softmax scale * log2(e)
-  int4 *seg;                   // per part: pieces of the segment that begins in it and ends in a later
-                               // one (0: none), its sequence, KV head and number
+  int4 *seg;                   // records: pieces of a segment (0: one or none) and its first part, its
+                               // sequence, KV head and number
   float *part;                 // partial results, two for each workgroup
   int32_t slot[FP_MAX_CACHE_LIST];
   int32_t cu[FP_MAX_CACHE_LIST + 1];
+  int32_t base[FP_MAX_CACHE_LIST];         // per sequence: records before its own (by_segment)
 };
 
 // Query rows of one unit of work on prefixes with many rows: 4 waves of 32.
