@@ -44,15 +44,15 @@ class CacheError(RuntimeError):
 # to the library as the bytes of int32 arrays, tensors as plain addresses.
 
 _int32 = np.dtype(np.int32)
-_bf16 = _device = _raw_stream = None
+_bf16 = _i32 = _device = _raw_stream = None
 
 
 def _load_torch():
     """torch's parts that the calls use; importing this package does not load it."""
-    global _bf16, _device, _raw_stream
+    global _bf16, _i32, _device, _raw_stream
     import torch
     torch.cuda.init()
-    _bf16 = torch.bfloat16
+    _bf16, _i32 = torch.bfloat16, torch.int32
     _device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 
 

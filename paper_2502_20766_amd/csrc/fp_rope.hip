@@ -142,8 +142,46 @@ __device__ __forceinline__ void turn(const RopeArgs &r, const Lane<D> &l, const 
   b = narrow(y);
 }
 
-// ---- rotate: a wave takes one token and 64 / (D / 16) heads at a time, a.groups waves sharing the
-// heads of a token.
+// Heads of one token, by a wave: chunks of 64 / (D / 16) heads, kBatch at a time, whose loads are in flight
+// together (9001 tokens of 34 heads 36.1 us; one at a time 37.4, four at a time 37.2).  `from` and `to`: a
+// head's places, `weight` its norm's weights; `first` runs once the first loads are on their way.
+constexpr int kBatch = 2;
+
+template <int D, bool NORM, bool HALF, class From, class To, class Weight, class First>
+__device__ __forceinline__ void turn_heads(const RopeArgs &r, const Lane<D> &l, int heads, int chunk0,
+                                           int chunk_step, const float (&cs)[8], const float (&sn)[8],
+                                           const From &from, const To &to, const Weight &weight,
+                                           const First &first) {
+  using L = Lane<D>;
+  const int mine = (threadIdx.x & 63) / L::PER;
+  for (int h0 = chunk0 * L::HEADS, begun = 0; h0 < heads; h0 += kBatch * chunk_step * L::HEADS) {
+    Unit x[kBatch], y[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int h = h0 + i * chunk_step * L::HEADS;
+      if (h >= heads) break;
+      const Unit *at = (const Unit *)from(min(h + mine, heads - 1));
+      x[i] = at[l.a];
+      y[i] = at[l.b];
+    }
+    if (!begun) first();
+    begun = 1;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int h = h0 + i * chunk_step * L::HEADS;
+      if (h >= heads) break;
+      const int head = min(h + mine, heads - 1);
+      turn<D, NORM, HALF>(r, l, weight(head), cs, sn, x[i], y[i]);
+      if (h + mine < heads) {
+        Unit *at = (Unit *)to(head);
+        at[l.a] = x[i];
+        at[l.b] = y[i];
+      }
+    }
+  }
+}
+
+// ---- rotate: a wave takes one token, or of few tokens a chunk of the heads (a.groups waves to a token).
 template <int D, bool NORM, bool HALF>
 __global__ __launch_bounds__(kThreads) void rotate_heads(RotateArgs a) {
   using L = Lane<D>;
@@ -152,22 +190,19 @@ __global__ __launch_bounds__(kThreads) void rotate_heads(RotateArgs a) {
   const int64_t token = wave / a.groups;
   if (token >= a.tokens) return;
   const L l(lane % L::PER, a.rope.rotary);
+  const int pos = a.positions ? a.positions[token] : 0;
   float cs[8], sn[8];
-  turn_of<D, HALF>(a.rope, l, a.positions ? a.positions[token] : 0, cs, sn);
-  const int heads = a.hq + a.hkv;
-  for (int h0 = (int)(wave - token * a.groups) * L::HEADS; h0 < heads; h0 += a.groups * L::HEADS) {
-    const int h = min(h0 + lane / L::PER, heads - 1);
-    const bool live = h0 + lane / L::PER < heads, query = h < a.hq;
-    const int at = (query ? h : h - a.hq) * D;
-    const uint16_t *from = (query ? a.q + token * a.q_stride : a.k + token * a.k_stride) + at;
-    uint16_t *to = (query ? a.qo + token * a.qo_stride : a.ko + token * a.ko_stride) + at;
-    Unit x = ((const Unit *)from)[l.a], y = ((const Unit *)from)[l.b];
-    turn<D, NORM, HALF>(a.rope, l, query ? a.rope.wq : a.rope.wk, cs, sn, x, y);
-    if (live) {
-      ((Unit *)to)[l.a] = x;
-      ((Unit *)to)[l.b] = y;
-    }
-  }
+  turn_heads<D, NORM, HALF>(
+      a.rope, l, a.hq + a.hkv, (int)(wave - token * a.groups), a.groups, cs, sn,
+      [&](int h) {
+        return h < a.hq ? a.q + token * a.q_stride + h * D : a.k + token * a.k_stride + (h - a.hq) * D;
+      },
+      [&](int h) {
+        return h < a.hq ? a.qo + token * a.qo_stride + h * D
+                        : a.ko + token * a.ko_stride + (h - a.hq) * D;
+      },
+      [&](int h) { return h < a.hq ? a.rope.wq : a.rope.wk; },
+      [&]() { turn_of<D, HALF>(a.rope, l, pos, cs, sn); });
 }
 
 // ---- append: as cache_write, a workgroup has the new tokens among 64 positions of one slot, and of
@@ -201,22 +236,14 @@ __global__ __launch_bounds__(kThreads) void cache_append(CacheView c, AppendArgs
   if (h >= c.hkv) {                          // queries
     const int lane = tid & 63;
     const L l(lane % L::PER, x.rope.rotary);
-    const int t0 = p0 + kQueryTokens * (h - c.hkv);
-    for (int t = t0 + (tid >> 6); t < t0 + kQueryTokens; t += kThreads / 64) {
-      if (t < lo || t >= end) continue;
+    const int t0 = max(p0 + kQueryTokens * (h - c.hkv), lo);
+    const int t1 = min(p0 + kQueryTokens * (h - c.hkv + 1), end);
+    for (int t = t0 + (tid >> 6); t < t1; t += kThreads / 64) {
       const int64_t row = row0 + (t - start);
-      turn_of<D, HALF>(x.rope, l, t, cs, sn);
-      for (int h0 = 0; h0 < x.hq; h0 += L::HEADS) {
-        const int qh = h0 + lane / L::PER, at = min(qh, x.hq - 1) * D;
-        const uint16_t *from = x.q + row * x.q_stride + at;
-        uint16_t *to = x.qo + row * x.qo_stride + at;
-        Unit u = ((const Unit *)from)[l.a], v = ((const Unit *)from)[l.b];
-        turn<D, NORM, HALF>(x.rope, l, x.rope.wq, cs, sn, u, v);
-        if (qh < x.hq) {
-          ((Unit *)to)[l.a] = u;
-          ((Unit *)to)[l.b] = v;
-        }
-      }
+      turn_heads<D, NORM, HALF>(
+          x.rope, l, x.hq, 0, 1, cs, sn, [&](int qh) { return x.q + row * x.q_stride + qh * D; },
+          [&](int qh) { return x.qo + row * x.qo_stride + qh * D; }, [&](int) { return x.rope.wq; },
+          [&]() { turn_of<D, HALF>(x.rope, l, t, cs, sn); });
     }
     return;
   }

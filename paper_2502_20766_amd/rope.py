@@ -79,23 +79,23 @@ class HeadNorm:
 
 def _refs(rope, norm, d, index):
     """References to the structures of a call on device `index`, None for what it lacks."""
-    if norm is not None and norm.dim is not None and (norm.dim != d or norm.index != index):
+    if norm is None:
+        return (None if rope is None else rope.ref), None
+    if norm.dim is not None and (norm.dim != d or norm.index != index):
         raise ValueError(f"norm weights of {norm.dim} elements on device {norm.index}; the heads have "
                          f"{d} on {index}")
-    return (None if rope is None else rope.ref), (None if norm is None else norm.ref)
+    return (None if rope is None else rope.ref), norm.ref
 
 
-def _rows(x, name, index, d=None):
-    """Tokens, heads, head dim and the stride between tokens of [T, heads, d] bf16 with contiguous
-    rows on device `index`."""
-    shape, stride = x.shape, x.stride()
-    if len(shape) == 3 and x.get_device() == index and x.dtype is _cache._bf16:
-        n, h, e = shape
-        if (d is None or e == d) and h > 0 and (
-                n == 0 or (stride[2] == 1 and (h == 1 or stride[1] == e))):
-            return n, h, e, stride[0] if n > 1 else h * e
-    raise ValueError(f"{name} must be a bf16 tensor [T, heads, d] with contiguous rows on the device of "
-                     f"the others")
+def _stride(x, name, shape, index):
+    """Elements between tokens of x, a bf16 tensor of `shape` with contiguous rows on device `index`."""
+    if x.shape == shape and x.get_device() == index and x.dtype is _cache._bf16:
+        n, h, d = shape
+        token, head, one = x.stride()
+        if n == 0 or (one == 1 and (h == 1 or head == d)):
+            return token if n > 1 else h * d
+    raise ValueError(f"{name} must be a bf16 tensor of shape {tuple(shape)} with contiguous rows on the "
+                     f"device of the others")
 
 
 def _new(n, h, d, device, stream):
@@ -119,43 +119,44 @@ def rotate(q, k, positions, rope, norm=None, q_out=None, k_out=None, stream=None
         import torch
         with torch.cuda.device(index):
             return rotate(q, k, positions, rope, norm, q_out, k_out, stream)
-    raw = _cache._raw_stream(index) if stream is None else stream.cuda_stream
-    if getattr(stream, "device_index", index) != index:
-        raise ValueError(f"the stream is on device {stream.device_index}, the tensors on {index}")
-    T, heads, d, _ = _rows(first, "q" if q is not None else "k", index)
-    args, outs, counts = [], [], []
-    for x, out, name in ((q, q_out, "q"), (k, k_out, "k")):
-        if x is None:
-            if out is not None:
-                raise ValueError(f"{name}_out without {name}")
-            counts.append(0)
-            args.append((None, 0, None, 0))
-            outs.append(None)
-            continue
-        n, h, _, stride = _rows(x, name, index, d)
-        if out is None:
-            out = _new(n, h, d, x.device, stream)
-        m, ho, _, so = _rows(out, name + "_out", index, d)
-        if n != T or m != T or ho != h:
-            raise ValueError(f"{name} has shape {tuple(x.shape)}, its output {tuple(out.shape)}; the "
-                             f"call has {T} tokens")
-        if n == 1:
-            stride = so = h * d
-        counts.append(h)
-        args.append((x.data_ptr(), stride, out.data_ptr(), so))
-        outs.append(out)
+    if stream is None:
+        raw = _cache._raw_stream(index)
+    else:
+        raw = stream.cuda_stream
+        if getattr(stream, "device_index", index) != index:
+            raise ValueError(f"the stream is on device {stream.device_index}, the tensors on {index}")
+    if len(first.shape) != 3:
+        raise ValueError(f"q and k are [T, heads, d], got {tuple(first.shape)}")
+    T, heads, d = first.shape
+    hq = hkv = qs = ks = qos = kos = 0
+    qp = kp = qo = ko = None
+    if q is not None:
+        hq = heads
+        qs = _stride(q, "q", q.shape, index)
+        if q_out is None:
+            q_out = _new(T, hq, d, q.device, stream)
+        qos = _stride(q_out, "q_out", q.shape, index)
+        qp, qo = q.data_ptr(), q_out.data_ptr()
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    if k is not None:
+        hkv = k.shape[1] if len(k.shape) == 3 else 0
+        ks = _stride(k, "k", (T, hkv, d), index)
+        if k_out is None:
+            k_out = _new(T, hkv, d, k.device, stream)
+        kos = _stride(k_out, "k_out", (T, hkv, d), index)
+        kp, ko = k.data_ptr(), k_out.data_ptr()
+    elif k_out is not None:
+        raise ValueError("k_out without k")
+    at = None
     if rope is not None:
-        import torch
         if not (positions is not None and positions.get_device() == index
-                and positions.dtype == torch.int32 and positions.shape == (T,)
-                and positions.is_contiguous()):
+                and positions.dtype is _cache._i32 and positions.shape == (T,)
+                and (T < 2 or positions.stride(0) == 1)):
             raise ValueError(f"positions must be a contiguous int32 CUDA tensor of {T} elements on the "
                              f"device of the others")
         at = positions.data_ptr()
-    else:
-        at = None
     r, w = _refs(rope, norm, d, index)
-    (qp, qs, qo, qos), (kp, ks, ko, kos) = args
-    _cache._call(lib().fp_rotate(T, counts[0], counts[1], d, qp, qs, kp, ks, at, r, w, qo, qos, ko,
-                                 kos, raw), "fp_rotate")
-    return outs[0], outs[1]
+    _cache._call(lib().fp_rotate(T, hq, hkv, d, qp, qs, kp, ks, at, r, w, qo, qos, ko, kos, raw),
+                 "fp_rotate")
+    return q_out, k_out
