@@ -943,7 +943,7 @@ fp_status fp_cache_append(const fp_cache *cache, int32_t layer, int32_t n, const
   if (cu[n] == 0) return FP_OK;
   if ((st = write_rows(cache, k, k_stride, v, v_stride, &a.w)) != FP_OK) return st;
   if (!rows_ok(num_q_heads, c.d, q, q_stride, q_out, q_out_stride)) return FP_ERR_INVALID_ARG;
-  if (blocks * fp::append_parts(c, num_q_heads > 0) >= (1 << 24)) return FP_ERR_UNSUPPORTED;
+  if (blocks * fp::append_parts(c, num_q_heads) >= (1 << 24)) return FP_ERR_UNSUPPORTED;
   a.hq = num_q_heads;
   a.q = num_q_heads > 0 ? (const uint16_t *)q : nullptr;
   a.qo = (uint16_t *)q_out;

@@ -195,7 +195,8 @@ struct RotateArgs {
   int64_t q_stride, k_stride, qo_stride, ko_stride;
   const int32_t *positions;
   int32_t tokens, hq, hkv;
-  int32_t groups;              // set by the launcher: waves that share the heads of a token
+  int32_t groups, set;         // set by the launcher: waves that share the heads of a token, tokens of
+                               // a wave
   RopeArgs rope;
 };
 
@@ -205,6 +206,7 @@ struct AppendArgs {
   uint16_t *qo;
   int64_t q_stride, qo_stride;
   int32_t hq;
+  int32_t query_tokens, set;   // set by the launcher: positions of a part of the queries, tokens of a wave
   RopeArgs rope;
 };
 
@@ -293,6 +295,6 @@ hipError_t launch_chunk_attn(const ChunkArgs &a, int d, hipStream_t s);
 hipError_t launch_rotate(const RotateArgs &a, int d, hipStream_t s);
 hipError_t launch_cache_append(const CacheView &c, const AppendArgs &a, hipStream_t s);
 // Workgroups of launch_cache_append per 64 positions of a slot.
-int append_parts(const CacheView &c, bool queries);
+int append_parts(const CacheView &c, int query_heads);
 
 }  // namespace fp

@@ -7,6 +7,7 @@
 // All in float32, rounded once.  The angle is held as a fraction of a turn: p times round(2^64 f_i /
 // 2 pi), modulo 2^64, which no position can make less exact; its upper 32 bits give a quadrant and an
 // angle within pi / 4, of which sine and cosine are the Taylor series.
+#include <algorithm>
 #include <type_traits>
 
 #include "fp_cache_dev.h"
@@ -144,16 +145,16 @@ __device__ __forceinline__ void turn(const RopeArgs &r, const Lane<D> &l, const 
 
 // Heads of one token, by a wave: chunks of 64 / (D / 16) heads, kBatch at a time, whose loads are in flight
 // together (9001 tokens of 34 heads 36.1 us; one at a time 37.4, four at a time 37.2).  `from` and `to`: a
-// head's places, `weight` its norm's weights; `first` runs once the first loads are on their way.
+// head's places, `weight` its norm's weights; `first` runs once the first loads are on their way.  A lane
+// has head `mine` of each chunk, and loads another in its place where there is none.
 constexpr int kBatch = 2;
 
 template <int D, bool NORM, bool HALF, class From, class To, class Weight, class First>
-__device__ __forceinline__ void turn_heads(const RopeArgs &r, const Lane<D> &l, int heads, int chunk0,
-                                           int chunk_step, const float (&cs)[8], const float (&sn)[8],
-                                           const From &from, const To &to, const Weight &weight,
-                                           const First &first) {
+__device__ __forceinline__ void turn_heads(const RopeArgs &r, const Lane<D> &l, int heads, int mine,
+                                           int chunk0, int chunk_step, const float (&cs)[8],
+                                           const float (&sn)[8], const From &from, const To &to,
+                                           const Weight &weight, const First &first) {
   using L = Lane<D>;
-  const int mine = (threadIdx.x & 63) / L::PER;
   for (int h0 = chunk0 * L::HEADS, begun = 0; h0 < heads; h0 += kBatch * chunk_step * L::HEADS) {
     Unit x[kBatch], y[kBatch];
 #pragma unroll
@@ -181,19 +182,42 @@ __device__ __forceinline__ void turn_heads(const RopeArgs &r, const Lane<D> &l, 
   }
 }
 
-// ---- rotate: a wave takes one token, or of few tokens a chunk of the heads (a.groups waves to a token).
+// Of what has fewer heads than a wave holds it takes `set` tokens, the lane that of number `token` of them
+// and its head `head`.
+template <int D>
+struct Place {
+  int token, head;
+  __device__ __forceinline__ Place(int set, int heads) {
+    const int i = (threadIdx.x & 63) / Lane<D>::PER;
+    token = set > 1 ? i / heads : 0;
+    head = i - token * heads;
+    if (set > 1 && token >= set) token = 0, head = heads;
+  }
+};
+
+template <int D>
+int set_of(int heads) {
+  return std::max(1, Lane<D>::HEADS / heads);
+}
+
+// ---- rotate: a wave takes one token, or of few tokens a chunk of the heads (a.groups waves to a token),
+// or of few heads several tokens (33348 tokens of 3 heads of 64 31.4 us a token at a time, 12.9 five).
 template <int D, bool NORM, bool HALF>
 __global__ __launch_bounds__(kThreads) void rotate_heads(RotateArgs a) {
   using L = Lane<D>;
   const int lane = threadIdx.x & 63;
   const int64_t wave = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
-  const int64_t token = wave / a.groups;
-  if (token >= a.tokens) return;
+  const int64_t unit = wave / a.groups, token0 = unit * a.set;
+  if (token0 >= a.tokens) return;
+  const int heads = a.hq + a.hkv;
+  Place<D> place(a.set, heads);
+  if (token0 + place.token >= a.tokens) place.token = 0, place.head = heads;
+  const int64_t token = token0 + place.token;
   const L l(lane % L::PER, a.rope.rotary);
   const int pos = a.positions ? a.positions[token] : 0;
   float cs[8], sn[8];
   turn_heads<D, NORM, HALF>(
-      a.rope, l, a.hq + a.hkv, (int)(wave - token * a.groups), a.groups, cs, sn,
+      a.rope, l, heads, place.head, (int)(wave - unit * a.groups), a.groups, cs, sn,
       [&](int h) {
         return h < a.hq ? a.q + token * a.q_stride + h * D : a.k + token * a.k_stride + (h - a.hq) * D;
       },
@@ -206,9 +230,14 @@ __global__ __launch_bounds__(kThreads) void rotate_heads(RotateArgs a) {
 }
 
 // ---- append: as cache_write, a workgroup has the new tokens among 64 positions of one slot, and of
-// them one KV head or an eighth of the queries (kQueryTokens positions, all heads).
-constexpr int kQueryTokens = 8;
-constexpr int kQueryParts = 64 / kQueryTokens;
+// them one KV head or a part of the queries (x.query_tokens positions, all heads: eight, or more of few
+// heads, so that a wave has two chunks).
+template <int D>
+int query_tokens(int heads) {
+  int n = 8;
+  while (2 * n <= std::min(64, 8 * set_of<D>(heads))) n *= 2;
+  return n;
+}
 
 template <int D, bool NORM, bool HALF>
 __global__ __launch_bounds__(kThreads) void cache_append(CacheView c, AppendArgs x) {
@@ -218,7 +247,7 @@ __global__ __launch_bounds__(kThreads) void cache_append(CacheView c, AppendArgs
   const WriteArgs &a = x.w;
   __shared__ __attribute__((aligned(16))) uint16_t tile[64][D + 8];
   __shared__ int s_i, s_page[4];
-  const int per = c.hkv + (x.q ? kQueryParts : 0);
+  const int per = c.hkv + (x.q ? 64 / x.query_tokens : 0);
   const int blk = blockIdx.x / per, h = blockIdx.x - blk * per, tid = threadIdx.x;
   if (tid < a.list.n && a.blk[tid] <= blk && blk < a.blk[tid + 1]) s_i = tid;
   const int error = c.state[1];
@@ -236,14 +265,18 @@ __global__ __launch_bounds__(kThreads) void cache_append(CacheView c, AppendArgs
   if (h >= c.hkv) {                          // queries
     const int lane = tid & 63;
     const L l(lane % L::PER, x.rope.rotary);
-    const int t0 = max(p0 + kQueryTokens * (h - c.hkv), lo);
-    const int t1 = min(p0 + kQueryTokens * (h - c.hkv + 1), end);
-    for (int t = t0 + (tid >> 6); t < t1; t += kThreads / 64) {
-      const int64_t row = row0 + (t - start);
+    const int t0 = max(p0 + x.query_tokens * (h - c.hkv), lo);
+    const int t1 = min(p0 + x.query_tokens * (h - c.hkv + 1), end);
+    const Place<D> place(x.set, x.hq);
+    for (int t = t0 + x.set * (tid >> 6); t < t1; t += x.set * (kThreads / 64)) {
+      const bool mine = t + place.token < t1;
+      const int at = mine ? t + place.token : t;
+      const int64_t row = row0 + (at - start);
       turn_heads<D, NORM, HALF>(
-          x.rope, l, x.hq, 0, 1, cs, sn, [&](int qh) { return x.q + row * x.q_stride + qh * D; },
+          x.rope, l, x.hq, mine ? place.head : x.hq, 0, 1, cs, sn,
+          [&](int qh) { return x.q + row * x.q_stride + qh * D; },
           [&](int qh) { return x.qo + row * x.qo_stride + qh * D; }, [&](int) { return x.rope.wq; },
-          [&]() { turn_of<D, HALF>(x.rope, l, t, cs, sn); });
+          [&]() { turn_of<D, HALF>(x.rope, l, at, cs, sn); });
     }
     return;
   }
@@ -292,20 +325,33 @@ __global__ __launch_bounds__(kThreads) void cache_append(CacheView c, AppendArgs
   write_values<D>(c, tile, s_page, p0, lo, end, tile_of);
 }
 
+}  // namespace
+
+int append_parts(const CacheView &c, int heads) {
+  if (heads == 0) return c.hkv;
+  return c.hkv + 64 / (c.d == 64 ? query_tokens<64>(heads) : query_tokens<128>(heads));
+}
+
+namespace {
+
 template <int D, bool NORM, bool HALF>
 hipError_t rotate(const RotateArgs &a, hipStream_t s) {
   RotateArgs b = a;
   const int chunks = (a.hq + a.hkv + Lane<D>::HEADS - 1) / Lane<D>::HEADS;
+  b.set = set_of<D>(a.hq + a.hkv);
   b.groups = a.tokens <= 1024 ? chunks : 1;
-  const int64_t waves = (int64_t)a.tokens * b.groups;
+  const int64_t waves = ((int64_t)a.tokens + b.set - 1) / b.set * b.groups;
   rotate_heads<D, NORM, HALF><<<(unsigned)((waves + 3) / 4), kThreads, 0, s>>>(b);
   return hipGetLastError();
 }
 
 template <int D, bool NORM, bool HALF>
 hipError_t append(const CacheView &c, const AppendArgs &a, hipStream_t s) {
-  const int per = c.hkv + (a.q ? kQueryParts : 0);
-  cache_append<D, NORM, HALF><<<a.w.blk[a.w.list.n] * per, kThreads, 0, s>>>(c, a);
+  AppendArgs b = a;
+  b.set = a.q ? set_of<D>(a.hq) : 1;
+  b.query_tokens = a.q ? query_tokens<D>(a.hq) : 64;
+  const int per = append_parts(c, a.q ? a.hq : 0);
+  cache_append<D, NORM, HALF><<<a.w.blk[a.w.list.n] * per, kThreads, 0, s>>>(c, b);
   return hipGetLastError();
 }
 
@@ -323,8 +369,6 @@ hipError_t append(const CacheView &c, const AppendArgs &a, hipStream_t s) {
 }
 
 }  // namespace
-
-int append_parts(const CacheView &c, bool queries) { return c.hkv + (queries ? kQueryParts : 0); }
 
 hipError_t launch_rotate(const RotateArgs &a, int d, hipStream_t s) {
   return d == 64 ? rotate<64>(a, s) : rotate<128>(a, s);

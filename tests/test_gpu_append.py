@@ -199,3 +199,16 @@ def test_refusals():
         fpx.cache_append(c, 0, q, k, v, [0], [0, 3], fpx.Rope(128))
     with pytest.raises(fpx.FlexPrefillError):
         fpx.cache_append(c, 1, q, k, v, [0], [0, 3], rope)
+
+
+@pytest.mark.parametrize("d,hkv,hq", [(64, 1, 1), (64, 1, 2), (128, 1, 3), (128, 2, 4), (64, 1, 5),
+                                      (64, 3, 6), (64, 1, 15), (128, 1, 8)])
+@pytest.mark.parametrize("norm", [False, True])
+def test_few_query_heads(d, hkv, hq, norm):
+    """Queries of several tokens side by side; parts of the 64 positions of 8 to 64 tokens."""
+    a = Append(hq, norm=norm, layers=1, pages=64, hkv=hkv, d=d, slots=5, max_pages=20, page=16, seed=d + hq)
+    for slots, counts in (([3, 0, 1], [1, 70, 15]), ([1, 3], [1, 1]), ([0, 1, 3, 4], [64, 17, 0, 129]),
+                          ([4, 0], [1, 63])):
+        a.reserve(slots, counts)
+        a.put(slots, counts)
+    a.same()

@@ -215,3 +215,20 @@ def test_refusals():
     with pytest.raises(fpx.FlexPrefillError):       # an output shifted against its input
         fpx.rotate(x[:, :3], None, pos, rope, q_out=torch.empty(4 * 6 * 128 + 4, dtype=torch.bfloat16,
                                                                 device="cuda")[4:].view(4, 6, 128)[:, :3])
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(1, 1, 64), (1, 1, 128), (2, 1, 64), (3, 0, 128), (3, 1, 128),
+                                      (5, 2, 64), (7, 0, 64), (4, 4, 64), (5, 3, 128), (15, 0, 64)])
+@pytest.mark.parametrize("T", [1, 3, 16, 1023, 1500])
+def test_few_heads_of_many_tokens(hq, hkv, d, T):
+    """Heads of several tokens side by side, the last ones of which are not there."""
+    check(T, hq, hkv, d, norm="bf16", seed=T + hq)
+    x = bits(np.random.default_rng(T).standard_normal((T, hq, d)))
+    t, at = _dev(x), torch.arange(T, dtype=torch.int32, device="cuda")
+    import paper_2502_20766_amd as fpx
+    rope = fpx.Rope(d, layout="interleaved")
+    around = torch.full((T + 2, hq, d), 3.0, dtype=torch.bfloat16, device="cuda")
+    want, _ = fpx.rotate(t, None, at, rope, q_out=around[1:-1])
+    assert bool((around[0] == 3).all()) and bool((around[-1] == 3).all())
+    fpx.rotate(t, None, at, rope, q_out=t)
+    assert torch.equal(t, want)
