@@ -868,6 +868,12 @@ __global__ __launch_bounds__(kJoinThreads) void chunk_join(ChunkArgs a) {
         a.o + ((int64_t)(a.cu[b] + tok) * a.hq + rec.z * a.G + srow - tok * a.G) * D + 4 * lane) = o;
   };
   const float c = a.scale_log2;
+  // What a piece (its reference and sum) counts beside the largest reference.  A sum of 0 is that of a
+  // piece without a key that the row sees, whose O may not be there.  All others count: NaN comes through
+  // whatever its reference, infinity however small its weight.
+  auto factor = [&](float2 ml, float top) {
+    return ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f((ml.x - top) * c);
+  };
   if (n <= kFewPieces) {
     constexpr int AT_ONCE = kJoinThreads / LPP, PER = 32 / AT_ONCE;
     const int lane = threadIdx.x % LPP, group = threadIdx.x / LPP;
@@ -900,8 +906,7 @@ __global__ __launch_bounds__(kJoinThreads) void chunk_join(ChunkArgs a) {
         acc[i] = f32x4{};
 #pragma unroll
         for (int q = 0; q < kFewPieces; ++q) {
-          // (a sum of 0: no key seen; a NaN has to come through, whatever its reference)
-          ml[i][q].x = ml[i][q].y == 0.f ? 0.f : __builtin_amdgcn_exp2f((ml[i][q].x - top) * c);
+          ml[i][q].x = factor(ml[i][q], top);
           l[i] = fmaf(ml[i][q].x, ml[i][q].y, l[i]);
         }
       }
@@ -909,7 +914,7 @@ __global__ __launch_bounds__(kJoinThreads) void chunk_join(ChunkArgs a) {
       for (int i = 0; i < PER; ++i)
 #pragma unroll
         for (int q = 0; q < kFewPieces; ++q)
-          if (q < n && ml[i][q].x != 0.f)
+          if (q < n && ml[i][q].y != 0.f)
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[i][e] = fmaf(ml[i][q].x, x[i][q][e], acc[i][e]);
 #pragma unroll
@@ -941,8 +946,8 @@ __global__ __launch_bounds__(kJoinThreads) void chunk_join(ChunkArgs a) {
 #pragma unroll
       for (int d = 32; d > 0; d /= 2) top = fmaxf(top, __shfl_xor(top, d));
       const float old = top_all == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((top_all - top) * c);
-      const float f = ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f((ml.x - top) * c);
-      float sum = f * ml.y;
+      const float f = ml.y == 0.f ? -1.f : factor(ml, top);      // (-1: nothing to add)
+      float sum = ml.y == 0.f ? 0.f : f * ml.y;
 #pragma unroll
       for (int d = 32; d > 0; d /= 2) sum += __shfl_xor(sum, d);
       l = l * old + sum;
@@ -956,13 +961,13 @@ __global__ __launch_bounds__(kJoinThreads) void chunk_join(ChunkArgs a) {
         for (int u = 0; u < U; ++u) {
           const int at = i + u * WPR * PPW + lane / LPP;
           fi[u] = __shfl(f, at & 63);     // (by all lanes)
-          if (at >= k) fi[u] = 0.f;
+          if (at >= k) fi[u] = -1.f;
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (fi[u] != 0.f) acc[e] = fmaf(fi[u], x[u][e], acc[e]);
+            if (!(fi[u] < 0.f)) acc[e] = fmaf(fi[u], x[u][e], acc[e]);
       }
     }
 #pragma unroll

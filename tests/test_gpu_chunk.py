@@ -234,3 +234,22 @@ def test_refusals():
         fpx.chunk_attn(q, c, 0, b, workspace=ws[:-1])
     with pytest.raises(fpx.FlexPrefillError):
         fpx.chunk_attn(q, c, 1, b)
+
+
+@pytest.mark.parametrize("hq,hkv,d,m", [(4, 1, 64, 3), (4, 1, 128, 3), (4, 2, 128, 300)])
+@pytest.mark.parametrize("n", [1200, 30000])
+def test_values_that_are_not_finite_behind_vanishing_weights(hq, hkv, d, m, n):
+    """A weight that float32 rounds to zero times infinity is not finite, also where the keys of such
+    weights make up whole pieces of a sequence that is cut."""
+    s = Chunks([n], [m], hq, hkv, d, 64, seed=n)
+    low, zero = bits(np.full((hkv, d), -256.0)), bits(np.zeros((hkv, d)))
+    for t in range(n):
+        s.put(0, t, k=low if t < n // 2 else zero)
+    row = s.seqs[0][1][10].copy()
+    row[0, 5] = bits(np.inf)
+    s.put(0, 10, v=row)
+    q = bits(np.ones((m, hq, d)))
+    o = floats(_bits(s.fpx.chunk_attn(_dev(q), s.cache(), 0, s.of())))
+    odd = np.zeros((hq, d), bool)
+    odd[:hq // hkv, 5] = True
+    assert not np.isfinite(o[:, odd]).any() and np.isfinite(o[:, ~odd]).all()
