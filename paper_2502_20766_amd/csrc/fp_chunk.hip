@@ -492,23 +492,30 @@ void chunk_fwd(ChunkArgs a) {
       if (!active) return;
       if (k0 >= lim_all) return;
       f32x16 sacc[2] = {f32x16{}, f32x16{}};
+      // Fragments are read eight products before their use, in this order (left alone the compiler keeps
+      // registers for one pair and waits for each: three short sequences 13.4 us against 13.1, 48 chunks
+      // and single tokens 292 against 287).
+      constexpr int KA = 4, VA = 8;
+      bf16x8 kf[KA][2], vf[VA];
+      auto read_k = [&](int k) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          kf[k % KA][i] = *reinterpret_cast<const bf16x8 *>(tile + kaddr[k] + i * 32 * S::RB);
+      };
+      auto read_v = [&](int n) {
+        vf[n % VA] = *reinterpret_cast<const bf16x8 *>(tile + vaddr + n % DB * 1024 + n / DB * S::STEP);
+      };
+#pragma unroll
+      for (int k = 0; k < KA; ++k) read_k(k);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
-        bf16x8 kf[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-          kf[i] = *reinterpret_cast<const bf16x8 *>(tile + kaddr[k] + i * 32 * S::RB);
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-          sacc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], qf[k], sacc[i], 0, 0, 0);
+          sacc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k % KA][i], qf[k], sacc[i], 0, 0, 0);
+        if (k + KA < KS) read_k(k + KA);
+        __builtin_amdgcn_sched_barrier(0);
       }
-      __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
-#pragma unroll
-      for (int i = 0; i < 2 * KS - 6; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-      }
-      __builtin_amdgcn_sched_group_barrier(0x8, 6, 0);
       if (k0 + kKeys > lim_w) mask<2>(sacc, lim - k0 - 8 * lh);
       float mt = -INFINITY;
 #pragma unroll
@@ -537,13 +544,14 @@ void chunk_fwd(ChunkArgs a) {
           pf[2 * i + (v >> 3)][v & 7] = (__bf16)__builtin_amdgcn_exp2f(fmaf(sacc[i][v], c, -mc));
       l_run = sum_weights(pf, l_run);
 #pragma unroll
-      for (int t4 = 0; t4 < 4; ++t4)
+      for (int n = 0; n < VA; ++n) read_v(n);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int db = 0; db < DB; ++db) {
-          const bf16x8 vf =
-              *reinterpret_cast<const bf16x8 *>(tile + vaddr + db * 1024 + t4 * S::STEP);
-          oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[t4], oacc[db], 0, 0, 0);
-        }
+      for (int n = 0; n < 4 * DB; ++n) {
+        oacc[n % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[n % VA], pf[n / DB], oacc[n % DB], 0, 0, 0);
+        if (n + VA < 4 * DB) read_v(n + VA);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     };
     // (in pairs: a branch on the buffer in every step would move O from register to register)
     for (int t = t0; t < t1; t += 2) {
