@@ -995,6 +995,8 @@ fp_status fp_chunk_attn(const fp_cache *cache, const fp_chunk *batch, int32_t la
   a.width = dm.width;
   a.rows = dm.rows;
   a.tile_rows = dm.tile_rows;
+  const int64_t tiles = dm.tiles * c.hkv;
+  a.tiles = tiles <= (1 << 22) ? (int32_t)tiles : 0;
   int64_t records = 0;
   for (int i = 0; i < batch->batch; ++i) {
     const int64_t rows = ((int64_t)batch->cu[i + 1] - batch->cu[i]) * dm.G, span = dm.rows * dm.width;

@@ -8,14 +8,16 @@
 // v_mfma_f32_32x32x16_bf16: S^T = K Q^T with K rows permuted so that a lane's scores are the
 // consecutive keys that P^T of O^T += V^T P^T needs, one update of the reference for 64 keys.
 //
-// How the work is divided.  A segment is a.width row tiles of one sequence and KV head that lie side by
-// side, with the keys that the last of them sees.  Segments, one after the other, form a line whose
-// places are rows of keys; it is cut into equal parts, one for each cluster of a.width workgroups, each of
-// which takes one of the row tiles.  The workgroups of a cluster go through the same keys at the same
-// time, so those come from memory, and mostly from the XCD's L2, once.  A piece (a part's share of a
-// segment) that is not all of it leaves O, its reference and its sum in float32, and a last launch joins
-// the pieces of a row in the order of the line.  The cuts follow from the lengths alone, so results do
-// not depend on timing.
+// How the work is divided.  Row tiles of about equal length, or short ones, are not cut: a workgroup has
+// one with all of its keys, the longest ones of a sequence first.  Else a segment is a.width row tiles of
+// one sequence and KV head that lie side by side, with the keys that the last of them sees.  Segments, one
+// after the other, form a line whose places are rows of keys; it is cut into equal parts, one for each
+// cluster of a.width workgroups, each of which takes one of the row tiles.  The workgroups of a cluster go
+// through the same keys at the same time, so those come from memory, and mostly from the XCD's L2, once.
+// A piece (a part's share of a segment) that is not all of it leaves O, its reference and its sum in
+// float32, and a last launch joins the pieces of a row in the order of the line.  All of it follows from
+// the lengths alone, so results do not depend on timing.
+#include <algorithm>
 #include <type_traits>
 
 #include "fp_attn_dev.h"
@@ -42,6 +44,13 @@ constexpr int kPartTiles = 3;
 // Key tiles from a segment's start or end within which a cut moves there.
 constexpr int kSnapTiles = 4;
 
+// Row tiles are not cut where the longest sequence has at most so many key tiles more than twice a
+// workgroup's equal share of all of them: the device then hands out whole row tiles, and whoever is done
+// first takes the next.  Four whole prompts at head dim 64 720 -> 664 us, 59 chunks over 500 tokens 30 ->
+// 22; but 8 sequences of 20 tiles 22 -> 29, 48 of which one has 300 285 -> 459.  (With 1 in place of 2: 41
+// sequences of 20 tiles 39 us instead of 35.)
+constexpr int kWholeTiles = 14, kWholeShares = 2;
+
 // A segment: sequence, KV head, its number there, its places in the line.
 struct Segment {
   int seq, head, seg;
@@ -53,6 +62,7 @@ struct Segment {
 struct Plan {
   int64_t start[kMaxList + 1];
   int64_t scan[kMaxList / 64];
+  int tiles[kMaxList / 64], longest[kMaxList / 64];
   int len[kMaxList];                      // tokens of a sequence (0: no slot)
   int64_t lo, hi;                         // this workgroup's part
   Segment first;                          // the segment that its uncut start lies in
@@ -110,8 +120,8 @@ template <class G>
 struct Series {
   int64_t fixed;
   int step, n, rows;
-  __device__ __forceinline__ Series(const ChunkArgs &a, int m, int len) {
-    const int span = a.width * G::ROWS;
+  __device__ __forceinline__ Series(const ChunkArgs &a, int width, int m, int len) {
+    const int span = width * G::ROWS;
     rows = m * a.G;
     n = (int)((uint32_t)(rows + span - 1) / (uint32_t)span);
     fixed = a.G * (int64_t)(G::KEYS * kSegCost + (len > 0 ? G::KEYS + max(len - m, 0) : 0));
@@ -129,6 +139,7 @@ struct Series {
 
 struct Part {
   int p, tile;          // number of the part, row tile of its segments
+  int width;            // row tiles of a segment
   int64_t lo, hi;       // places; lo >= hi: none
 };
 
@@ -140,8 +151,28 @@ __device__ __forceinline__ int64_t snap(const ChunkArgs &a, int64_t x, int64_t s
   return x - start <= near ? start : end - x <= near ? end : x;
 }
 
-// Fills the plan and finds this workgroup's part.
-template <class G>
+// Inclusive prefix sum over the wave, or the largest value in its last lane.
+template <bool MAX>
+__device__ __forceinline__ int wave_fold(int x) {
+  auto step = [&](auto ctrl, auto rows) {
+    const int y = __builtin_amdgcn_update_dpp(0, x, decltype(ctrl)::value, decltype(rows)::value, 0xf,
+                                              false);
+    x = MAX ? max(x, y) : x + y;
+  };
+  using std::integral_constant;
+  typedef integral_constant<int, 0xf> All;
+  step(integral_constant<int, 0x111>{}, All{});
+  step(integral_constant<int, 0x112>{}, All{});
+  step(integral_constant<int, 0x114>{}, All{});
+  step(integral_constant<int, 0x118>{}, All{});
+  step(integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});
+  step(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});
+  return x;
+}
+
+// Fills the plan and finds this workgroup's part.  With WHOLE that may be one row tile with all of its
+// keys, of which the device then starts as many as there are, one after the other; `parts` is 0.
+template <class G, bool WHOLE>
 __device__ __forceinline__ Part make_plan(const ChunkArgs &a, Plan &plan, int &parts) {
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
   int len = 0, m = 0;
@@ -151,16 +182,55 @@ __device__ __forceinline__ Part make_plan(const ChunkArgs &a, Plan &plan, int &p
     if (slot >= 0) len = min(max(a.len[slot], 0), a.max_pages << a.page_shift);
   }
   if (t < kMaxList) plan.len[t] = len;
-  const Series<G> series(a, m, len);
+  const Series<G> series(a, a.width, m, len);
   const int64_t whole = series.whole(), cost = whole * a.hkv;
   const int64_t sum = wave_scan(cost);
   if (lane == 63 && w < kMaxList / 64) plan.scan[w] = sum;
+  const int tiles = (int)((uint32_t)(m * a.G + G::ROWS - 1) / G::ROWS);
+  int tiles_sum = 0;
+  if constexpr (WHOLE) {
+    tiles_sum = wave_fold<false>(tiles);
+    const int longest = wave_fold<true>(m > 0 ? (len + G::KEYS - 1) / G::KEYS : 0);
+    if (lane == 63) {
+      plan.tiles[w] = tiles_sum;
+      plan.longest[w] = longest;
+    }
+  }
   __syncthreads();
   int64_t start = sum - cost, total = 0;
 #pragma unroll
   for (int j = 0; j < kMaxList / 64; ++j) {
     if (j < w) start += plan.scan[j];
     total += plan.scan[j];
+  }
+  Part r;
+  r.width = a.width;
+  if constexpr (WHOLE) {
+    int first = tiles_sum - tiles, longest = 0;
+    for (int j = 0; j < kMaxList / 64; ++j) {
+      if (j < w) first += plan.tiles[j];
+      longest = max(longest, plan.longest[j]);
+    }
+    // (in float: all workgroups compute the same)
+    if (a.tiles > 0 &&
+        longest - kWholeTiles <=
+            kWholeShares * ((float)total * a.width / ((float)(G::KEYS * a.G) * a.wgs))) {
+      const int tile = blockIdx.x / a.hkv, head = blockIdx.x - tile * a.hkv;
+      if (t == 0) plan.hi = 0;
+      __syncthreads();
+      if (first <= tile && tile < first + tiles) {     // the last ones, which see most, before the others
+        plan.first = {t, head, tiles - 1 - (tile - first), 0, INT64_MAX};
+        plan.hi = INT64_MAX;
+      }
+      __syncthreads();
+      parts = 0;
+      r.p = blockIdx.x;
+      r.tile = 0;
+      r.width = 1;
+      r.lo = 0;
+      r.hi = plan.hi;
+      return r;
+    }
   }
   if (t < kMaxList) plan.start[t] = start;
   if (t == 0) plan.start[kMaxList] = total;
@@ -170,8 +240,10 @@ __device__ __forceinline__ Part make_plan(const ChunkArgs &a, Plan &plan, int &p
   // Workgroups of one XCD (every eighth) take neighbouring parts; where there is not work for all, the
   // clusters are dealt out over the XCDs.
   const int x = blockIdx.x & 7, y = blockIdx.x >> 3, room = a.wgs / 8 / a.width;
-  Part r;
-  if (8 * parts * a.width > 7 * a.wgs || parts > 8 * room) {
+  if ((int)blockIdx.x >= a.wgs) {
+    r.p = most;
+    r.tile = 0;
+  } else if (8 * parts * a.width > 7 * a.wgs || parts > 8 * room) {
     const int wg = x * (a.wgs / 8) + y;
     r.p = wg / a.width;
     r.tile = wg - r.p * a.width;
@@ -219,13 +291,13 @@ __device__ __forceinline__ int64_t uniform(int64_t x) {
 template <class G>
 __device__ __forceinline__ Segment after(const ChunkArgs &a, const Plan &plan, const Segment &s) {
   Segment r = {s.seq, s.head, s.seg + 1, s.end, 0};
-  Series<G> series(a, a.cu[s.seq + 1] - a.cu[s.seq], uniform(plan.len[s.seq]));
+  Series<G> series(a, a.width, a.cu[s.seq + 1] - a.cu[s.seq], uniform(plan.len[s.seq]));
   if (r.seg == series.n) {
     r.seg = 0;
     if (++r.head == a.hkv) {
       r.head = 0;
       while (uniform(plan.start[r.seq + 1]) <= r.start) ++r.seq;
-      series = Series<G>(a, a.cu[r.seq + 1] - a.cu[r.seq], uniform(plan.len[r.seq]));
+      series = Series<G>(a, a.width, a.cu[r.seq + 1] - a.cu[r.seq], uniform(plan.len[r.seq]));
     }
   }
   r.end = r.start + series.end(r.seg) - series.begin(r.seg);
@@ -259,7 +331,7 @@ __device__ __forceinline__ Piece piece_of(const ChunkArgs &a, const Plan &plan, 
   Piece r;
   r.s = s;
   const int len = uniform(plan.len[s.seq]), m = a.cu[s.seq + 1] - a.cu[s.seq];
-  const int rows = m * a.G, span = a.width * G::ROWS;
+  const int rows = m * a.G, span = part.width * G::ROWS;
   r.src.row = a.slot[s.seq];
   r.src.head = s.head;
   r.src.key0 = 0;
@@ -306,7 +378,7 @@ __device__ __forceinline__ void record(const ChunkArgs &a, const Plan &plan, con
   }
   const int4 rec = make_int4(pieces | part.p << 16, p.s.seq, p.s.head, p.s.seg);
   if (a.by_segment) {
-    const int n = Series<G>(a, a.cu[p.s.seq + 1] - a.cu[p.s.seq], 0).n;
+    const int n = Series<G>(a, a.width, a.cu[p.s.seq + 1] - a.cu[p.s.seq], 0).n;
     if (p.here && p.begins) a.seg[a.base[p.s.seq] + p.s.head * n + p.s.seg] = rec;
   } else if (last) {
     a.seg[part.p] = rec;
@@ -411,8 +483,10 @@ void chunk_fwd(ChunkArgs a) {
   const float lazy_raw = fminf(kLazy / c, 3.0e38f);
   if (tid < 2) s_odd[tid] = 0;
   int parts;
-  const Part part = make_plan<G>(a, plan, parts);
-  const bool keeps = part.tile == 0 && tid == 0;       // writes the part's record
+  const Part part = make_plan<G, true>(a, plan, parts);
+  const bool keeps = parts > 0 && part.tile == 0 && tid == 0;    // writes the part's record
+  if (parts == 0 && tid == 0 && (int)blockIdx.x < a.records)
+    a.seg[blockIdx.x] = make_int4(0, 0, 0, 0);         // (there are at least as many workgroups)
   if (part.lo >= part.hi) {
     if (keeps && !a.by_segment && part.p < a.wgs / a.width) a.seg[part.p] = make_int4(0, 0, 0, 0);
     return;
@@ -617,7 +691,7 @@ void chunk_wide(ChunkArgs a) {
   const float lazy_raw = fminf(kLazy / c, 3.0e38f);
   if (tid < 2) sh.odd[tid] = 0;
   int parts;
-  const Part part = make_plan<G>(a, sh.plan, parts);
+  const Part part = make_plan<G, false>(a, sh.plan, parts);
   const bool keeps = part.tile == 0 && tid == 0;       // writes the part's record
   if (part.lo >= part.hi) {
     if (keeps && !a.by_segment && part.p < a.wgs / a.width) a.seg[part.p] = make_int4(0, 0, 0, 0);
@@ -844,8 +918,8 @@ void chunk_wide(ChunkArgs a) {
 }
 
 // ---- Joins the pieces of a segment that begins in part p and ends in a later one; blockIdx.y is a
-// record and a row tile of its segment, of which the workgroups blockIdx.x share the rows.  D / 4 lanes to a row, 16 bytes
-// each.  Up to kFewPieces pieces: 32 rows at a time, all their loads in flight together.  More: WPR waves
+// record and a row tile of its segment, of which the workgroups blockIdx.x share the rows.  D / 4 lanes to
+// a row, 16 bytes each.  Up to kFewPieces pieces: 32 rows at a time, all their loads in flight together.  More: WPR waves
 // to a row, each with every 64 / (D / 4) * WPR-th group of pieces, four loads in flight.
 constexpr int kFewPieces = 4;
 
@@ -998,10 +1072,13 @@ __global__ __launch_bounds__(kJoinThreads) void chunk_join(ChunkArgs a) {
 
 template <int D>
 hipError_t launch(const ChunkArgs &a, hipStream_t s) {
-  if (D == 128 && a.rows == 256) chunk_wide<<<a.wgs, 512, 0, s>>>(a);
-  else chunk_fwd<D><<<a.wgs, 256, 0, s>>>(a);
+  const bool wide = D == 128 && a.rows == 256;
+  if (wide) chunk_wide<<<a.wgs, 512, 0, s>>>(a);
+  else chunk_fwd<D><<<std::max(a.wgs, a.tiles), 256, 0, s>>>(a);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  // (a cache whose slots are so short is never cut)
+  const bool short_slots = (int64_t)a.max_pages << a.page_shift <= kWholeTiles * kKeys;
+  if (e != hipSuccess || (!wide && a.tiles > 0 && short_slots)) return e;
   // 32 rows to a workgroup where there are many tiles, few of them cut into many pieces; else four, or one
   const int tiles = a.records * a.width, few = a.tile_rows <= 32 ? 1 : 4;
   const int per = (int64_t)tiles * a.tile_rows > 8192 * few ? 32 : few;

@@ -253,3 +253,22 @@ def test_values_that_are_not_finite_behind_vanishing_weights(hq, hkv, d, m, n):
     odd = np.zeros((hq, d), bool)
     odd[:hq // hkv, 5] = True
     assert not np.isfinite(o[:, odd]).any() and np.isfinite(o[:, ~odd]).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("n", [880, 895, 896, 897, 911, 960, 961])
+def test_where_sequences_begin_to_be_cut(d, page, n):
+    """Lengths about 14 key tiles, to which sequences stay whole whatever the rest, one launch if the
+    table has room for no more; alone, and beside short and idle ones."""
+    Chunks([n], [1], 4, 1, d, page, seed=n).go()
+    Chunks([n, 3, None, 400, 0, n - 1], [200, 3, 2, 1, 4, 33], 4, 2, d, page, seed=n).go()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_whole_row_tiles_of_many_sequences(d):
+    """More row tiles than workgroups at a time, of which none is cut, and the same with one sequence so
+    long that they are."""
+    lens, news = [700 + 13 * i for i in range(40)], [120 + 11 * i for i in range(40)]
+    Chunks(lens, news, 4, 4, d, 64, seed=d).go()
+    Chunks(lens + [20000], news + [2], 4, 4, d, 64, seed=d).go()
