@@ -17,6 +17,11 @@
 // A piece (a part's share of a segment) that is not all of it leaves O, its reference and its sum in
 // float32, and a last launch joins the pieces of a row in the order of the line.  All of it follows from
 // the lengths alone, so results do not depend on timing.
+//
+// Bounds: products and softmax for chunks (4096 tokens after 127k, 32 heads of 128: 8.0 ms, 1.09 PFLOP/s, at
+// the clock of the power limit; four whole prompts of 1001-9001 tokens, 64 heads of 64: 630 us), memory for
+// single tokens (43 of them beside five chunks, over up to 20k tokens: 289 us, 3.2 TB/s), latency for short
+// ones (three of up to 112 tokens: 10.7 us).
 #include <algorithm>
 #include <type_traits>
 
@@ -919,8 +924,8 @@ void chunk_wide(ChunkArgs a) {
 
 // ---- Joins the pieces of a segment that begins in part p and ends in a later one; blockIdx.y is a
 // record and a row tile of its segment, of which the workgroups blockIdx.x share the rows.  D / 4 lanes to
-// a row, 16 bytes each.  Up to kFewPieces pieces: 32 rows at a time, all their loads in flight together.  More: WPR waves
-// to a row, each with every 64 / (D / 4) * WPR-th group of pieces, four loads in flight.
+// a row, 16 bytes each.  Up to kFewPieces pieces: 32 rows at a time, all their loads in flight together.
+// More: WPR waves to a row, each with every 64 / (D / 4) * WPR-th group of pieces, four loads in flight.
 constexpr int kFewPieces = 4;
 
 template <int D, int WPR>
