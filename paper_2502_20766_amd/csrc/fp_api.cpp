@@ -458,9 +458,10 @@ fp_status check_chunk(const fp_cache *c, const fp_chunk *b, ChunkDims *dm) {
     most = std::max(most, rows);
     dm->tiles += (rows + 127) / 128;
   }
-  // places of the line, an int64 in the kernels (a tile takes G per key and a few more, see Series)
+  // places of the line (a tile takes G per key and a few more, see Series): those of one of 16 parts or more
+  // are a quotient below 2^45, as the kernels' division needs it
   const double capacity = (double)c->max_pages * c->page;
-  if ((double)dm->tiles * c->num_kv_heads * (dm->G * (capacity + 512) + (double)most) > 4e18)
+  if ((double)dm->tiles * c->num_kv_heads * (dm->G * (capacity + 512) + (double)most) > 5e14)
     return FP_ERR_UNSUPPORTED;
   // Eight waves where that leaves few rows of a tile empty, and clusters of as many row tiles as do.
   const int64_t tiles_128 = dm->tiles;

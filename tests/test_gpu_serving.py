@@ -110,17 +110,17 @@ def test_sparse_prefill_of_rotated_heads(gpu):     # noqa: F811
 class Loop:
     """Steps of a loop over its own cache, alike for the same seed."""
 
-    def __init__(self, fpx, counts, hq, hkv, d, workspaces=None):
+    def __init__(self, fpx, counts, hq, hkv, d, first=None, max_pages=40):
         self.fpx, self.hq, self.hkv, self.d, self.layers = fpx, hq, hkv, d, 2
         g = torch.Generator("cuda").manual_seed(3)
         n = len(counts)
-        self.c = fpx.Cache(self.layers, 40 * n, hkv, d, n, 40, 16)
+        self.c = fpx.Cache(self.layers, max_pages * n, hkv, d, n, max_pages, 16)
         self.c.k.zero_(), self.c.v.zero_()
         self.rope, self.norm = model_of(fpx, d, True)
         self.slots, self.counts = np.arange(n, dtype=np.int32), np.array(counts, np.int32)
         self.cu = np.cumsum([0] + list(counts)).astype(np.int32)
         self.batch = fpx.ChunkBatch(self.slots, self.cu, hq)
-        first = [45 + 30 * i for i in range(n)]
+        first = first or [45 + 30 * i for i in range(n)]
         cu = np.cumsum([0] + first)
         fpx.cache_reserve(self.c, self.slots, first)
         for layer in range(self.layers):
@@ -132,7 +132,7 @@ class Loop:
         self.q = torch.zeros(T, hq, d, dtype=torch.bfloat16, device="cuda")
         self.o = [torch.zeros_like(self.q) for _ in range(self.layers)]
         sizes = fpx.cache_workspace_size(self.c), fpx.chunk_workspace_size(self.c, self.batch)
-        self.ws = workspaces or [torch.empty(s, dtype=torch.uint8, device="cuda") for s in sizes]
+        self.ws = [torch.empty(s, dtype=torch.uint8, device="cuda") for s in sizes]
 
     def step(self):
         hq, hkv, x = self.hq, self.hkv, self.x
@@ -182,6 +182,23 @@ def test_two_graphs_of_steps_that_share_their_workspaces(gpu, d):     # noqa: F8
             a.same(b)
     for a in live:
         a.c.check()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_graph_whose_sequences_become_long(gpu, d):     # noqa: F811
+    """Captured while row tiles stay whole, replayed beyond the lengths at which they are cut."""
+    make = lambda: Loop(gpu, [30, 1, 0], 4, 2, d, [800, 880, 5], 90)     # noqa: E731
+    live, eager = make(), make()
+    graph = live.capture()
+    g = torch.Generator("cuda").manual_seed(8)
+    for i in range(20):
+        x = randn(g, *live.x.shape)
+        live.x.copy_(x), eager.x.copy_(x)
+        graph.replay()
+        eager.step()
+        torch.cuda.synchronize()
+        live.same(eager)
+    live.c.check()
 
 
 def test_rotate_in_a_graph(gpu):     # noqa: F811

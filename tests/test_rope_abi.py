@@ -202,3 +202,12 @@ def test_binding_refuses_before_the_library():
             call()
     with pytest.raises(fpx.FlexPrefillError):
         fpx.Rope(40)
+
+
+@pytest.mark.parametrize("rows,status", [(1 << 24, OK), (1 << 29, UNSUPPORTED)])
+def test_chunks_whose_places_no_part_can_count(lib, rows, status):
+    """Row tiles times the keys that a slot has room for: up to 2^45 for each of 16 parts."""
+    c, n = _cache(), ctypes.c_size_t()
+    c.max_pages = (1 << 26) // c.page
+    b = _batch(cu=(0, rows, rows, rows, rows))
+    assert lib.fp_chunk_workspace_size(ctypes.byref(c), b.ref, ctypes.byref(n)) == status
