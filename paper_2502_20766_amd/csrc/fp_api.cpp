@@ -435,7 +435,8 @@ fp_status write_rows(const fp_cache *cache, const void *k, int64_t k_stride, con
 // A batch of chunks: query heads per KV head, how its row tiles are taken, workspace.
 struct ChunkDims {
   int G;
-  int64_t tiles;               // row tiles of a KV head
+  int64_t tiles;               // row tiles of 128 of a KV head
+  int64_t row_tiles;           // ... of `rows`
   int wgs, width, rows, tile_rows;   // see fp::ChunkArgs
   size_t bytes_seg, bytes;
 };
@@ -477,7 +478,8 @@ fp_status check_chunk(const fp_cache *c, const fp_chunk *b, ChunkDims *dm) {
   // keys: 4096 tokens over 128k in row tiles of 256 take 8654, 8373 and 8309 us at widths 1, 4 and 8 (of
   // 128: 9947, 9245, 8947), 200 over 120k (25 tiles of 128) 444, 438, 418 and 418 at 1, 2, 5 and 25.
   dm->width = 1;
-  const int64_t tiles = tiles_of(dm->rows) / (dm->rows / 128), longest = (most + dm->rows - 1) / dm->rows;
+  dm->row_tiles = tiles_of(dm->rows) / (dm->rows / 128);
+  const int64_t tiles = dm->row_tiles, longest = (most + dm->rows - 1) / dm->rows;
   double best = 0;
   for (int w = 1; w <= 16 && w <= longest && tiles > b->batch; w += b->batch <= 8 ? 1 : w) {
     const double full = (double)tiles * (dm->rows / 128) / (double)tiles_of((int64_t)dm->rows * w);
@@ -996,7 +998,7 @@ fp_status fp_chunk_attn(const fp_cache *cache, const fp_chunk *batch, int32_t la
   a.width = dm.width;
   a.rows = dm.rows;
   a.tile_rows = dm.tile_rows;
-  const int64_t tiles = dm.tiles * c.hkv;
+  const int64_t tiles = dm.row_tiles * c.hkv;
   a.tiles = tiles <= (1 << 22) ? (int32_t)tiles : 0;
   int64_t records = 0;
   for (int i = 0; i < batch->batch; ++i) {

@@ -49,12 +49,13 @@ constexpr int kPartTiles = 3;
 // Key tiles from a segment's start or end within which a cut moves there.
 constexpr int kSnapTiles = 4;
 
-// Row tiles are not cut where the longest sequence has at most so many key tiles more than twice a
-// workgroup's equal share of all of them: the device then hands out whole row tiles, and whoever is done
-// first takes the next.  Four whole prompts at head dim 64 720 -> 664 us, 59 chunks over 500 tokens 30 ->
-// 22; but 8 sequences of 20 tiles 22 -> 29, 48 of which one has 300 285 -> 459.  (With 1 in place of 2: 41
-// sequences of 20 tiles 39 us instead of 35.)
-constexpr int kWholeTiles = 14, kWholeShares = 2;
+// Row tiles are not cut where the longest sequence has at most so many key tiles more than SHARES times a
+// workgroup's equal share of all of them (two, one for row tiles of 256): the device then hands out whole
+// row tiles, and whoever is done first takes the next.  Four whole prompts at head dim 64 720 -> 664 us, 59
+// chunks over 500 tokens 30 -> 22; but 8 sequences of 20 tiles 22 -> 29, 48 of which one has 300 285 -> 459.
+// (With 1 in place of 2: 41 sequences of 20 tiles 39 us instead of 35.)  Of 256: a prompt of 20000 tokens
+// 3425 -> 3319; with 2 in place of 1 2048 tokens after 30001 857 -> 888, 12 prompts on a small rank 69 -> 82.
+constexpr int kWholeTiles = 14;
 
 // A segment: sequence, KV head, its number there, its places in the line.
 struct Segment {
@@ -175,9 +176,9 @@ __device__ __forceinline__ int wave_fold(int x) {
   return x;
 }
 
-// Fills the plan and finds this workgroup's part.  With WHOLE that may be one row tile with all of its
+// Fills the plan and finds this workgroup's part.  That may be one row tile with all of its
 // keys, of which the device then starts as many as there are, one after the other; `parts` is 0.
-template <class G, bool WHOLE>
+template <class G, int SHARES>
 __device__ __forceinline__ Part make_plan(const ChunkArgs &a, Plan &plan, int &parts) {
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
   int len = 0, m = 0;
@@ -192,14 +193,11 @@ __device__ __forceinline__ Part make_plan(const ChunkArgs &a, Plan &plan, int &p
   const int64_t sum = wave_scan(cost);
   if (lane == 63 && w < kMaxList / 64) plan.scan[w] = sum;
   const int tiles = (int)((uint32_t)(m * a.G + G::ROWS - 1) / G::ROWS);
-  int tiles_sum = 0;
-  if constexpr (WHOLE) {
-    tiles_sum = wave_fold<false>(tiles);
-    const int longest = wave_fold<true>(m > 0 ? (len + G::KEYS - 1) / G::KEYS : 0);
-    if (lane == 63) {
-      plan.tiles[w] = tiles_sum;
-      plan.longest[w] = longest;
-    }
+  const int tiles_sum = wave_fold<false>(tiles);
+  const int longest_here = wave_fold<true>(m > 0 ? (len + G::KEYS - 1) / G::KEYS : 0);
+  if (lane == 63 && w < kMaxList / 64) {
+    plan.tiles[w] = tiles_sum;
+    plan.longest[w] = longest_here;
   }
   __syncthreads();
   int64_t start = sum - cost, total = 0;
@@ -210,32 +208,30 @@ __device__ __forceinline__ Part make_plan(const ChunkArgs &a, Plan &plan, int &p
   }
   Part r;
   r.width = a.width;
-  if constexpr (WHOLE) {
-    int first = tiles_sum - tiles, longest = 0;
-    for (int j = 0; j < kMaxList / 64; ++j) {
-      if (j < w) first += plan.tiles[j];
-      longest = max(longest, plan.longest[j]);
+  int first = tiles_sum - tiles, longest = 0;
+  for (int j = 0; j < kMaxList / 64; ++j) {
+    if (j < w) first += plan.tiles[j];
+    longest = max(longest, plan.longest[j]);
+  }
+  // (in float: all workgroups compute the same)
+  if (a.tiles > 0 &&
+      longest - kWholeTiles <=
+          SHARES * ((float)total * a.width / ((float)(G::KEYS * a.G) * a.wgs))) {
+    const int tile = blockIdx.x / a.hkv, head = blockIdx.x - tile * a.hkv;
+    if (t == 0) plan.hi = 0;
+    __syncthreads();
+    if (first <= tile && tile < first + tiles) {     // the last ones, which see most, before the others
+      plan.first = {t, head, tiles - 1 - (tile - first), 0, INT64_MAX};
+      plan.hi = INT64_MAX;
     }
-    // (in float: all workgroups compute the same)
-    if (a.tiles > 0 &&
-        longest - kWholeTiles <=
-            kWholeShares * ((float)total * a.width / ((float)(G::KEYS * a.G) * a.wgs))) {
-      const int tile = blockIdx.x / a.hkv, head = blockIdx.x - tile * a.hkv;
-      if (t == 0) plan.hi = 0;
-      __syncthreads();
-      if (first <= tile && tile < first + tiles) {     // the last ones, which see most, before the others
-        plan.first = {t, head, tiles - 1 - (tile - first), 0, INT64_MAX};
-        plan.hi = INT64_MAX;
-      }
-      __syncthreads();
-      parts = 0;
-      r.p = blockIdx.x;
-      r.tile = 0;
-      r.width = 1;
-      r.lo = 0;
-      r.hi = plan.hi;
-      return r;
-    }
+    __syncthreads();
+    parts = 0;
+    r.p = blockIdx.x;
+    r.tile = 0;
+    r.width = 1;
+    r.lo = 0;
+    r.hi = plan.hi;
+    return r;
   }
   if (t < kMaxList) plan.start[t] = start;
   if (t == 0) plan.start[kMaxList] = total;
@@ -488,7 +484,7 @@ void chunk_fwd(ChunkArgs a) {
   const float lazy_raw = fminf(kLazy / c, 3.0e38f);
   if (tid < 2) s_odd[tid] = 0;
   int parts;
-  const Part part = make_plan<G, true>(a, plan, parts);
+  const Part part = make_plan<G, 2>(a, plan, parts);
   const bool keeps = parts > 0 && part.tile == 0 && tid == 0;    // writes the part's record
   if (parts == 0 && tid == 0 && (int)blockIdx.x < a.records)
     a.seg[blockIdx.x] = make_int4(0, 0, 0, 0);         // (there are at least as many workgroups)
@@ -696,8 +692,10 @@ void chunk_wide(ChunkArgs a) {
   const float lazy_raw = fminf(kLazy / c, 3.0e38f);
   if (tid < 2) sh.odd[tid] = 0;
   int parts;
-  const Part part = make_plan<G, false>(a, sh.plan, parts);
-  const bool keeps = part.tile == 0 && tid == 0;       // writes the part's record
+  const Part part = make_plan<G, 1>(a, sh.plan, parts);
+  const bool keeps = parts > 0 && part.tile == 0 && tid == 0;    // writes the part's record
+  if (parts == 0 && tid == 0 && (int)blockIdx.x < a.records)
+    a.seg[blockIdx.x] = make_int4(0, 0, 0, 0);
   if (part.lo >= part.hi) {
     if (keeps && !a.by_segment && part.p < a.wgs / a.width) a.seg[part.p] = make_int4(0, 0, 0, 0);
     return;
@@ -1078,12 +1076,12 @@ __global__ __launch_bounds__(kJoinThreads) void chunk_join(ChunkArgs a) {
 template <int D>
 hipError_t launch(const ChunkArgs &a, hipStream_t s) {
   const bool wide = D == 128 && a.rows == 256;
-  if (wide) chunk_wide<<<a.wgs, 512, 0, s>>>(a);
+  if (wide) chunk_wide<<<std::max(a.wgs, a.tiles), 512, 0, s>>>(a);
   else chunk_fwd<D><<<std::max(a.wgs, a.tiles), 256, 0, s>>>(a);
   const hipError_t e = hipGetLastError();
   // (a cache whose slots are so short is never cut)
   const bool short_slots = (int64_t)a.max_pages << a.page_shift <= kWholeTiles * kKeys;
-  if (e != hipSuccess || (!wide && a.tiles > 0 && short_slots)) return e;
+  if (e != hipSuccess || (a.tiles > 0 && short_slots)) return e;
   // 32 rows to a workgroup where there are many tiles, few of them cut into many pieces; else four, or one
   const int tiles = a.records * a.width, few = a.tile_rows <= 32 ? 1 : 4;
   const int per = (int64_t)tiles * a.tile_rows > 8192 * few ? 32 : few;

@@ -256,7 +256,7 @@ struct ChunkArgs {
   int32_t records;             // what the join looks at: one for every segment or for every part
   int32_t by_segment;
   int32_t tile_rows;           // rows of a partial result: `rows`, fewer where no sequence has as many
-  int32_t tiles;               // row tiles of 128 rows of all sequences and KV heads (0: too many for a grid)
+  int32_t tiles;               // row tiles of all sequences and KV heads (0: too many for a grid)
   float scale_log2;            // softmax scale * log2(e)
   int4 *seg;                   // records: pieces of a segment (0: one or none) and its first part, its
                                // sequence, KV head and number

@@ -272,3 +272,9 @@ def test_whole_row_tiles_of_many_sequences(d):
     lens, news = [700 + 13 * i for i in range(40)], [120 + 11 * i for i in range(40)]
     Chunks(lens, news, 4, 4, d, 64, seed=d).go()
     Chunks(lens + [20000], news + [2], 4, 4, d, 64, seed=d).go()
+
+
+def test_whole_row_tiles_of_256():
+    """Prompts that fill row tiles of 256, of which none is cut; a row tile that ends a sequence early."""
+    Chunks([1025, 900, 1100, None, 960, 0], [1025, 900, 1100, 5, 960, 3], 8, 2, 128, 64, seed=1).go()
+    Chunks([1500, 1400, 1300], [640, 640, 576], 8, 4, 128, 32, seed=2).go()
