@@ -26,28 +26,14 @@
 #include <type_traits>
 
 #include "fp_attn_dev.h"
+#include "fp_chunk_plan.h"
 #include "fp_internal.h"
 #include "fp_paged_dev.h"
 
 namespace fp {
 namespace {
 
-constexpr int kMaxList = FP_MAX_CACHE_LIST;
 constexpr int kJoinThreads = 256;
-
-// A workgroup: `WAVES` waves of 32 rows, key tiles of `TILE` keys.
-template <int WAVES, int TILE>
-struct Geo {
-  static constexpr int THREADS = 64 * WAVES, ROWS = 32 * WAVES, KEYS = TILE;
-  static_assert(THREADS >= kMaxList, "the plan has one thread per sequence");
-};
-
-// Key tiles that a segment takes of the line beside its own: the cost of starting and ending a piece.
-constexpr int kSegCost = 2;
-// Fewest key tiles of a part: less than a segment's, so that every short one gets a part of its own.
-constexpr int kPartTiles = 3;
-// Key tiles from a segment's start or end within which a cut moves there.
-constexpr int kSnapTiles = 4;
 
 // Row tiles are not cut where the longest sequence has at most so many key tiles more than SHARES times a
 // workgroup's equal share of all of them (two, one for row tiles of 256): the device then hands out whole
@@ -56,12 +42,6 @@ constexpr int kSnapTiles = 4;
 // (With 1 in place of 2: 41 sequences of 20 tiles 39 us instead of 35.)  Of 256: a prompt of 20000 tokens
 // 3425 -> 3319; with 2 in place of 1 2048 tokens after 30001 857 -> 888, 12 prompts on a small rank 69 -> 82.
 constexpr int kWholeTiles = 14;
-
-// A segment: sequence, KV head, its number there, its places in the line.
-struct Segment {
-  int seq, head, seg;
-  int64_t start, end;
-};
 
 // The line: places where the segments of a sequence begin, in (key, query head) pairs: a key tile is 64 G
 // places, so that the places of a sequence's segments are an arithmetic series.
@@ -73,20 +53,6 @@ struct Plan {
   int64_t lo, hi;                         // this workgroup's part
   Segment first;                          // the segment that its uncut start lies in
 };
-
-// a / b for 0 <= a < 2^62 and b > 0 where the result is below 2^45: an estimate, off by one at most, by a
-// reciprocal in float64.  (The division itself is a call's worth of instructions, and the plan has six.)
-__device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
-  const double y = (double)b;
-  double r = __builtin_amdgcn_rcp(y);
-  r = fma(fma(-y, r, 1.0), r, r);
-  r = fma(fma(-y, r, 1.0), r, r);
-  int64_t q = (int64_t)((double)a * r);
-  const int64_t rest = a - q * b;
-  if (rest < 0) --q;
-  else if (rest >= b) ++q;
-  return q;
-}
 
 // Inclusive prefix sum over the wave: within rows of 16 lanes, then the rows' sums handed on.
 __device__ __forceinline__ int64_t wave_scan(int64_t x) {
@@ -105,56 +71,6 @@ __device__ __forceinline__ int64_t wave_scan(int64_t x) {
   add(integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{}, std::false_type{});  // row_bcast 15
   add(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{}, std::false_type{});  // row_bcast 31
   return x;
-}
-
-// A line of `total` places in `parts` equal parts, the first total % parts of them one place longer.
-struct Cut {
-  int64_t per, rem;
-  __device__ __forceinline__ Cut(int64_t total, int parts) : per(divide(total, parts)) {
-    rem = total - per * parts;
-  }
-  __device__ __forceinline__ int64_t begin(int p) const { return per * p + min((int64_t)p, rem); }
-  __device__ __forceinline__ int owner(int64_t x) const {
-    const int64_t longer = rem * (per + 1);
-    return (int)(x < longer ? divide(x, per + 1) : rem + divide(x - longer, per));
-  }
-};
-
-// A sequence's segments of one KV head: segment i takes fixed + (i + 1) * step places, the last one fixed +
-// its rows.
-template <class G>
-struct Series {
-  int64_t fixed;
-  int step, n, rows;
-  __device__ __forceinline__ Series(const ChunkArgs &a, int width, int m, int len) {
-    const int span = width * G::ROWS;
-    rows = m * a.G;
-    n = (int)((uint32_t)(rows + span - 1) / (uint32_t)span);
-    fixed = a.G * (int64_t)(G::KEYS * kSegCost + (len > 0 ? G::KEYS + max(len - m, 0) : 0));
-    step = len > 0 ? span : 0;
-    if (len == 0) rows = 0;
-  }
-  __device__ __forceinline__ int64_t begin(int i) const {
-    return i * fixed + (int64_t)step * ((int64_t)i * (i + 1) / 2);
-  }
-  __device__ __forceinline__ int64_t end(int i) const {
-    return i + 1 < n ? begin(i + 1) : begin(i) + fixed + rows;
-  }
-  __device__ __forceinline__ int64_t whole() const { return n > 0 ? end(n - 1) : 0; }
-};
-
-struct Part {
-  int p, tile;          // number of the part, row tile of its segments
-  int width;            // row tiles of a segment
-  int64_t lo, hi;       // places; lo >= hi: none
-};
-
-// A cut of the line in segment [start, end) of it: at `x`, or where that is near an end there, which
-// leaves short segments whole and long ones no short pieces.
-template <class G>
-__device__ __forceinline__ int64_t snap(const ChunkArgs &a, int64_t x, int64_t start, int64_t end) {
-  const int64_t near = (int64_t)kSnapTiles * G::KEYS * a.G;
-  return x - start <= near ? start : end - x <= near ? end : x;
 }
 
 // Inclusive prefix sum over the wave, or the largest value in its last lane.
@@ -235,25 +151,8 @@ __device__ __forceinline__ Part make_plan(const ChunkArgs &a, Plan &plan, int &p
   }
   if (t < kMaxList) plan.start[t] = start;
   if (t == 0) plan.start[kMaxList] = total;
-  const int most = a.wgs / a.width;
-  const int64_t want = divide(total, kPartTiles * G::KEYS * (int64_t)a.G);
-  parts = (int)min(max(want, (int64_t)1), (int64_t)most);
-  // Workgroups of one XCD (every eighth) take neighbouring parts; where there is not work for all, the
-  // clusters are dealt out over the XCDs.
-  const int x = blockIdx.x & 7, y = blockIdx.x >> 3, room = a.wgs / 8 / a.width;
-  if ((int)blockIdx.x >= a.wgs) {
-    r.p = most;
-    r.tile = 0;
-  } else if (8 * parts * a.width > 7 * a.wgs || parts > 8 * room) {
-    const int wg = x * (a.wgs / 8) + y;
-    r.p = wg / a.width;
-    r.tile = wg - r.p * a.width;
-  } else {
-    const int c = y / a.width;
-    r.p = c < room ? c * 8 + x : most;
-    r.tile = y - c * a.width;
-  }
-  r.lo = r.hi = 0;
+  parts = parts_of<G>(a, total);
+  r = place_of(a, blockIdx.x, parts);
   if (r.p < parts) {
     const Cut cut(total, parts);
     // its two ends, each by the thread of the sequence that it lies in
@@ -262,16 +161,9 @@ __device__ __forceinline__ Part make_plan(const ChunkArgs &a, Plan &plan, int &p
       if (at >= total) {
         if (t == 0) plan.hi = total;
       } else if (start <= at && at < start + cost) {
-        const int64_t in = at - start, head = divide(in, whole), z = in - head * whole;
-        int lo = 0, hi = series.n;                     // begin(lo) <= z < begin(hi)
-        while (hi - lo > 1) {
-          const int mid = (lo + hi) / 2;
-          if (series.begin(mid) <= z) lo = mid;
-          else hi = mid;
-        }
-        const int64_t from = at - z + series.begin(lo), to = at - z + series.end(lo);
-        (i ? plan.hi : plan.lo) = snap<G>(a, at, from, to);
-        if (i == 0) plan.first = {t, (int)head, lo, from, to};
+        const Segment s = segment_at(series, whole, t, start, at);
+        (i ? plan.hi : plan.lo) = snap<G>(a, at, s.start, s.end);
+        if (i == 0) plan.first = s;
       }
     }
   }
@@ -305,82 +197,16 @@ __device__ __forceinline__ Segment after(const ChunkArgs &a, const Plan &plan, c
   return r;
 }
 
-// Where a piece's keys lie, as Loader needs it.
-struct Source {
-  int row;              // cache slot whose pages are read
-  int head;             // KV head
-  int key0, limit;      // keys: first, and the sequence's tokens
-  int once;             // no other workgroup reads these keys
-};
-
-// A run of key tiles of one row tile in one workgroup; every field is wave-uniform.
-struct Piece {
-  Source src;
-  int t0, t1;           // tiles [t0, t1) of its keys that this row tile sees
-  int row0, rows;       // rows of the sequence and KV head: first, and how many (0: none)
-  int vis;              // keys that the sequence's first query sees (may be negative)
-  int here;             // the part has any of the segment's tiles, or its start if it has none
-  int begins, ends;     // the part has the segment's first tile, its last
-  int64_t last;         // last place of the segment's last tile
-  Segment s;
-};
-
-// The piece of a segment in the workgroup's part.
-template <class G>
-__device__ __forceinline__ Piece piece_of(const ChunkArgs &a, const Plan &plan, const Segment &s,
-                                          const Part &part) {
-  Piece r;
-  r.s = s;
-  const int len = uniform(plan.len[s.seq]), m = a.cu[s.seq + 1] - a.cu[s.seq];
-  const int rows = m * a.G, span = part.width * G::ROWS;
-  r.src.row = a.slot[s.seq];
-  r.src.head = s.head;
-  r.src.key0 = 0;
-  r.src.limit = len;
-  r.src.once = rows <= G::ROWS;
-  r.vis = len - m + 1;
-  // tiles that the segment's last row sees, and those in this part
-  const int tile = G::KEYS * a.G;
-  auto tiles_of = [&](int end) {
-    const int keys = len > 0 ? max(r.vis + (end - 1) / a.G, 0) : 0;
-    return (keys + G::KEYS - 1) / G::KEYS;
-  };
-  const int all = tiles_of(min((s.seg + 1) * span, rows));
-  const int64_t first = s.start + kSegCost * (int64_t)tile;
-  r.last = first + (int64_t)tile * all - 1;
-  const int t0 = part.lo <= first ? 0 : (int)min(divide(part.lo - first, tile), (int64_t)all);
-  const int t1 = part.hi >= s.end ? all
-                 : part.hi <= first ? 0 : (int)min(divide(part.hi - first, tile), (int64_t)all);
-  // (rows without a key belong to the part where they begin)
-  const bool here = all > 0 ? t0 < t1 : part.lo <= s.start;
-  r.row0 = s.seg * span + part.tile * G::ROWS;
-  r.rows = here ? max(min(rows - r.row0, G::ROWS), 0) : 0;
-  r.t0 = t0;
-  r.t1 = r.rows > 0 ? max(min(t1, tiles_of(r.row0 + r.rows)), t0) : t0;
-  r.here = here;
-  r.begins = t0 == 0;
-  r.ends = t1 == all;
-  return r;
-}
-
 // What the join needs: of a segment that goes on in later parts, how many pieces it has and its first part.
 // With `by_segment` there is a record for every segment, from the part that it begins in, else one for
 // every part, of the segment that begins in it and goes on.
 template <class G>
 __device__ __forceinline__ void record(const ChunkArgs &a, const Plan &plan, const Part &part, int parts,
                                        const Piece &p, bool last) {
-  const bool goes_on = p.here && p.begins && !p.ends;
-  int pieces = 0;
-  if (goes_on) {
-    // (a cut near the segment's end has moved there)
-    const int64_t near = (int64_t)kSnapTiles * G::KEYS * a.G;
-    const Cut cut(plan.start[kMaxList], parts);
-    pieces = cut.owner(min(p.last, p.s.end - near - 1)) - part.p + 1;
-  }
+  const int pieces = pieces_of<G>(a, plan.start[kMaxList], parts, part, p);
   const int4 rec = make_int4(pieces | part.p << 16, p.s.seq, p.s.head, p.s.seg);
   if (a.by_segment) {
-    const int n = Series<G>(a, a.width, a.cu[p.s.seq + 1] - a.cu[p.s.seq], 0).n;
-    if (p.here && p.begins) a.seg[a.base[p.s.seq] + p.s.head * n + p.s.seg] = rec;
+    if (p.here && p.begins) a.seg[record_of<G>(a, p)] = rec;
   } else if (last) {
     a.seg[part.p] = rec;
   }
@@ -504,7 +330,7 @@ void chunk_fwd(ChunkArgs a) {
   if (next.end <= part.lo) next = after<G>(a, plan, next);
   int worked = 1;
   while (true) {
-    s_piece[w] = piece_of<G>(a, plan, next, part);
+    s_piece[w] = piece_of<G>(a, next, uniform(plan.len[next.seq]), part);
     asm volatile("" ::: "memory");
     const Piece &me = s_piece[w];
     const Source src = {uniform(me.src.row), uniform(me.src.head), 0, uniform(me.src.limit),
@@ -714,7 +540,7 @@ void chunk_wide(ChunkArgs a) {
   if (next.end <= part.lo) next = after<G>(a, sh.plan, next);
   int worked = 1;
   while (true) {
-    sh.piece[w] = piece_of<G>(a, sh.plan, next, part);
+    sh.piece[w] = piece_of<G>(a, next, uniform(sh.plan.len[next.seq]), part);
     asm volatile("" ::: "memory");
     const Piece &me = sh.piece[w];
     const Source src = {uniform(me.src.row), uniform(me.src.head), 0, uniform(me.src.limit),
