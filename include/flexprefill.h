@@ -364,7 +364,8 @@ typedef struct fp_head_norm {
  * Hkv may be 0, and its pointers NULL.  An output may be its own input (same pointer and stride),
  * and must not overlap an input otherwise.  positions: int32 on the device, of any sign and size.
  * Computed in float32 and rounded once; cosines and sines are off by at most 2^-22 (times the
- * amplitude), whatever the position.  A NaN or an infinity stays within its head (norm) or its pair. */
+ * amplitude) from those of the position times the frequency, a float64 number, whatever both are.  A NaN
+ * or an infinity stays within its head (norm) or its pair. */
 fp_status fp_rotate(int32_t tokens, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
                     const void *q, int64_t q_stride, const void *k, int64_t k_stride,
                     const int32_t *positions, const fp_rope *rope, const fp_head_norm *norm,

@@ -357,6 +357,21 @@ fp_status check_decode(const fp_cache *c, const fp_decode *b, DecodeDims *dm) {
   return FP_OK;
 }
 
+// f / 2 pi without its whole turns, rounded to 2^-64; |f| <= 2^20.  f is a whole number of 53 bits times a
+// power of two; of its product with the first 128 bits of 1 / 2 pi less than 2^-95 of a turn is left out,
+// however many turns there are.
+uint64_t turn_fraction(double f) {
+  constexpr uint64_t kHigh = 0x28BE60DB9391054Aull, kLow = 0x7F09D5F47D4D3770ull;   // 2^128 / 2 pi
+  int e;
+  const uint64_t m = (uint64_t)(frexp(fabs(f), &e) * 9007199254740992.0);   // |f| = m 2^(e - 53)
+  // m 2^128 / 2 pi is t 2^64 and a word less; 2^64 |f| / 2 pi is t / 2^(53 - e)
+  const unsigned __int128 t =
+      (unsigned __int128)m * kHigh + (uint64_t)((unsigned __int128)m * kLow >> 64);
+  const int shift = 53 - e;              // 32 or more
+  const uint64_t x = shift > 127 ? 0 : (uint64_t)(((t >> (shift - 1)) + 1) >> 1);
+  return f < 0 ? 0 - x : x;
+}
+
 // The kernels' view of a rotation and of norms; either may be null.
 fp_status rope_args(const fp_rope *rope, const fp_head_norm *norm, int32_t d, fp::RopeArgs *r) {
   memset(r, 0, sizeof(*r));
@@ -868,7 +883,7 @@ fp_status fp_rope_init(const fp_rope_params *p, fp_rope *rope) {
          !(p->high_turns > p->low_turns) || !isfinite(p->high_turns)))
       return FP_ERR_INVALID_ARG;
   }
-  constexpr long double kTurn = 6.283185307179586476925286766559005768L;
+  constexpr double kTurn = 6.283185307179586476925;
   const double base =
       p->scaling == FP_ROPE_BASE ? p->base * pow(p->factor, (double)R / (R - 2)) : p->base;
   fp_rope r;
@@ -880,17 +895,13 @@ fp_status fp_rope_init(const fp_rope_params *p, fp_rope *rope) {
     double f = p->inv_freq ? p->inv_freq[i] : pow(base, -2.0 * i / R);
     if (!p->inv_freq && p->scaling == FP_ROPE_LINEAR) f /= p->factor;
     if (!p->inv_freq && p->scaling == FP_ROPE_PARTS) {
-      const double turns = p->original_len * f / (double)kTurn;
+      const double turns = p->original_len * f / kTurn;
       const double g =
           std::min(std::max((turns - p->low_turns) / (p->high_turns - p->low_turns), 0.0), 1.0);
       f = f * g + f / p->factor * (1 - g);
     }
     if (!(fabs(f) <= 1048576.0)) return FP_ERR_INVALID_ARG;
-    // the fraction of a turn, in 2^-64
-    long double turn = f / kTurn;
-    turn -= floorl(turn);
-    const long double scaled = rintl(turn * 18446744073709551616.0L);
-    r.step[i] = scaled >= 18446744073709551616.0L ? 0 : (uint64_t)scaled;
+    r.step[i] = turn_fraction(f);
   }
   *rope = r;
   return FP_OK;

@@ -5,8 +5,8 @@
 // position p with frequency f_i:
 //   (u, v) -> A (u cos p f_i - v sin p f_i, v cos p f_i + u sin p f_i).
 // All in float32, rounded once.  The angle is held as a fraction of a turn: p times round(2^64 f_i /
-// 2 pi), modulo 2^64, which no position can make less exact; its upper 32 bits give a quadrant and an
-// angle within pi / 4, of which sine and cosine are the Taylor series.
+// 2 pi), modulo 2^64, which is off by at most 2^-34 of a turn at any position; its upper 32 bits give a
+// quadrant and an angle within pi / 4, of which sine and cosine are the Taylor series.
 //
 // Memory bounds it: every head is read and written once, by 16-byte chunks, and nothing else is read but a
 // position a token (131072 tokens of 40 heads of 128 with norms 494 us, 5.4 TB/s; appends of 64k tokens 256
