@@ -35,6 +35,12 @@ namespace {
 
 constexpr int kJoinThreads = 256;
 
+// A score that is the reference of its row has a weight of 2^-kBelow.  No weight is then above 2^-26, and
+// those of the 2^26 tokens that a slot holds at most do not sum to more than 1: sums of the largest values of
+// their type stay within float32 until they are divided.  The smallest normal bf16 number is 2^-92 of the
+// reference's weight: keys that count less than that are lost.
+constexpr float kBelow = kLazy + 26.f;
+
 // Row tiles are not cut where the longest sequence has at most so many key tiles more than SHARES times a
 // workgroup's equal share of all of them (two, one for row tiles of 256): the device then hands out whole
 // row tiles, and whoever is done first takes the next.  Four whole prompts at head dim 64 720 -> 664 us, 59
@@ -423,9 +429,7 @@ void chunk_fwd(ChunkArgs a) {
       for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int v = 0; v < 16; ++v) mt = fmaxf(mt, sacc[i][v]);
-      // The reference moves only when a score rises 2^kLazy above it in weight, and has a weight of
-      // 2^-kLazy, so that no weight is above 1: sums of large values do not pass float32 before they
-      // are divided.
+      // The reference moves only when a score rises 2^kLazy above it in weight; its own weight is 2^-kBelow.
       if (__ballot(mt > m_trig)) {
         const float m_new = fmaxf(m_ref, wave_pair_max(mt));
         const float f = m_ref == m_new ? 1.f : __builtin_amdgcn_exp2f((m_ref - m_new) * c);
@@ -434,7 +438,7 @@ void chunk_fwd(ChunkArgs a) {
         for (int i = 0; i < DB; ++i) oacc[i] *= f;
         m_ref = m_new;
         const bool none = m_new == -INFINITY;
-        mc = none ? 0.f : fmaf(m_new, c, kLazy);
+        mc = none ? 0.f : fmaf(m_new, c, kBelow);
         m_trig = none ? -INFINITY : m_new + lazy_raw;
       }
       bf16x8 pf[4];
@@ -645,7 +649,7 @@ void chunk_wide(ChunkArgs a) {
           l_run *= alpha;
           m_ref = m_new;
           const bool none = m_new == -INFINITY;
-          mc = none ? 0.f : fmaf(m_new, c, kLazy);
+          mc = none ? 0.f : fmaf(m_new, c, kBelow);
           m_trig = none ? -INFINITY : m_new + lazy_raw;
           pending = moves;
         }
