@@ -26,8 +26,8 @@ def cache_append(cache: Cache, layer, q, k, v, slots, cu_seqlens, rope, norm=Non
     """cache_write of keys normed (where `norm` is given) and rotated (where `rope` is) on the way,
     each by its place in its slot, and of values as they are; the queries of the same tokens are normed
     and rotated into q_out, which is returned.  q: [T, Hq, d] or None, k, v: [T, Hkv, d], bf16, rows
-    contiguous; q_out may be q.  Where tokens are left out (see cache_write) so are their rows of
-    q_out."""
+    contiguous; q_out may be q.  Tokens beyond a slot's length, and all after a failed reserve, are left
+    out, their rows of q_out too; tokens of a page that is not the slot's alone only from the cache."""
     if _cache._device() != cache.index:
         return _there(cache, cache_append, cache, layer, q, k, v, slots, cu_seqlens, rope, norm,
                       q_out, stream)
@@ -82,8 +82,8 @@ def chunk_workspace_size(cache: Cache, batch: ChunkBatch) -> int:
 
 def chunk_attn(q, cache: Cache, layer, batch: ChunkBatch, out=None, workspace=None, stream=None):
     """Causal attention of the batch's new tokens over their sequences.  q: [T, Hq, d] bf16, rows
-    contiguous, sequence by sequence; returns o of the same shape.  The last bits of a row depend on
-    the rest of the batch."""
+    contiguous, sequence by sequence; returns o of the same shape.  Weights are rounded to 2^-8 of
+    themselves (decode_attn: 2^-16), and the last bits of a row depend on the rest of the batch."""
     if _cache._device() != cache.index:
         return _there(cache, chunk_attn, q, cache, layer, batch, out, workspace, stream)
     T, hq, d = batch.rows, batch.heads, cache.head_dim
