@@ -362,7 +362,9 @@ typedef struct fp_head_norm {
  * [tokens][Hkv][d] bf16, a token's heads contiguous, strides in elements from one token to the next
  * (>= heads * d, a multiple of 8; pointers 16-byte aligned); d in {64, 128}, rotary_dim <= d.  Hq or
  * Hkv may be 0, and its pointers NULL.  An output may be its own input (same pointer and stride),
- * and must not overlap an input otherwise.  positions: int32 on the device, of any sign and size.
+ * and must not overlap an input otherwise.  positions: int32 on the device, of any sign and size.  Up to
+ * 2^25 tokens, and 8192 heads of each kind.  A norm sums squares in float32, which those of elements below
+ * 2^60 stay within.
  * Computed in float32 and rounded once; cosines and sines are off by at most 2^-22 (times the
  * amplitude) from those of the position times the frequency, a float64 number, whatever both are.  A NaN
  * or an infinity stays within its head (norm) or its pair. */
@@ -376,7 +378,8 @@ fp_status fp_rotate(int32_t tokens, int32_t num_q_heads, int32_t num_kv_heads, i
  * queries of the same tokens are normed and rotated into q_out.  A token's position is its place in
  * the slot, so row cu[i] + j of a slot of n tokens has position n - (cu[i+1] - cu[i]) + j.  As in
  * fp_cache_write rows beyond a slot's length are left out (of q_out too), and nothing is done once
- * a reserve, fork or truncate has failed or been left out.  q, q_out: rows [Hq][d] bf16, strides,
+ * a reserve, fork or truncate has failed or been left out; keys and values of a page that other slots
+ * hold too are left out (FP_CACHE_SHARED), the queries of those tokens are written.  q, q_out: rows [Hq][d] bf16, strides,
  * alignment and overlap as in fp_rotate; q == NULL with Hq 0: keys and values alone.  rope and norm
  * may be NULL.  Takes up to 2^24 / (Hkv + 8) pieces of 64 tokens. */
 fp_status fp_cache_append(const fp_cache *cache, int32_t layer, int32_t n, const int32_t *slots,
@@ -403,7 +406,8 @@ fp_status fp_chunk_workspace_size(const fp_cache *cache, const fp_chunk *batch, 
  * sequence of n tokens attends to its keys 0 .. n - m + t.  Rows, strides and alignment of q and o, rows
  * without a key and what of the cache reaches a row are as in fp_decode_attn.  Slots may repeat.
  * Scores, maxima, sums and O are float32; the weights that multiply the values are rounded to bf16, 2^-8,
- * and the sum is that of the rounded weights.  The same call on the same state gives the same bits;
+ * and the sum is that of the rounded weights, as in fp_sparse_attn.  (fp_decode_attn rounds them to 2^-16
+ * over a sequence's own keys: the same token comes out coarser here.)  The same call on the same state gives the same bits;
  * where keys are cut into ranges follows from the lengths of the whole batch, so the last bits of a row
  * depend on the rest of it.  FP_ERR_UNSUPPORTED: more than 256 sequences, 8192 heads or 2^31 - 2^16 rows
  * (tokens times Hq / Hkv) of one sequence, or 5e14 places (rows / 128 times Hq times what a slot can hold). */

@@ -479,7 +479,9 @@ fp_status check_chunk(const fp_cache *c, const fp_chunk *b, ChunkDims *dm) {
   const double capacity = (double)c->max_pages * c->page;
   if ((double)dm->tiles * c->num_kv_heads * (dm->G * (capacity + 512) + (double)most) > 5e14)
     return FP_ERR_UNSUPPORTED;
-  // Eight waves where that leaves few rows of a tile empty, and clusters of as many row tiles as do.
+  // Row tiles of 256, in eight waves, where they take up at most 17/16 of the rows that tiles of 128 do.  A
+  // chunk over 60000 tokens, 4 query heads to each of 8 KV heads, in tiles of 128 and of 256, us: 9 tiles of
+  // 128 (10/9 of the rows) 289 and 301, 11 350 and 358, 15 466 and 464, 17 571 and 563, 20 628 and 604.
   const int64_t tiles_128 = dm->tiles;
   auto tiles_of = [&](int64_t span) {        // row tiles of 128 that tiles of `span` rows take up
     int64_t n = 0;
@@ -489,9 +491,11 @@ fp_status check_chunk(const fp_cache *c, const fp_chunk *b, ChunkDims *dm) {
   };
   dm->rows = c->head_dim == 128 && 16 * tiles_of(256) <= 17 * tiles_128 ? 256 : 128;
   dm->wgs = fp::decode_wgs(c->head_dim) / (dm->rows / 128);
-  // Clusters of the width that leaves the fewest row tiles and workgroups empty.  Narrow ones share fewer
-  // keys: 4096 tokens over 128k in row tiles of 256 take 8654, 8373 and 8309 us at widths 1, 4 and 8 (of
-  // 128: 9947, 9245, 8947), 200 over 120k (25 tiles of 128) 444, 438, 418 and 418 at 1, 2, 5 and 25.
+  // Clusters of the width that leaves the fewest row tiles and workgroups empty; narrow ones, which share
+  // fewer keys, count up to 5% less.  In row tiles of 256, us: 4096 tokens over 128k at widths 1, 2, 4, 8, 16
+  // 7580, 7600, 7750, 7740, 7610 (8 is taken; no more apart than runs are); 2048 over 30k, 56 tiles to each of
+  // 4 KV heads, 860, 876, 849, 846 (taken), 895; 200 over 120k, 13 tiles to each of 2, at 1, 2, 5, 7, 13 398,
+  // 424, 435, 411, 394 (taken).
   dm->width = 1;
   dm->row_tiles = tiles_of(dm->rows) / (dm->rows / 128);
   const int64_t tiles = dm->row_tiles, longest = (most + dm->rows - 1) / dm->rows;

@@ -26,8 +26,10 @@ class Rope:
     rotary_dim) radians per position, or by inv_freq[i].  layout "half": pairs (i, i + rotary_dim /
     2); "interleaved": (2 i, 2 i + 1).  scaling stretches the frequencies by `factor` for contexts
     longer than a model was made for: "linear", all of them; "base", by a larger base; "parts", those
-    that make fewer than high_turns turns in original_len positions, those below low_turns wholly.
-    amplitude multiplies cosines and sines."""
+    that make fewer than high_turns turns in original_len positions, those below low_turns wholly, by a
+    share that is linear in the turns.  (A share that is linear in the pair's number, between ends that
+    are rounded to whole pairs, is another rule, whose angles differ a little: such frequencies are given
+    as inv_freq.)  amplitude multiplies cosines and sines."""
 
     def __init__(self, rotary_dim, base=10000.0, layout="half", scaling=None, factor=1.0,
                  original_len=0, low_turns=1.0, high_turns=32.0, amplitude=1.0, inv_freq=None):
