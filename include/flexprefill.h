@@ -408,10 +408,11 @@ fp_status fp_chunk_workspace_size(const fp_cache *cache, const fp_chunk *batch, 
  * Scores, maxima, sums and O are float32; the weights that multiply the values are rounded to bf16, 2^-8,
  * and the sum is that of the rounded weights, as in fp_sparse_attn.  (fp_decode_attn rounds them to 2^-16
  * over a sequence's own keys: the same token comes out coarser here.)  Scores times the scale are to stay
- * below 2^29: from there on their rounding to float32 alone can make a row 0 or infinite.  The same call on the same state gives the same bits;
- * where keys are cut into ranges follows from the lengths of the whole batch, so the last bits of a row
- * depend on the rest of it.  FP_ERR_UNSUPPORTED: more than 256 sequences, 8192 heads or 2^31 - 2^16 rows
- * (tokens times Hq / Hkv) of one sequence, or 5e14 places (rows / 128 times Hq times what a slot can hold). */
+ * below 2^29: from there on their rounding to float32 alone can make a row 0 or infinite.
+ * The same call on the same state gives the same bits; where keys are cut into ranges follows from the
+ * lengths of the whole batch, so the last bits of a row depend on the rest of it.
+ * FP_ERR_UNSUPPORTED: more than 256 sequences, 8192 heads or 2^31 - 2^16 rows (tokens times Hq / Hkv) of
+ * one sequence, or 5e14 places (rows / 128 times Hq times what a slot can hold). */
 fp_status fp_chunk_attn(const fp_cache *cache, const fp_chunk *batch, int32_t layer, const void *q,
                         int64_t q_stride, void *o, void *ws, size_t ws_bytes, void *stream);
 
